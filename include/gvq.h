@@ -250,6 +250,91 @@ int gvq_basis_export_cov(const gvq_basis_t* h, double* cov, int64_t* n_samples);
 int gvq_basis_import(gvq_basis_t* h, const float* U, const float* mu);
 
 /*
+ * ---- Operators around an aggregated gradient: 4-bit layers that make it, and Muon's step that uses it ----
+ *
+ * Conventions as above, but without a handle: the caller owns every buffer, the workspace among them (device memory of the bytes
+ * that the _workspace call gives, 16-byte aligned, free again once the stream's work is done; its contents mean nothing between calls).
+ * Nothing is allocated, nothing waits.  Matrices are row-major with a row stride `ld` in elements, at least the number of columns;
+ * they need to be aligned to their elements only (whole 16-byte words are faster).  A size of 0 is a matrix without elements: GVQ_OK, and a
+ * sum over nothing is 0.  Sizes are at most GVQ_MX_MAX.  Inputs and outputs of one call do not overlap unless it says so.
+ */
+#define GVQ_MX_MAX 4194304   /* most rows or columns of a 4-bit matrix (2^22) */
+#define GVQ_MAX_STEPS 64     /* most Newton-Schulz steps of one call */
+
+/*
+ * Microscaled 4-bit matrices.  32 consecutive numbers of a row share one scale s = 2^(floor(log2 m) - 2), m their largest magnitude
+ * (at least 2^-127), and each is kept as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times s, with its sign; ties go to the even code (0, 1, 2, 4),
+ * what lies above 6 s becomes 6 s.  A block that holds an infinity or a NaN is NaN throughout.
+ *   codes  : [rows][64 ceil(cols/128)] bytes, column 2 i in the low and 2 i + 1 in the high half of byte i; bit 3 is the sign, bits
+ *            0..2 count the magnitudes above; columns behind the last one are 0;
+ *   scales : [rows][4 ceil(cols/128)] bytes, s = 2^(byte - 127), 255 = NaN.
+ * Their sizes, or GVQ_EINVAL.
+ */
+int64_t gvq_mx_code_bytes(int64_t rows, int64_t cols);
+int64_t gvq_mx_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * x [rows][cols] -> blocks along its rows (codes, scales) and / or along its columns (codes_t, scales_t: the 4-bit matrix of x's
+ * transpose, cols rows of rows numbers), in one pass; either pair may be NULL.  noise: NULL, or device bytes [rows][cols] with row
+ * stride noise_ld, uniformly random: a number between two neighbours becomes the upper one (in magnitude) if the fraction of the
+ * way there is above (noise + 1/2) / 256, which makes the rounding unbiased to 1/512 of the distance; both directions use the same byte.
+ */
+int gvq_mx_quantize(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld, const void* noise, int64_t noise_ld,
+                    void* codes, void* scales, void* codes_t, void* scales_t, void* stream);
+
+/* The values that codes and scales stand for (exact, but for what bf16 cannot hold: below 2^-126 and above its largest). */
+int gvq_mx_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, gvq_dtype_t out_dtype, int64_t ld,
+                      void* stream);
+
+/*
+ * out [m][n] = A B^T (accumulate != 0: out + A B^T), A [m][k] and B [n][k] 4-bit matrices with blocks along k.  Exact products, fp32
+ * sums, rounded once to out_dtype.
+ */
+int gvq_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n, int64_t k,
+                  void* out, gvq_dtype_t out_dtype, int64_t ld, int accumulate, void* stream);
+
+/*
+ * A layer with a 4-bit weight: y [rows][n_out] = Q(x) W^T, x [rows][n_in] quantised on the way, W [n_out][n_in] in codes and scales.
+ * Any number of rows, from one token on.
+ */
+int64_t gvq_mx_linear_workspace(int64_t rows, int64_t n_in);
+int gvq_mx_linear(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const void* w_scales,
+                  int64_t n_out, void* y, gvq_dtype_t y_dtype, int64_t ld_y, void* workspace, void* stream);
+
+/*
+ * Its gradients.  dx [rows][n_in] = Q(dy) Q(W), blocks along n_out: wt_codes, wt_scales hold W's transpose ([n_in][n_out], the second
+ * pair of gvq_mx_quantize); dw [n_out][n_in] = Q(dy^T) Q(x^T)^T (accumulate != 0: added to dw), blocks along rows.  noise (may be
+ * NULL) rounds dy stochastically in both.  dx or dw may be NULL; what only it needs is then not looked at.
+ */
+int64_t gvq_mx_linear_backward_workspace(int64_t rows, int64_t n_in, int64_t n_out);
+int gvq_mx_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
+                           int64_t n_out, const void* noise, int64_t noise_ld, const void* wt_codes, const void* wt_scales, void* dx,
+                           gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate,
+                           void* workspace, void* stream);
+
+/*
+ * Newton-Schulz orthogonalisation of `batch` matrices [rows][cols], `stride` elements apart (out: stride_out): X = g / (|g|_F + eps),
+ * then `steps` times X <- a X + (b A + c A A) X, A = X X^T (of the shorter side; at most GVQ_MAX_STEPS), which drives every singular value
+ * towards 1 and keeps the singular vectors.  coef: host array [steps][3] of a, b, c, or NULL for 3.4445, -4.7750, 2.0315 in every step.
+ * Products of 22-bit numbers with fp32 sums, about fp32's accuracy, for |X| < 16, |b A + c A A| < 64 (entries; the default
+ * polynomial keeps them below 1.3 and 7).  A zero matrix gives zero; an infinity or a NaN makes its whole matrix NaN.  At most 2^30 numbers
+ * (rows and columns rounded up to 32) and 2^20 rows or columns per matrix, 65535 matrices.  out may be g.
+ */
+int64_t gvq_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols);
+int gvq_orthogonalize(const void* g, gvq_dtype_t dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                      const double* coef, int steps, double eps, void* out, gvq_dtype_t out_dtype, int64_t ld_out, int64_t stride_out,
+                      void* workspace, void* stream);
+
+/*
+ * One step of Muon on a weight matrix: momentum <- beta momentum + grad; U = nesterov ? grad + beta momentum : momentum;
+ * weight <- (1 - lr weight_decay) weight - lr scale O, O = U orthogonalised as above.  weight (fp32 or bf16) and momentum (fp32) are
+ * updated in place.  workspace: gvq_orthogonalize_workspace(1, rows, cols) bytes.
+ */
+int gvq_muon_step(void* weight, gvq_dtype_t weight_dtype, int64_t ld_weight, const void* grad, gvq_dtype_t grad_dtype, int64_t ld_grad,
+                  float* momentum, int64_t ld_momentum, int64_t rows, int64_t cols, double lr, double beta, double weight_decay,
+                  int nesterov, double scale, const double* coef, int steps, double eps, void* workspace, void* stream);
+
+/*
  * Text for a status code.  For GVQ_EHIP the text includes the message of the most recent
  * failed HIP call in this process.  The pointer stays valid until the next call.
  */

@@ -1,0 +1,38 @@
+// Newton-Schulz orthogonalisation and the Muon step: launchers (host side).
+#pragma once
+#include "gvq_internal.h"
+
+struct MuonMatrix {
+    int64_t batch, rows, cols;
+};
+
+struct MuonPlan {   // where things lie in a workspace, in bytes
+    int64_t ldc, ldr, ldm;        // padded row lengths in numbers: of natural, transposed and square planes
+    int64_t nat[2], tr[2], gram, poly, sums;
+    int64_t per;                  // bytes of one matrix's planes
+    int64_t bytes;                // of the whole workspace
+    int parts;                    // partial sums of squares of a matrix
+};
+// false: the sizes are out of range.
+bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p);
+
+struct MuonArgs {
+    MuonMatrix x;
+    const void* grad;
+    gvq_dtype_t grad_dtype;
+    int64_t ld_grad, stride_grad;    // elements
+    float* momentum;                 // null: orthogonalise the gradient itself
+    int64_t ld_momentum;
+    float beta;
+    int nesterov;
+    const double* coef;              // host [steps][3], null: the default
+    int steps;
+    double eps;
+    void* out;                       // decay == null ? the result : the weight
+    gvq_dtype_t out_dtype;
+    int64_t ld_out, stride_out;
+    int update;                      // 0: out = X, 1: out = keep * out - rate * X
+    float keep, rate;
+    char* workspace;
+};
+int gvq_launch_muon(const MuonArgs& a, hipStream_t st);

@@ -16,6 +16,8 @@ F32, BF16 = 0, 1
 OK, EINVAL, EALIGN, ENOTFIT, EHIP, ENOMEM, ENONFINITE, ENOCONV, ETOOBIG = 0, -1, -2, -3, -4, -5, -6, -7, -8
 STATIC_MAX_SLICES = 1 << 21
 MAX_D = 1024
+MX_MAX = 1 << 22
+MAX_STEPS = 64
 
 _lib = None
 
@@ -65,11 +67,26 @@ def lib():
         L.gvq_strerror.argtypes = [i32]
         L.gvq_strerror.restype = C.c_char_p
         L.gvq_set_option.argtypes = [i32, i32]
+        L.gvq_mx_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp]
+        L.gvq_mx_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+        L.gvq_mx_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i32, i64, i32, vp]
+        L.gvq_mx_linear.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp, vp]
+        L.gvq_mx_linear_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, i64, vp, vp, vp, i32, i64, vp, i32, i64, i32,
+                                             vp, vp]
+        f64 = C.c_double
+        L.gvq_orthogonalize.argtypes = [vp, i32, i64, i64, i64, i64, i64, vp, i32, f64, vp, i32, i64, i64, vp, vp]
+        L.gvq_muon_step.argtypes = [vp, i32, i64, vp, i32, i64, vp, i64, i64, i64, f64, f64, f64, i32, f64, vp, i32, f64, vp, vp]
+        for name, n in (("gvq_mx_code_bytes", 2), ("gvq_mx_scale_bytes", 2), ("gvq_mx_linear_workspace", 2),
+                        ("gvq_mx_linear_backward_workspace", 3), ("gvq_orthogonalize_workspace", 3)):
+            getattr(L, name).argtypes = [i64] * n
+            getattr(L, name).restype = i64
         for name in ("gvq_basis_create", "gvq_basis_destroy", "gvq_fit_basis", "gvq_fit_status",
                      "gvq_compress", "gvq_aggregate", "gvq_decompress", "gvq_basis_export",
                      "gvq_basis_export_cov", "gvq_basis_import", "gvq_set_option", "gvq_local_loss",
                      "gvq_select_k", "gvq_compress_segment", "gvq_decompress_segment", "gvq_flatten_conv",
-                     "gvq_unflatten_conv", "gvq_fit_basis_first_slice", "gvq_local_loss_static"):
+                     "gvq_unflatten_conv", "gvq_fit_basis_first_slice", "gvq_local_loss_static", "gvq_mx_quantize",
+                     "gvq_mx_dequantize", "gvq_mx_matmul", "gvq_mx_linear", "gvq_mx_linear_backward", "gvq_orthogonalize",
+                     "gvq_muon_step"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -105,6 +122,12 @@ def _stream(stream):
 def _check(status, where):
     if status != OK:
         raise GvqError(status, where)
+
+
+def _size(n, where):
+    if n < 0:
+        raise GvqError(int(n), where)
+    return n
 
 
 # ---- the C entry points, same names, raw arguments ---------------------------------------
@@ -195,6 +218,66 @@ def gvq_select_k(h, lam, n_bases, stream=None):
 
 def gvq_set_option(option, value):
     _check(lib().gvq_set_option(int(option), int(value)), "gvq_set_option")
+
+
+def gvq_mx_code_bytes(rows, cols):
+    return _size(lib().gvq_mx_code_bytes(rows, cols), "gvq_mx_code_bytes")
+
+
+def gvq_mx_scale_bytes(rows, cols):
+    return _size(lib().gvq_mx_scale_bytes(rows, cols), "gvq_mx_scale_bytes")
+
+
+def gvq_mx_quantize(x, dtype, rows, cols, ld, noise, noise_ld, codes, scales, codes_t, scales_t, stream=None):
+    _check(lib().gvq_mx_quantize(_ptr(x), dtype, rows, cols, ld, _ptr(noise), noise_ld, _ptr(codes), _ptr(scales), _ptr(codes_t),
+                                 _ptr(scales_t), _stream(stream)), "gvq_mx_quantize")
+
+
+def gvq_mx_dequantize(codes, scales, rows, cols, out, out_dtype, ld, stream=None):
+    _check(lib().gvq_mx_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), out_dtype, ld, _stream(stream)),
+           "gvq_mx_dequantize")
+
+
+def gvq_mx_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, out_dtype, ld, accumulate=False, stream=None):
+    _check(lib().gvq_mx_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, _ptr(out), out_dtype, ld,
+                               accumulate, _stream(stream)), "gvq_mx_matmul")
+
+
+def gvq_mx_linear_workspace(rows, n_in):
+    return _size(lib().gvq_mx_linear_workspace(rows, n_in), "gvq_mx_linear_workspace")
+
+
+def gvq_mx_linear(x, dtype, rows, n_in, ld_x, w_codes, w_scales, n_out, y, y_dtype, ld_y, workspace, stream=None):
+    _check(lib().gvq_mx_linear(_ptr(x), dtype, rows, n_in, ld_x, _ptr(w_codes), _ptr(w_scales), n_out, _ptr(y), y_dtype, ld_y,
+                               _ptr(workspace), _stream(stream)), "gvq_mx_linear")
+
+
+def gvq_mx_linear_backward_workspace(rows, n_in, n_out):
+    return _size(lib().gvq_mx_linear_backward_workspace(rows, n_in, n_out), "gvq_mx_linear_backward_workspace")
+
+
+def gvq_mx_linear_backward(dy, ld_dy, x, ld_x, dtype, rows, n_in, n_out, noise, noise_ld, wt_codes, wt_scales, dx, dx_dtype, ld_dx,
+                           dw, dw_dtype, ld_dw, accumulate, workspace, stream=None):
+    _check(lib().gvq_mx_linear_backward(_ptr(dy), ld_dy, _ptr(x), ld_x, dtype, rows, n_in, n_out, _ptr(noise), noise_ld,
+                                        _ptr(wt_codes), _ptr(wt_scales), _ptr(dx), dx_dtype, ld_dx, _ptr(dw), dw_dtype, ld_dw,
+                                        accumulate, _ptr(workspace), _stream(stream)), "gvq_mx_linear_backward")
+
+
+def gvq_orthogonalize_workspace(batch, rows, cols):
+    return _size(lib().gvq_orthogonalize_workspace(batch, rows, cols), "gvq_orthogonalize_workspace")
+
+
+def gvq_orthogonalize(g, dtype, batch, rows, cols, ld, stride, coef, steps, eps, out, out_dtype, ld_out, stride_out, workspace,
+                      stream=None):
+    _check(lib().gvq_orthogonalize(_ptr(g), dtype, batch, rows, cols, ld, stride, _ptr(coef), steps, eps, _ptr(out), out_dtype, ld_out,
+                                   stride_out, _ptr(workspace), _stream(stream)), "gvq_orthogonalize")
+
+
+def gvq_muon_step(weight, weight_dtype, ld_weight, grad, grad_dtype, ld_grad, momentum, ld_momentum, rows, cols, lr, beta,
+                  weight_decay, nesterov, scale, coef, steps, eps, workspace, stream=None):
+    _check(lib().gvq_muon_step(_ptr(weight), weight_dtype, ld_weight, _ptr(grad), grad_dtype, ld_grad, _ptr(momentum), ld_momentum,
+                               rows, cols, lr, beta, weight_decay, nesterov, scale, _ptr(coef), steps, eps, _ptr(workspace),
+                               _stream(stream)), "gvq_muon_step")
 
 
 class Basis:
