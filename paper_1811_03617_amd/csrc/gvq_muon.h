@@ -6,12 +6,20 @@ struct MuonMatrix {
     int64_t batch, rows, cols;
 };
 
+// Which tiles a product takes, and in how many parts its sum is cut.
+struct NsChoice {
+    int shape = 0, splits = 1;
+};
+
 struct MuonPlan {   // where things lie in a workspace, in bytes
-    int64_t ldc, ldr, ldm;        // padded row lengths in numbers: of natural, transposed and square planes
-    int64_t nat[2], tr[2], gram, poly, sums;
+    int64_t m, n;                 // shorter and longer side: X is kept as m rows of n numbers
+    int64_t ldn, ldm;             // padded row lengths in numbers
+    int64_t x[2], gram, poly;     // of one matrix: two planes each
     int64_t per;                  // bytes of one matrix's planes
+    int64_t sums, parts_at;       // partial sums of squares; partial products
     int64_t bytes;                // of the whole workspace
     int parts;                    // partial sums of squares of a matrix
+    NsChoice gram_by, poly_by, step_by;
 };
 // false: the sizes are out of range.
 bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p);

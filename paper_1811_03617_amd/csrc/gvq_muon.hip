@@ -26,9 +26,10 @@ struct PrepArgs {
     double* sums;        // [batch][parts]
     int parts;
     double eps;
-    char* ws;
-    int64_t per;
-    int64_t nat, tr, ldc, ldr;
+    char* x;             // planes of the first matrix, `per` bytes further for each next one
+    int64_t per, plane;  // plane: numbers
+    int64_t ld;
+    int turn;            // more rows than columns: X is the transpose
 };
 
 template <typename G>
@@ -81,7 +82,8 @@ __device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo)
     lo = (_Float16)(v - (float)hi);
 }
 
-// U / (|U| + eps) into the planes of both orientations, with zeros behind the last column: 64 x 64 numbers a work-group.
+// U / (|U| + eps) into the two planes of X, with zeros behind the last column: 64 x 64 numbers a work-group, through LDS if X is
+// the transpose.
 template <typename G>
 __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
 {
@@ -91,11 +93,15 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
     for (int i = threadIdx.x; i < a.parts; i += MUON_THREADS) s += a.sums[blockIdx.z * a.parts + i];
     const double inv = 1.0 / (sqrt(group_sum(s, lds)) + a.eps) * UNIT_X;
     const G* g = (const G*)a.grad + blockIdx.z * a.stride_grad;
-    char* ws = a.ws + blockIdx.z * a.per;
+    _Float16* X = (_Float16*)(a.x + blockIdx.z * a.per);
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
     const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
-    _Float16* nat = (_Float16*)(ws + a.nat);
-    _Float16* tr = (_Float16*)(ws + a.tr);
+    auto put = [&](int64_t at, float v) {
+        _Float16 hi, lo;
+        split_f16(v, hi, lo);
+        X[at] = hi;
+        X[a.plane + at] = lo;
+    };
 #pragma unroll 4
     for (int y = y0; y < 64; y += MUON_THREADS / 64) {
         const int64_t r = r0 + y, c = c0 + x;
@@ -108,24 +114,15 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
             }
             v = (float)((double)u * inv);
         }
-        tile[y * 65 + x] = v;
-        if (r < a.rows && c < a.ldc) {
-            _Float16 hi, lo;
-            split_f16(v, hi, lo);
-            nat[r * a.ldc + c] = hi;
-            nat[a.rows * a.ldc + r * a.ldc + c] = lo;
-        }
+        if (a.turn) tile[y * 65 + x] = v;
+        else if (r < a.rows && c < a.ld) put(r * a.ld + c, v);
     }
+    if (!a.turn) return;
     __syncthreads();
 #pragma unroll 4
     for (int y = y0; y < 64; y += MUON_THREADS / 64) {
         const int64_t c = c0 + y, r = r0 + x;
-        if (c < a.cols && r < a.ldr) {
-            _Float16 hi, lo;
-            split_f16(tile[x * 65 + y], hi, lo);
-            tr[c * a.ldr + r] = hi;
-            tr[a.cols * a.ldr + c * a.ldr + r] = lo;
-        }
+        if (c < a.cols && r < a.ld) put(c * a.ld + r, tile[x * 65 + y]);
     }
 }
 
@@ -134,14 +131,17 @@ enum { NS_GRAM = 0, NS_POLY = 1, NS_STEP = 2, NS_LAST = 3 };
 
 struct NsArgs {
     TileOperand a, b;          // of the first matrix; `per` bytes further for each next one
-    int steps, nm, nn, band;
+    int steps, nm, nn, band;   // steps of 32 numbers of the sum; tiles, and how they are swept
+    int rows, cols;            // of the result
     int64_t per;
     float scale;               // of the sum, in units of the result
     float ca, cb;              // POLY: result = ca old + cb sum; STEP, LAST: ca old + sum
-    const _Float16* old;       // POLY: A, STEP and LAST: X, in natural layout
-    int64_t old_plane;
-    _Float16 *nat, *tr;        // results (POLY, GRAM: tr == nat, mirrored)
-    int64_t nat_plane, tr_plane, ldn, ldt;
+    const _Float16* old;       // POLY: A, STEP and LAST: X
+    _Float16* res;             // result (not LAST)
+    int64_t plane, ld;         // of old and res, in numbers
+    float* parts;              // splits > 1: [matrix][split][ldp rows][ldp_cols]
+    int64_t ld_part, part;     // numbers of a row, of a split
+    int splits;
     void* out;                 // LAST
     int64_t ld_out, stride_out;
     int update, words;
@@ -178,45 +178,70 @@ __device__ __forceinline__ void last_store4<unsigned short>(unsigned short* p, b
     }
 }
 
-// Four neighbouring results of row r from column c on into the planes: natural, and transposed (or mirrored).
-__device__ __forceinline__ void store_planes(const NsArgs& a, _Float16* nat, _Float16* tr, int r, int c, int rows, int cols, bool turn, f4 v)
+// What becomes of four neighbouring sums of row r from column c on (FLIP: of four rows from r on in column c).  a X is added here and
+// not as a I to the polynomial, which would save reading X a second time: in the product it would be the largest term by far of a
+// sum that is rounded every 32 numbers (1024 x 1024 of planted low rank: 2.5e-5 off instead of 1.1e-5).
+template <int KIND, bool FLIP>
+__device__ __forceinline__ f4 ns_value4(const NsArgs& a, const _Float16* old, int r, int c, f4 v)
 {
-    h4 hi, lo;
+    v *= a.scale;
+    if (KIND == NS_GRAM) return v;
+    f4 o;
+    if (!FLIP) {
+        const h4 hi = *(const h4*)(old + r * a.ld + c), lo = *(const h4*)(old + a.plane + r * a.ld + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        _Float16 h, l;
-        split_f16(c + i < cols && r < rows ? v[i] : 0.f, h, l);
-        hi[i] = h; lo[i] = l;
-    }
-    if (r < rows && c < a.ldn) {
-        *(h4*)(nat + (int64_t)r * a.ldn + c) = hi;
-        *(h4*)(nat + a.nat_plane + (int64_t)r * a.ldn + c) = lo;
-    }
-    if (turn && r < a.ldt) {
+        for (int i = 0; i < 4; ++i) o[i] = (float)hi[i] + (float)lo[i];
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < cols) {
-                tr[(int64_t)(c + i) * a.ldt + r] = hi[i];
-                tr[a.tr_plane + (int64_t)(c + i) * a.ldt + r] = lo[i];
-            }
+        for (int i = 0; i < 4; ++i) o[i] = r + i < a.rows ? (float)old[(r + i) * a.ld + c] + (float)old[a.plane + (r + i) * a.ld + c] : 0.f;
     }
+    return a.ca * o + (KIND == NS_POLY ? a.cb * v : v);
 }
 
-// KIND: which product; GRAM and POLY compute the tiles on and above the diagonal and mirror them.
-template <typename T, int KIND, typename OUT>
+// Upper triangle of tiles, column by column: column tn holds the tiles (0 .. tn, tn), tn (tn + 1) / 2 of them before it.
+__device__ __forceinline__ void triangle_at(int t, int& tm, int& tn)
+{
+    tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while (tn * (tn + 1) / 2 > t) --tn;
+    while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
+    tm = t - tn * (tn + 1) / 2;
+}
+
+// LDS of a wave that hands its tile out through it (one plane, rows padded by 8 numbers), and of a work-group.
+template <typename T>
+__host__ __device__ constexpr int ns_wave_lds()
+{
+    const int R = T::BM / T::WM, C = T::BN / T::WN;
+    return 2 * (R * (C + 8) > C * (R + 8) ? R * (C + 8) : C * (R + 8));
+}
+template <typename T>
+constexpr int ns_lds()
+{
+    static_assert(ns_wave_lds<T>() * T::WAVES <= 160 * 1024 && ns_wave_lds<T>() % 16 == 0, "LDS of a compute unit");
+    return T::LDS > ns_wave_lds<T>() * T::WAVES ? T::LDS : ns_wave_lds<T>() * T::WAVES;
+}
+
+// KIND: which product; GRAM and POLY compute the tiles on and above the diagonal and mirror them.  With SPLIT a work-group
+// leaves its part of the sum for ns_join_kernel.
+template <typename T, int KIND, typename OUT, bool SPLIT>
 __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
 {
     extern __shared__ char lds[];
-    int tm, tn;
-    if (KIND == NS_GRAM || KIND == NS_POLY) {
-        // column tn of the triangle holds the tiles (0 .. tn, tn), tn (tn + 1) / 2 of them before it
-        const int t = tile_of_block(blockIdx.x, a.nm * (a.nm + 1) / 2);
-        tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-        while (tn * (tn + 1) / 2 > t) --tn;
-        while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
-        tm = t - tn * (tn + 1) / 2;
+    constexpr bool SYM = KIND == NS_GRAM || KIND == NS_POLY;
+    const int tiles = SYM ? a.nm * (a.nm + 1) / 2 : a.nm * a.nn;
+    int tm, tn, split = 0, step0 = 0, steps = a.steps;
+    if (SPLIT) {
+        // the tiles of one part side by side on one XCD: they share its rows' bytes
+        const int t = tile_of_block(blockIdx.x, tiles * a.splits);
+        split = t / tiles;
+        step0 = (int)((int64_t)a.steps * split / a.splits);
+        steps = (int)((int64_t)a.steps * (split + 1) / a.splits) - step0;
+        if (SYM) triangle_at(t - split * tiles, tm, tn);
+        else tile_at(t - split * tiles, a.nm, a.nn, a.band, tm, tn);
+    } else if (SYM) {
+        triangle_at(tile_of_block(blockIdx.x, tiles), tm, tn);
     } else {
-        tile_at(tile_of_block(blockIdx.x, a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
+        tile_at(tile_of_block(blockIdx.x, tiles), a.nm, a.nn, a.band, tm, tn);
     }
     const int64_t off = blockIdx.y * a.per;
     TileOperand A = a.a, B = a.b;
@@ -227,109 +252,305 @@ __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
     for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = f4{0.f, 0.f, 0.f, 0.f};
-    tile_product<T>(A, B, tm * T::BM, tn * T::BN, 0, a.steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = tm * T::BM + wave / T::WN * (T::BM / T::WM) + (lane & 15);
-    const int c0 = tn * T::BN + wave % T::WN * (T::BN / T::WN) + 4 * (lane >> 4);
-    _Float16* nat = (_Float16*)((char*)a.nat + off);
-    _Float16* tr = (_Float16*)((char*)a.tr + off);
+    tile_product<T>(A, B, tm * T::BM, tn * T::BN, step0, steps, lds, acc);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    constexpr int R = T::BM / T::WM, C = T::BN / T::WN;   // of a wave
+    const int rw = tm * T::BM + wave / T::WN * R, cw = tn * T::BN + wave % T::WN * C;
+    if (SPLIT) {
+        float* p = a.parts + ((int64_t)blockIdx.y * a.splits + split) * a.part;
+#pragma unroll
+        for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni)
+                *(f4*)(p + (rw + 16 * mi + (lane & 15)) * a.ld_part + cw + 16 * ni + 4 * (lane >> 4)) = acc[mi][ni];
+        return;
+    }
     const _Float16* old = (const _Float16*)((const char*)a.old + off);
+    if constexpr (KIND == NS_LAST) {
+        OUT* out = (OUT*)a.out + blockIdx.y * a.stride_out;
 #pragma unroll
-    for (int mi = 0; mi < T::MI; ++mi) {
-        const int r = r0 + 16 * mi;
+        for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
-        for (int ni = 0; ni < T::NI; ++ni) {
-            const int c = c0 + 16 * ni;
-            f4 v = acc[mi][ni] * a.scale;
-            if (KIND != NS_GRAM && r < A.rows && c < a.ldn) {
-                const h4 hi = *(const h4*)(old + (int64_t)r * a.ldn + c), lo = *(const h4*)(old + a.old_plane + (int64_t)r * a.ldn + c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = a.ca * ((float)hi[i] + (float)lo[i]) + (KIND == NS_POLY ? a.cb * v[i] : v[i]);
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const int r = rw + 16 * mi + (T::FLIP ? 4 * (lane >> 4) : lane & 15), c = cw + 16 * ni + (T::FLIP ? lane & 15 : 4 * (lane >> 4));
+                if (r >= a.rows || c >= a.cols) continue;
+                const f4 v = ns_value4<KIND, T::FLIP>(a, old, r, c, acc[mi][ni]) * (1.f / UNIT_X);
+                OUT* to = T::FLIP ? out + (int64_t)c * a.ld_out + r : out + (int64_t)r * a.ld_out + c;
+                last_store4<OUT>(to, a.words != 0, T::FLIP ? a.rows - r : a.cols - c, a.update, a.keep, a.rate, v);
             }
-            if (KIND == NS_LAST) {
-                if (r < A.rows && c < B.rows)
-                    last_store4<OUT>((OUT*)a.out + blockIdx.y * a.stride_out + (int64_t)r * a.ld_out + c, a.words != 0, B.rows - c, a.update,
-                                     a.keep, a.rate, v * (1.f / UNIT_X));
-            } else {
-                store_planes(a, nat, tr, r, c, A.rows, B.rows, KIND == NS_STEP || tm != tn, v);
+    } else {
+        // Into the planes, and for a tile above the diagonal into its mirror image: through the wave's share of LDS, so that rows
+        // leave in 16-byte words side by side.  Each wave reads what it wrote itself; only the last products' reads of the
+        // others have to be over first.
+        _Float16* res = (_Float16*)((char*)a.res + off);
+        constexpr int NP = C + 8, TP = R + 8;   // padded rows: neighbours in different banks
+        _Float16* w = (_Float16*)(lds + wave * ns_wave_lds<T>());
+#pragma unroll
+        for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const int r = rw + 16 * mi + (lane & 15), c = cw + 16 * ni + 4 * (lane >> 4);
+                f4 v = {0.f, 0.f, 0.f, 0.f};
+                if (r < a.rows && c < a.ld) v = ns_value4<KIND, false>(a, old, r, c, acc[mi][ni]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c + i >= a.cols) v[i] = 0.f;
+                acc[mi][ni] = v;
             }
+        __syncthreads();
+#pragma unroll 1
+        for (int pl = 0; pl < 2; ++pl) {   // the first term, then what is left of each number
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) {
+                    h4 q;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[i] = (_Float16)acc[mi][ni][i];
+                    *(h4*)(w + (16 * mi + (lane & 15)) * NP + 16 * ni + 4 * (lane >> 4)) = q;
+                }
+            wave_lds_sync();
+            for (int i = lane; i < R * (C / 8); i += 64) {
+                const int r = i / (C / 8), c = i % (C / 8) * 8;
+                if (rw + r < a.rows && cw + c < a.ld) *(u4*)(res + (rw + r) * a.ld + cw + c) = *(const u4*)(w + r * NP + c);
+            }
+            wave_lds_sync();
+            if (SYM && tm != tn) {
+#pragma unroll
+                for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < T::NI; ++ni)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            w[(16 * ni + 4 * (lane >> 4) + i) * TP + 16 * mi + (lane & 15)] = (_Float16)acc[mi][ni][i];
+                wave_lds_sync();
+                for (int i = lane; i < C * (R / 8); i += 64) {
+                    const int c = i / (R / 8), r = i % (R / 8) * 8;
+                    // (a tile left of the last tile column has whole rows)
+                    if (cw + c < a.cols) *(u4*)(res + (cw + c) * a.ld + rw + r) = *(const u4*)(w + c * TP + r);
+                }
+                wave_lds_sync();
+            }
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[mi][ni][i] -= (float)(_Float16)acc[mi][ni][i];
+            res += a.plane;
+        }
+    }
+}
+
+// The parts of a sum added up in their order, and what the product's own kernel does with a sum otherwise: 32 x 32 results a
+// work-group, on and above the diagonal where the result is symmetric.  TURN: LAST writes the transpose.
+template <int KIND, typename OUT, bool TURN>
+__global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a)
+{
+    constexpr bool SYM = KIND == NS_GRAM || KIND == NS_POLY;
+    __shared__ float tile[32 * 36];
+    int tm, tn;
+    if (SYM) triangle_at(blockIdx.x, tm, tn);
+    else { tm = blockIdx.x / a.nn; tn = blockIdx.x - tm * a.nn; }
+    const int64_t off = blockIdx.y * a.per;
+    const int y = threadIdx.x >> 3, x = 4 * (threadIdx.x & 7), r = tm * 32 + y, c = tn * 32 + x;
+    const float* p = a.parts + (int64_t)blockIdx.y * a.splits * a.part + r * a.ld_part + c;
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) v += *(const f4*)(p + s * a.part);
+    const _Float16* old = (const _Float16*)((const char*)a.old + off);
+    const bool in = r < a.rows && c < a.ld;
+    if (in) v = ns_value4<KIND, false>(a, old, r, c, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!in || c + i >= a.cols) v[i] = 0.f;
+    if (KIND == NS_LAST) v *= 1.f / UNIT_X;
+    if (KIND == NS_LAST && !TURN) {
+        if (in && c < a.cols)
+            last_store4<OUT>((OUT*)a.out + blockIdx.y * a.stride_out + (int64_t)r * a.ld_out + c, a.words != 0, a.cols - c, a.update, a.keep, a.rate, v);
+        return;
+    }
+    _Float16* res = (_Float16*)((char*)a.res + off);
+    auto put = [&](int64_t at, f4 v) {
+        h4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            _Float16 h, l;
+            split_f16(v[i], h, l);
+            hi[i] = h; lo[i] = l;
+        }
+        *(h4*)(res + at) = hi;
+        *(h4*)(res + a.plane + at) = lo;
+    };
+    if (KIND != NS_LAST && in) put(r * a.ld + c, v);
+    if ((SYM && tm != tn) || KIND == NS_LAST) {
+        // the other way round: row c + .. of four neighbouring r
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tile[(x + i) * 36 + y] = v[i];
+        __syncthreads();
+        const int c2 = tn * 32 + y, r2 = tm * 32 + x;
+        const f4 w = *(const f4*)(tile + y * 36 + x);
+        if (KIND == NS_LAST) {
+            if (c2 < a.cols && r2 < a.rows)
+                last_store4<OUT>((OUT*)a.out + blockIdx.y * a.stride_out + (int64_t)c2 * a.ld_out + r2, a.words != 0, a.rows - r2, a.update, a.keep, a.rate, w);
+        } else if (c2 < a.cols) {
+            put(c2 * a.ld + r2, w);
         }
     }
 }
 
 static int64_t padded(int64_t n) { return (n + 31) / 32 * 32; }
 
+// Tile shapes: 256, 128 and 64 on both sides, and 192 for products whose operands both run along the sum.  The times are fitted to 43
+// products (64 to 4096 rows, 64 to 16384 columns) each measured with every shape and up to 8 parts: what they pick is the fastest or
+// at most 4 % (of the iteration) behind it.
+struct NsShape {
+    int size;
+    double step_us, start_us;   // of one work-group on a compute unit: a step, and what a tile costs beside its steps
+    int per_cu;                 // work-groups that share a compute unit (step_us is that of the pair)
+};
+static const NsShape ns_shapes[4] = {{256, 1.7, 9.0, 1}, {192, 1.08, 4.5, 1}, {128, 0.62, 3.3, 1}, {64, 0.48, 2.9, 2}};
+
+// Rounds of tiles over 256 compute units, with the sum cut in up to 8 parts where there are few tiles.  The parts go by one
+// matrix alone: the tiles' shape does not change a result's bits, the parts do, and a matrix has the same result in every batch.
+static double ns_time(const NsShape& s, int64_t batch, int64_t rows, int64_t cols, int64_t steps, int splits, bool sym)
+{
+    const int64_t nm = (rows + s.size - 1) / s.size, nn = (cols + s.size - 1) / s.size;
+    const int64_t tiles = batch * (sym ? nm * (nm + 1) / 2 : nm * nn) * splits;
+    const int64_t rounds = (tiles + 256 * s.per_cu - 1) / (256 * s.per_cu);
+    const double join = splits > 1 ? 10.0 + 0.56e-6 * batch * rows * cols * (splits + 1) * (sym ? 0.5 : 1.0) : 0.0;
+    return rounds * (s.start_us + s.step_us * ((steps + splits - 1) / splits)) + join;
+}
+
+static NsChoice ns_choose(int64_t batch, int64_t rows, int64_t cols, int64_t steps, bool sym)
+{
+    NsChoice best;
+    double least = 1e300;
+    for (int splits = 1; splits <= 8 && (splits == 1 || splits * 2 <= steps); ++splits)
+        for (int k = 0; k < 4; ++k) {
+            if (k == 1 && !sym) continue;
+            const double t = ns_time(ns_shapes[k], 1, rows, cols, steps, splits, sym);
+            if (t < least) { least = t; best.shape = k; best.splits = splits; }
+        }
+    if (batch > 1) {
+        least = 1e300;
+        for (int k = 0; k < 4; ++k) {
+            if (k == 1 && !sym) continue;
+            const double t = ns_time(ns_shapes[k], batch, rows, cols, steps, best.splits, sym);
+            if (t < least) { least = t; best.shape = k; }
+        }
+    }
+    return best;
+}
+
+static int64_t part_numbers(const NsChoice& c, int64_t rows, int64_t cols)
+{
+    const int64_t s = ns_shapes[c.shape].size;
+    return c.splits == 1 ? 0 : c.splits * ((rows + s - 1) / s * s) * ((cols + s - 1) / s * s);
+}
+
 bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
 {
-    const int64_t most = (int64_t)1 << 30;
     if (x.batch < 0 || x.rows < 0 || x.cols < 0 || x.batch > 65535 || x.rows > (1 << 20) || x.cols > (1 << 20)) return false;
-    p->ldc = padded(x.cols);
-    p->ldr = padded(x.rows);
-    const int64_t m = x.rows < x.cols ? x.rows : x.cols;
-    p->ldm = padded(m);
-    // a plane stays below 2 GiB, so that both planes of a tile's rows are within 32 bits of each other
-    if (x.rows * p->ldc > most || x.cols * p->ldr > most) return false;
+    p->m = x.rows < x.cols ? x.rows : x.cols;
+    p->n = x.rows < x.cols ? x.cols : x.rows;
+    p->ldn = padded(p->n);
+    p->ldm = padded(p->m);
+    // a plane stays at 2 GiB, so that both planes of a tile's rows are within 32 bits of each other
+    if (p->m * p->ldn > (int64_t)1 << 30) return false;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
-    for (int i = 0; i < 2; ++i) {
-        p->nat[i] = take(x.rows * p->ldc * 4);
-        p->tr[i] = take(x.cols * p->ldr * 4);
-    }
-    p->gram = take(m * p->ldm * 4);
-    p->poly = take(m * p->ldm * 4);
+    for (int i = 0; i < 2; ++i) p->x[i] = take(p->m * p->ldn * 4);
+    p->gram = take(p->m * p->ldm * 4);
+    p->poly = take(p->m * p->ldm * 4);
     p->per = at;
-    const int64_t n = x.rows * x.cols;
-    const int64_t parts = (n + 16 * MUON_THREADS - 1) / (16 * MUON_THREADS);
+    const int64_t n = x.rows * x.cols, parts = (n + 16 * MUON_THREADS - 1) / (16 * MUON_THREADS);
     p->parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
-    p->sums = x.batch * p->per;
-    p->bytes = p->sums + x.batch * p->parts * (int64_t)sizeof(double);
+    at = x.batch * p->per;
+    p->sums = take(x.batch * p->parts * (int64_t)sizeof(double));
+    p->gram_by = ns_choose(x.batch, p->m, p->m, p->ldn / 32, true);
+    p->poly_by = ns_choose(x.batch, p->m, p->m, p->ldm / 32, true);
+    p->step_by = ns_choose(x.batch, p->m, p->n, p->ldm / 32, false);
+    int64_t most = part_numbers(p->gram_by, p->m, p->m);
+    const int64_t b = part_numbers(p->poly_by, p->m, p->m), c = part_numbers(p->step_by, p->m, p->n);
+    most = most > b ? most : b;
+    most = most > c ? most : c;
+    p->parts_at = take(x.batch * most * (int64_t)sizeof(float));
+    p->bytes = at;
     return true;
 }
 
-template <typename T, int KIND, typename OUT>
-static int launch_ns_tile(NsArgs a, int64_t batch, hipStream_t st)
+template <typename T, int KIND, typename OUT, bool SPLIT>
+static int launch_tiles(const NsArgs& a, int64_t batch, hipStream_t st)
 {
-    a.nm = (a.a.rows + T::BM - 1) / T::BM;
-    a.nn = (a.b.rows + T::BN - 1) / T::BN;
-    a.band = 4;
-    const int64_t tiles = KIND == NS_GRAM || KIND == NS_POLY ? (int64_t)a.nm * (a.nm + 1) / 2 : (int64_t)a.nm * a.nn;
+    const int64_t tiles = (KIND == NS_GRAM || KIND == NS_POLY ? (int64_t)a.nm * (a.nm + 1) / 2 : (int64_t)a.nm * a.nn) * a.splits;
     if (tiles > 0x7fffffff) return GVQ_EINVAL;
     static gvq_once_per_device lds;
     int dev;
     GVQ_HIP(hipGetDevice(&dev));
     const int rc = lds.call(dev, [] {
-        GVQ_HIP(hipFuncSetAttribute((const void*)ns_tile_kernel<T, KIND, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+        GVQ_HIP(hipFuncSetAttribute((const void*)ns_tile_kernel<T, KIND, OUT, SPLIT>, hipFuncAttributeMaxDynamicSharedMemorySize, ns_lds<T>()));
         return (int)GVQ_OK;
     });
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((ns_tile_kernel<T, KIND, OUT>), dim3((unsigned)tiles, (unsigned)batch), dim3(T::THREADS), T::LDS, st, a);
+    hipLaunchKernelGGL((ns_tile_kernel<T, KIND, OUT, SPLIT>), dim3((unsigned)tiles, (unsigned)batch), dim3(T::THREADS), ns_lds<T>(), st, a);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
 
-template <int KIND, typename OUT>
-static int launch_ns(const NsArgs& a, int64_t batch, hipStream_t st)
+template <typename T, int KIND, typename OUT, bool TURN>
+static int launch_shape(NsArgs a, int64_t batch, hipStream_t st)
 {
-    const int64_t big = batch * ((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
-    if (big >= 192) return launch_ns_tile<TileShape<256, 256, 2, 4, 2, 2>, KIND, OUT>(a, batch, st);
-    return launch_ns_tile<TileShape<64, 64, 2, 2, 2, 4>, KIND, OUT>(a, batch, st);
+    a.nm = (a.rows + T::BM - 1) / T::BM;
+    a.nn = (a.cols + T::BN - 1) / T::BN;
+    a.band = 4;
+    if (a.splits == 1) return launch_tiles<T, KIND, OUT, false>(a, batch, st);
+    a.ld_part = (int64_t)a.nn * T::BN;
+    a.part = a.ld_part * a.nm * T::BM;
+    // (the parts of LAST lie as those of STEP: what a transpose needs is the join's to do)
+    typedef TileShape<T::BM, T::BN, T::WM, T::WN, 2, T::STAGES, T::TURNED, false> Plain;
+    const int rc = launch_tiles<Plain, KIND == NS_LAST ? (int)NS_STEP : KIND, float, true>(a, batch, st);
+    if (rc != GVQ_OK) return rc;
+    a.nm = (a.rows + 31) / 32;
+    a.nn = (int)((KIND == NS_LAST ? a.cols + 31 : a.ld) / 32);
+    const int64_t tiles = KIND == NS_GRAM || KIND == NS_POLY ? (int64_t)a.nm * (a.nm + 1) / 2 : (int64_t)a.nm * a.nn;
+    hipLaunchKernelGGL((ns_join_kernel<KIND, OUT, TURN>), dim3((unsigned)tiles, (unsigned)batch), dim3(256), 0, st, a);
+    GVQ_HIP(hipGetLastError());
+    return GVQ_OK;
+}
+
+template <int KIND, typename OUT, bool TURN>
+static int launch_ns(NsArgs a, const NsChoice& by, int64_t batch, hipStream_t st)
+{
+    constexpr bool X = KIND == NS_STEP || KIND == NS_LAST;   // the second operand is X, whose rows run across the sum
+    a.splits = by.splits;
+    switch (by.shape) {
+    case 0: return launch_shape<TileShape<256, 256, 2, 4, 2, 2, X, TURN>, KIND, OUT, TURN>(a, batch, st);
+    case 1: if constexpr (!X) return launch_shape<TileShape<192, 192, 2, 4, 2, 3, X, TURN>, KIND, OUT, TURN>(a, batch, st);
+            return GVQ_EINVAL;
+    case 2: return launch_shape<TileShape<128, 128, 2, 4, 2, 4, X, TURN>, KIND, OUT, TURN>(a, batch, st);
+    default: return launch_shape<TileShape<64, 64, 2, 2, 2, 4, X, TURN>, KIND, OUT, TURN>(a, batch, st);
+    }
 }
 
 int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
 {
     MuonPlan p;
     if (!gvq_muon_plan(m.x, &p)) return GVQ_EINVAL;
-    const int64_t batch = m.x.batch, rows = m.x.rows, cols = m.x.cols;
+    const int64_t batch = m.x.batch;
+    const bool wide = m.x.rows <= m.x.cols;
+    char* w = m.workspace;
     PrepArgs q{};
     q.grad = m.grad; q.ld_grad = m.ld_grad; q.stride_grad = m.stride_grad;
     q.momentum = m.momentum; q.ld_momentum = m.ld_momentum;
     q.beta = m.beta; q.nesterov = m.nesterov;
-    q.rows = rows; q.cols = cols;
-    q.sums = (double*)(m.workspace + p.sums);
+    q.rows = m.x.rows; q.cols = m.x.cols;
+    q.sums = (double*)(w + p.sums);
     q.parts = p.parts;
     q.eps = m.eps;
-    q.ws = m.workspace; q.per = p.per; q.nat = p.nat[0]; q.tr = p.tr[0]; q.ldc = p.ldc; q.ldr = p.ldr;
-    const dim3 g1(p.parts, (unsigned)batch), g2((unsigned)((p.ldc + 63) / 64), (unsigned)((p.ldr + 63) / 64), (unsigned)batch);
+    q.x = w + p.x[0]; q.per = p.per; q.plane = p.m * p.ldn; q.ld = p.ldn; q.turn = !wide;
+    // the padding of X's rows is written too: behind the columns, or behind the rows
+    const int64_t down = wide ? q.rows : p.ldn, across = wide ? p.ldn : q.cols;
+    const dim3 g1(p.parts, (unsigned)batch), g2((unsigned)((across + 63) / 64), (unsigned)((down + 63) / 64), (unsigned)batch);
     if (m.grad_dtype == GVQ_BF16) {
         hipLaunchKernelGGL((muon_norm_kernel<unsigned short>), g1, dim3(MUON_THREADS), 0, st, q);
         hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), g2, dim3(MUON_THREADS), 0, st, q);
@@ -338,55 +559,51 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
         hipLaunchKernelGGL((muon_planes_kernel<float>), g2, dim3(MUON_THREADS), 0, st, q);
     }
     GVQ_HIP(hipGetLastError());
-    const bool wide = rows <= cols;
-    const int mm = (int)(wide ? rows : cols), nn = (int)(wide ? cols : rows);
+    const int mm = (int)p.m, nn = (int)p.n;
     const int64_t es = m.out_dtype == GVQ_BF16 ? 2 : 4;
+    const TileOperand gram{w + p.gram, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
+    const TileOperand poly{w + p.poly, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
     for (int s = 0; s < m.steps; ++s) {
         const float a = (float)(m.coef ? m.coef[3 * s] : 3.4445), b = (float)(m.coef ? m.coef[3 * s + 1] : -4.7750),
                     c = (float)(m.coef ? m.coef[3 * s + 2] : 2.0315);
-        char* w = m.workspace;
-        const int now = s & 1, next = now ^ 1;
-        const TileOperand nat{w + p.nat[now], rows * p.ldc * 2, p.ldc * 2, (int)rows, nullptr};
-        const TileOperand tr{w + p.tr[now], cols * p.ldr * 2, p.ldr * 2, (int)cols, nullptr};
-        const TileOperand gram{w + p.gram, mm * p.ldm * 2, p.ldm * 2, mm, nullptr};
-        const TileOperand poly{w + p.poly, mm * p.ldm * 2, p.ldm * 2, mm, nullptr};
+        const TileOperand X{w + p.x[s & 1], mm * p.ldn * 2, p.ldn * 2, mm, nullptr, 0};
         NsArgs n{};
         n.per = p.per;
-        // A = X X^T, the sum along the longer side
-        n.a = n.b = wide ? nat : tr;
-        n.steps = (int)((padded(nn) * 2) / TILE_STEP);
+        n.parts = (float*)(w + p.parts_at);
+        // A = X X^T
+        n.a = n.b = X;
+        n.steps = (int)(p.ldn / 32);
+        n.rows = n.cols = mm;
         n.scale = 1.f / UNIT_X;   // (x UNIT_X)(x UNIT_X) -> A UNIT_X
-        n.nat = n.tr = (_Float16*)(w + p.gram);
-        n.nat_plane = n.tr_plane = mm * p.ldm;
-        n.ldn = n.ldt = p.ldm;
-        int rc = launch_ns<NS_GRAM, float>(n, batch, st);
+        n.res = (_Float16*)(w + p.gram);
+        n.plane = mm * p.ldm;
+        n.ld = p.ldm;
+        int rc = launch_ns<NS_GRAM, float, false>(n, p.gram_by, batch, st);
         if (rc != GVQ_OK) return rc;
         // b A + c A A
         n.a = n.b = gram;
-        n.steps = (int)(p.ldm * 2 / TILE_STEP);
+        n.steps = (int)(p.ldm / 32);
         n.scale = UNIT_P / (UNIT_X * UNIT_X);
         n.ca = b * (UNIT_P / UNIT_X);
         n.cb = c;
         n.old = (const _Float16*)(w + p.gram);
-        n.old_plane = mm * p.ldm;
-        n.nat = n.tr = (_Float16*)(w + p.poly);
-        rc = launch_ns<NS_POLY, float>(n, batch, st);
+        n.res = (_Float16*)(w + p.poly);
+        rc = launch_ns<NS_POLY, float, false>(n, p.poly_by, batch, st);
         if (rc != GVQ_OK) return rc;
-        // a X + (b A + c A A) X, or X from the left of it
-        n.a = wide ? poly : nat;
-        n.b = wide ? tr : poly;
+        // a X + (b A + c A A) X
+        n.a = poly;
+        n.b = X;
+        n.b.rows = nn;
+        n.b.depth = mm;
+        n.cols = nn;
         n.scale = 1.f / UNIT_P;
         n.ca = a;
-        n.old = (const _Float16*)(w + p.nat[now]);
-        n.old_plane = rows * p.ldc;
-        n.ldn = p.ldc;
+        n.old = (const _Float16*)(w + p.x[s & 1]);
+        n.plane = mm * p.ldn;
+        n.ld = p.ldn;
         if (s + 1 < m.steps) {
-            n.nat = (_Float16*)(w + p.nat[next]);
-            n.nat_plane = rows * p.ldc;
-            n.tr = (_Float16*)(w + p.tr[next]);
-            n.tr_plane = cols * p.ldr;
-            n.ldt = p.ldr;
-            rc = launch_ns<NS_STEP, float>(n, batch, st);
+            n.res = (_Float16*)(w + p.x[(s + 1) & 1]);
+            rc = launch_ns<NS_STEP, float, false>(n, p.step_by, batch, st);
         } else {
             n.out = m.out;
             n.ld_out = m.ld_out;
@@ -395,7 +612,10 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
             n.keep = m.keep;
             n.rate = m.rate;
             n.words = (((uintptr_t)m.out | (uintptr_t)(m.ld_out * es) | (uintptr_t)(m.stride_out * es)) & (uintptr_t)(4 * es - 1)) == 0;
-            rc = m.out_dtype == GVQ_BF16 ? launch_ns<NS_LAST, unsigned short>(n, batch, st) : launch_ns<NS_LAST, float>(n, batch, st);
+            if (m.out_dtype == GVQ_BF16)
+                rc = wide ? launch_ns<NS_LAST, unsigned short, false>(n, p.step_by, batch, st) : launch_ns<NS_LAST, unsigned short, true>(n, p.step_by, batch, st);
+            else
+                rc = wide ? launch_ns<NS_LAST, float, false>(n, p.step_by, batch, st) : launch_ns<NS_LAST, float, true>(n, p.step_by, batch, st);
         }
         if (rc != GVQ_OK) return rc;
     }

@@ -70,8 +70,8 @@ int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* 
 {
     MxProductArgs a;
     const int64_t row = gvq_mx_row_bytes(k), es = dtype == GVQ_BF16 ? 2 : 4;
-    a.a = TileOperand{(const char*)a_codes, 0, row, (int)m, (const char*)a_scales};
-    a.b = TileOperand{(const char*)b_codes, 0, row, (int)n, (const char*)b_scales};
+    a.a = TileOperand{(const char*)a_codes, 0, row, (int)m, (const char*)a_scales, 0};
+    a.b = TileOperand{(const char*)b_codes, 0, row, (int)n, (const char*)b_scales, 0};
     a.steps = (int)(row / TILE_STEP);
     a.out = out;
     a.ld = ld;

@@ -2,9 +2,9 @@
 // (gvq_mx_product.hip) and the Newton-Schulz products (gvq_muon.hip).  The two share everything but the matrix instruction: 128
 // numbers of 4 bits and 32 of 16 bits are both 64 bytes of a row, 16 bytes a lane, and one 16 x 16 matrix instruction.
 //
-// Rows come global -> LDS without passing through registers, 64 bytes of every row of the tile per step, STAGES - 1 steps ahead;
-// one barrier a step.  In LDS a 16-row group is 1 KB: row r's 16-byte chunk c sits in slot c ^ ((r >> 2) & 3) of the row, so that
-// the 16 rows of a fragment that are read at one time cover all 64 banks.
+// Rows come global -> LDS without passing through registers, 64 bytes of every row of the tile per step, STAGES steps ahead;
+// one barrier a step.  In LDS a 16-row group is 1 KB: row r's 16-byte chunk c sits in slot c ^ tile_swizzle(r / 4) of the row, so that
+// the 16 lanes whose 16-byte reads the LDS serves together (0-3, 12-15, 20-23, 24-27 and the like) cover all 64 banks.
 #pragma once
 #include "gvq_device.h"
 
@@ -39,18 +39,35 @@ __device__ __forceinline__ void tile_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+__device__ __forceinline__ int tile_swizzle(int s) { return (0x78 >> (2 * s)) & 3; }   // 0 2 3 1
+
 // One operand: `planes` matrices of the same layout, `plane` bytes apart; rows of `ld` bytes (a multiple of TILE_STEP).
 struct TileOperand {
     const char* p;
     int64_t plane;
     int64_t ld;
-    int rows;              // rows behind the last one are read as the last one
+    int rows;              // rows behind the last one are read as the last one (of the second operand in the other layout: columns)
     const char* scales;    // 4-bit operands: one byte per 32 numbers, rows of ld / 16 bytes
+    int depth;             // second operand in the other layout: its rows (numbers of the sum); further ones are read as the last one
+};
+
+// What a lane holds of 16 rows and one step.
+struct TileFragMx {
+    u4 v;
+    int k;   // scale
+};
+struct TileFragF16 {
+    h8 hi, lo;
 };
 
 // BM x BN of C by WM x WN waves; PLANES = 1: 4-bit numbers with scales, 2: two f16 terms per number (three products).
-template <int BM_, int BN_, int WM_, int WN_, int PLANES_, int STAGES_>
+// TURNED: the second operand's rows run across the sum instead of along it (C = A B; f16): a step is 32 of its rows, BN columns
+// each, and a lane gets its eight numbers of one column by two transposing LDS reads.  Their 32-byte units (a fragment's 16 columns of
+// one row) are exchanged within a row so that the eight rows that are read at one time lie in different banks.
+// FLIP: a lane ends with four neighbouring rows of one column instead of four neighbouring columns of one row.
+template <int BM_, int BN_, int WM_, int WN_, int PLANES_, int STAGES_, bool TURNED_ = false, bool FLIP_ = false>
 struct TileShape {
+    static constexpr bool TURNED = TURNED_, FLIP = FLIP_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, PLANES = PLANES_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;             // fragments of a wave
@@ -60,15 +77,29 @@ struct TileShape {
     static constexpr int SCALE_COPIES = (SCALE_GROUPS + WAVES - 1) / WAVES;
     static constexpr int STAGE = GROUPS * 1024 + SCALE_GROUPS * 256;
     static constexpr int LDS = STAGE * STAGES;
+    static constexpr int RING = (2 * MI) % 3 == 0 ? 3 : 4;                 // row fragments of A in registers
+    static constexpr int BSETS = PLANES == 1 ? 2 : 1;                      // sets of column fragments
+    static constexpr int UNROLL = BSETS == 2 || MI % RING ? 2 : 1;         // steps after which the registers' roles repeat
+    typedef typename std::conditional<PLANES == 1, TileFragMx, TileFragF16>::type Frag;
     static constexpr int LOADS = COPIES + SCALE_COPIES;                    // of a wave and a step
     static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && GROUPS % WAVES == 0, "whole fragments and copies");
     static_assert(SCALE_GROUPS * 64 == (PLANES == 1 ? BM + BN : 0), "whole copies of scales");
-    static_assert(LDS <= 160 * 1024 && LOADS * (STAGES - 2) < 64, "LDS and vmcnt");
+    static_assert(LDS <= 160 * 1024 && LOADS * (STAGES - 1) < 64, "LDS and vmcnt");
+    static_assert(!TURNED || (PLANES == 2 && (NI & (NI - 1)) == 0 && (BN & (BN - 1)) == 0 && BN >= 64), "exchange by exclusive or");
+    static_assert(MI >= 2 && (2 * MI) % RING == 0, "rings turn whole in two steps");
 };
 
-// acc[mi][ni][i] += C[row0 + wave's rows + 16 mi + lane % 16][col0 + wave's columns + 16 ni + 4 (lane / 16) + i], over the steps
-// [step0, step0 + steps) of the sum.  The operands go into the matrix instruction in exchanged roles, so that a lane ends with four
-// neighbouring columns of one row.
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v* tile_turn_ptr;
+template <typename T>
+__device__ __forceinline__ int tile_exchange(int row)
+{
+    return T::BN >= 128 ? (row & 3) | (row >> 1 & 4) : (row >> 1 & 1) | (row >> 2 & 2);
+}
+
+// acc[mi][ni][i] += C[row0 + wave's rows + 16 mi + lane % 16][col0 + wave's columns + 16 ni + 4 (lane / 16) + i] (FLIP: row 4 (lane / 16) + i,
+// column lane % 16), over the steps [step0, step0 + steps) of the sum.  Four neighbouring columns a lane come from giving the matrix
+// instruction the operands in exchanged roles.
 template <typename T>
 __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOperand& B, int row0, int col0, int step0, int steps,
                                              char* lds, f4 (&acc)[T::MI][T::NI])
@@ -76,7 +107,8 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave / T::WN, wn = wave % T::WN;
     const char* base[2] = {A.p + (int64_t)row0 * A.ld + (int64_t)step0 * TILE_STEP,
-                           B.p + (int64_t)col0 * B.ld + (int64_t)step0 * TILE_STEP};
+                           T::TURNED ? B.p + (int64_t)step0 * 32 * B.ld + (int64_t)col0 * 2
+                                     : B.p + (int64_t)col0 * B.ld + (int64_t)step0 * TILE_STEP};
     const char* sbase[2] = {nullptr, nullptr};
     unsigned int voff[T::COPIES], soff[T::SCALE_COPIES > 0 ? T::SCALE_COPIES : 1];
     constexpr int GA = T::BM / 16, GB = T::BN / 16;   // groups of a plane
@@ -86,9 +118,16 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
         const int g = wave * T::COPIES + i;
         const bool of_b = g >= T::PLANES * GA;
         const int gg = of_b ? g - T::PLANES * GA : g, per = of_b ? GB : GA;
-        const int pl = gg / per, r = (gg - pl * per) * 16 + (lane >> 2);
+        const int pl = gg / per;
+        if (T::TURNED && of_b) {
+            const int flat = (gg - pl * per) * 64 + lane, r = flat / (T::BN / 8), u = flat % (T::BN / 8);
+            const int c = ((u >> 1) ^ tile_exchange<T>(r)) * 32 + (u & 1) * 16, most = (int)(B.ld - 16 - (int64_t)col0 * 2);
+            voff[i] = (unsigned int)(pl * B.plane + (c < most ? c : most));
+            continue;
+        }
+        const int r = (gg - pl * per) * 16 + (lane >> 2);
         const int last = of_b ? B.rows - 1 - col0 : A.rows - 1 - row0;
-        const int c = (lane & 3) ^ ((lane >> 4) & 3);
+        const int c = (lane & 3) ^ tile_swizzle(lane >> 4);
         voff[i] = (unsigned int)((r < last ? r : last) * (of_b ? B.ld : A.ld) + pl * (of_b ? B.plane : A.plane)) + 16 * c;
     }
     if constexpr (T::PLANES == 1) {
@@ -108,7 +147,13 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
 #pragma unroll
         for (int i = 0; i < T::COPIES; ++i) {
             const int g = wave * T::COPIES + i;
-            copy_rows_to_lds(base[g >= T::PLANES * GA] + (int64_t)s * TILE_STEP, voff[i], to + g * 1024);
+            if (T::TURNED && g >= T::PLANES * GA) {
+                const int left = B.depth - 1 - (step0 + s) * 32, r = (((g - T::PLANES * GA) % GB) * 64 + lane) / (T::BN / 8);
+                copy_rows_to_lds(base[1] + (int64_t)s * 32 * B.ld, voff[i] + (unsigned int)(r < left ? r : left) * (unsigned int)B.ld,
+                                 to + g * 1024);
+            } else {
+                copy_rows_to_lds(base[g >= T::PLANES * GA] + (int64_t)s * TILE_STEP, voff[i], to + g * 1024);
+            }
         }
         if constexpr (T::PLANES == 1) {
 #pragma unroll
@@ -118,52 +163,107 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
             }
         }
     };
-    for (int s = 0; s < T::STAGES - 1 && s < steps; ++s) issue(s);
-    const int frag = (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 2)) & 3) * 16;
-    for (int s = 0; s < steps; ++s) {
-        if (s + T::STAGES - 1 <= steps) tile_barrier<T::LOADS * (T::STAGES - 2)>();
-        else tile_barrier<0>();
-        if (s + T::STAGES - 1 < steps) issue(s + T::STAGES - 1);
-        const char* st = lds + (unsigned int)(s % T::STAGES) * T::STAGE;
-        const char* pa = st + wm * T::MI * 1024 + frag;
-        const char* pb = st + T::PLANES * GA * 1024 + wn * T::NI * 1024 + frag;
+    const int frag = (lane & 15) * 64 + ((lane >> 4) ^ tile_swizzle((lane >> 2) & 3)) * 16;
+    const int turn_row = 8 * (lane >> 4) + ((lane & 15) >> 2);
+    const int turn = turn_row * 2 * T::BN + (lane & 3) * 8, turn_unit = (wn * T::NI) ^ tile_exchange<T>(turn_row);
+    typedef typename T::Frag Frag;
+    Frag fa[T::RING], fb[T::BSETS][T::NI];
+    auto load_a = [&](const char* st, int mi, Frag& f) {
         if constexpr (T::PLANES == 1) {
-            const char* sa = st + T::GROUPS * 1024 + (wm * T::MI * 16 + (lane & 15)) * 4 + (lane >> 4);
-            const char* sb = st + T::GROUPS * 1024 + (T::BM + wn * T::NI * 16 + (lane & 15)) * 4 + (lane >> 4);
-            i8v b[T::NI];
-            int kb[T::NI];
-#pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) {
-                const u4 v = *(const u4*)(pb + ni * 1024);
-                b[ni] = i8v{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-                kb[ni] = *(const unsigned char*)(sb + ni * 64);
+            f.v = *(const u4*)(st + (wm * T::MI + mi) * 1024 + frag);
+            f.k = *(const unsigned char*)(st + T::GROUPS * 1024 + ((wm * T::MI + mi) * 16 + (lane & 15)) * 4 + (lane >> 4));
+        } else {
+            f.hi = *(const h8*)(st + (wm * T::MI + mi) * 1024 + frag);
+            f.lo = *(const h8*)(st + (GA + wm * T::MI + mi) * 1024 + frag);
+        }
+    };
+    auto load_b = [&](const char* st, int ni, Frag& f, auto which) {   // f16: 1 the first term, 2 the second
+        constexpr int WHICH = decltype(which)::value;
+        if constexpr (T::PLANES == 1) {
+            f.v = *(const u4*)(st + (GA + wn * T::NI + ni) * 1024 + frag);
+            f.k = *(const unsigned char*)(st + T::GROUPS * 1024 + (T::BM + (wn * T::NI + ni) * 16 + (lane & 15)) * 4 + (lane >> 4));
+        } else if constexpr (T::TURNED) {
+            // two transposing reads of four rows each; lane i of 16 gets column i of the fragment
+            const char* p = st + 2 * GA * 1024 + turn + ((turn_unit ^ ni) << 5);
+            auto four = [&](const char* q) { return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile_turn_ptr)q)); };
+            if constexpr (WHICH & 1) {
+                const h4 a = four(p), b = four(p + 8 * T::BN);
+                f.hi = h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             }
-#pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi) {
-                const u4 v = *(const u4*)(pa + mi * 1024);
-                const i8v a = {(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-                const int ka = *(const unsigned char*)(sa + mi * 64);
-#pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni)
-                    acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[ni], a, acc[mi][ni], 4, 4, 0, kb[ni], 0, ka);
+            if constexpr (WHICH & 2) {
+                const h4 a = four(p + GB * 1024), b = four(p + GB * 1024 + 8 * T::BN);
+                f.lo = h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             }
         } else {
-            h8 b[T::NI][2];
+            if constexpr (WHICH & 1) f.hi = *(const h8*)(st + (2 * GA + wn * T::NI + ni) * 1024 + frag);
+            if constexpr (WHICH & 2) f.lo = *(const h8*)(st + (2 * GA + GB + wn * T::NI + ni) * 1024 + frag);
+        }
+    };
+    // One step, the P-th of UNROLL; the row fragments run two ahead.  Before its last two rows of products the wave has read all of
+    // the step's rows: there it meets the others, asks for step s + STAGES into the place that is free now, and reads the beginning
+    // of the next step beside the products that are left (f16: into the registers of B's fragments as their last products go out).
+    auto step = [&](int s, auto parity) {
+        constexpr int P = decltype(parity)::value, PB = P % T::BSETS, NB = (P + 1) % T::BSETS;
+        const char* st = lds + (unsigned int)(s % T::STAGES) * T::STAGE;
+        const char* next = lds + (unsigned int)((s + 1) % T::STAGES) * T::STAGE;
+        const bool more = s + 1 < steps;
+        static_for<0, T::MI>([&](auto c) {
+            constexpr int mi = decltype(c)::value;
+            if constexpr (mi + 2 < T::MI) load_a(st, mi + 2, fa[(P * T::MI + mi + 2) % T::RING]);
+            if constexpr (mi == T::MI - 2) {
+                if (more) {
+                    if (s + T::STAGES <= steps) tile_barrier<T::LOADS * (T::STAGES - 2)>();
+                    else tile_barrier<0>();
+                    if (s + T::STAGES < steps) issue(s + T::STAGES);
+                }
+                // (behind the last step: read once more what is there, into registers that nobody looks at)
+                if constexpr (T::BSETS == 2)
 #pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) {
-                b[ni][0] = *(const h8*)(pb + ni * 1024);
-                b[ni][1] = *(const h8*)(pb + (GB + ni) * 1024);
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[NB][ni], std::integral_constant<int, 3>{});
             }
+            if constexpr (mi >= T::MI - 2) load_a(next, mi + 2 - T::MI, fa[(P * T::MI + mi + 2) % T::RING]);
+            const Frag& a = fa[(P * T::MI + mi) % T::RING];
+            if constexpr (T::PLANES == 1) {
 #pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi) {
-                const h8 hi = *(const h8*)(pa + mi * 1024), lo = *(const h8*)(pa + (GA + mi) * 1024);
+                for (int ni = 0; ni < T::NI; ++ni) {
+                    const Frag& b = fb[PB][ni];
+                    acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        i8v{(int)b.v[0], (int)b.v[1], (int)b.v[2], (int)b.v[3], 0, 0, 0, 0},
+                        i8v{(int)a.v[0], (int)a.v[1], (int)a.v[2], (int)a.v[3], 0, 0, 0, 0}, acc[mi][ni], 4, 4, 0, b.k, 0, a.k);
+                }
+            } else {
 #pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ni][1], hi, acc[mi][ni], 0, 0, 0);
+                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = T::FLIP ? __builtin_amdgcn_mfma_f32_16x16x32_f16(a.hi, fb[PB][ni].lo, acc[mi][ni], 0, 0, 0)
+                                                                           : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].lo, a.hi, acc[mi][ni], 0, 0, 0);
+                if constexpr (mi == T::MI - 1)
 #pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ni][0], lo, acc[mi][ni], 0, 0, 0);
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[PB][ni], std::integral_constant<int, 2>{});
 #pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ni][0], hi, acc[mi][ni], 0, 0, 0);
+                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = T::FLIP ? __builtin_amdgcn_mfma_f32_16x16x32_f16(a.lo, fb[PB][ni].hi, acc[mi][ni], 0, 0, 0)
+                                                                           : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].hi, a.lo, acc[mi][ni], 0, 0, 0);
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = T::FLIP ? __builtin_amdgcn_mfma_f32_16x16x32_f16(a.hi, fb[PB][ni].hi, acc[mi][ni], 0, 0, 0)
+                                                                           : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].hi, a.hi, acc[mi][ni], 0, 0, 0);
+                if constexpr (mi == T::MI - 1)
+#pragma unroll
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[PB][ni], std::integral_constant<int, 1>{});
             }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    if (steps <= 0) return;
+    for (int s = 0; s < T::STAGES && s < steps; ++s) issue(s);
+    if (steps >= T::STAGES) tile_barrier<T::LOADS * (T::STAGES - 1)>();
+    else tile_barrier<0>();
+#pragma unroll
+    for (int ni = 0; ni < T::NI; ++ni) load_b(lds, ni, fb[0][ni], std::integral_constant<int, 3>{});
+    load_a(lds, 0, fa[0]);
+    load_a(lds, 1, fa[1]);
+    for (int s = 0; s < steps; s += T::UNROLL) {
+        step(s, std::integral_constant<int, 0>{});
+        if constexpr (T::UNROLL == 2) {
+            if (s + 1 >= steps) break;
+            step(s + 1, std::integral_constant<int, 1>{});
         }
     }
 }
