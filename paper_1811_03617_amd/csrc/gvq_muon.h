@@ -44,3 +44,32 @@ struct MuonArgs {
     char* workspace;
 };
 int gvq_launch_muon(const MuonArgs& a, hipStream_t st);
+
+// The gradient and momentum as kernels see them.
+struct MuonPrep {
+    const void* grad;
+    int64_t ld_grad, stride_grad;
+    float* momentum;
+    int64_t ld_momentum;
+    float beta;
+    int nesterov;
+    int64_t rows, cols;
+    int parts;           // partial sums of squares of a matrix
+    double eps;
+    int turn;            // more rows than columns: X is the transpose
+};
+MuonPrep gvq_muon_prep(const MuonArgs& a);
+float gvq_muon_coef(const MuonArgs& a, int step, int i);
+int gvq_muon_parts(const MuonMatrix& x);
+// M <- beta M + G and the sums of squares of U, `p.parts` per matrix.
+int gvq_launch_muon_norm(const MuonArgs& a, const MuonPrep& p, double* sums, hipStream_t st);
+
+// Matrices with at most 64 rows or columns (gvq_muon_small.hip).
+struct MuonSmallPlan {
+    int64_t m, n, ldn, run, groups, per, x, grams[2], sums, bytes;
+    int parts;
+    bool one;            // in one work-group, without a workspace
+};
+bool gvq_muon_small_takes(const MuonMatrix& x);
+int64_t gvq_muon_small_plan(const MuonMatrix& x, MuonSmallPlan* p);   // bytes of the workspace
+int gvq_launch_muon_small(const MuonArgs& a, hipStream_t st);

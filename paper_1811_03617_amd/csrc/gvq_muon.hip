@@ -8,78 +8,33 @@
 // So X, A and the polynomial are kept as two f16 terms, 22 bits, in fixed units of 2^-12 (X, A) and 2^-10 (the polynomial), and
 // every product is hi hi + hi lo + lo hi in fp32 sums: as exact as fp32 products (1.0 to 1.15 times their error), at a third of
 // the f16 matrix pipe's rate, which is five times the fp32 pipe's.
-#include "gvq_muon.h"
-#include "gvq_tile.h"
+#include "gvq_muon_device.h"
 
-#define UNIT_X 4096.f
-#define UNIT_P 1024.f
 #define MUON_THREADS 256
 
 struct PrepArgs {
-    const void* grad;
-    int64_t ld_grad, stride_grad;
-    float* momentum;
-    int64_t ld_momentum;
-    float beta;
-    int nesterov;
-    int64_t rows, cols;
+    MuonPrep p;
     double* sums;        // [batch][parts]
-    int parts;
-    double eps;
     char* x;             // planes of the first matrix, `per` bytes further for each next one
     int64_t per, plane;  // plane: numbers
     int64_t ld;
-    int turn;            // more rows than columns: X is the transpose
 };
-
-template <typename G>
-__device__ __forceinline__ float grad_at(const G* g, int64_t i);
-template <>
-__device__ __forceinline__ float grad_at<float>(const float* g, int64_t i) { return g[i]; }
-template <>
-__device__ __forceinline__ float grad_at<unsigned short>(const unsigned short* g, int64_t i) { return bf16_to_f32(g[i]); }
-
-// Sum over a work-group of MUON_THREADS, in a fixed order; every thread gets it.
-__device__ __forceinline__ double group_sum(double v, double* lds)
-{
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double s = 0;
-#pragma unroll
-    for (int w = 0; w < MUON_THREADS / 64; ++w) s += lds[w];
-    __syncthreads();
-    return s;
-}
 
 // M <- beta M + G, and the sum of squares of U, in float64 (squares of fp32 numbers are exact there and do not overflow).
 template <typename G>
 __global__ __launch_bounds__(MUON_THREADS) void muon_norm_kernel(PrepArgs a)
 {
     __shared__ double lds[MUON_THREADS / 64];
-    const G* g = (const G*)a.grad + blockIdx.y * a.stride_grad;
+    const G* g = (const G*)a.p.grad + blockIdx.y * a.p.stride_grad;
     double s = 0;
-    const int64_t n = a.rows * a.cols, step = (int64_t)gridDim.x * MUON_THREADS;
+    const int64_t n = a.p.rows * a.p.cols, step = (int64_t)gridDim.x * MUON_THREADS;
     for (int64_t i = (int64_t)blockIdx.x * MUON_THREADS + threadIdx.x; i < n; i += step) {
-        const int64_t r = i / a.cols, c = i - r * a.cols;
-        float u = grad_at<G>(g, r * a.ld_grad + c);
-        if (a.momentum) {
-            float* m = a.momentum + r * a.ld_momentum + c;
-            const float v = a.beta * *m + u;
-            *m = v;
-            u = a.nesterov ? u + a.beta * v : v;
-        }
+        const int64_t r = i / a.p.cols, c = i - r * a.p.cols;
+        const float u = momentum_at<G>(a.p, g, r, c);
         s += (double)u * u;
     }
-    s = group_sum(s, lds);
-    if (threadIdx.x == 0) a.sums[blockIdx.y * a.parts + blockIdx.x] = s;
-}
-
-__device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo)
-{
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
+    s = group_sum<MUON_THREADS>(s, lds);
+    if (threadIdx.x == 0) a.sums[blockIdx.y * a.p.parts + blockIdx.x] = s;
 }
 
 // U / (|U| + eps) into the two planes of X, with zeros behind the last column: 64 x 64 numbers a work-group, through LDS if X is
@@ -90,9 +45,9 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
     __shared__ double lds[MUON_THREADS / 64];
     __shared__ float tile[64 * 65];
     double s = 0;
-    for (int i = threadIdx.x; i < a.parts; i += MUON_THREADS) s += a.sums[blockIdx.z * a.parts + i];
-    const double inv = 1.0 / (sqrt(group_sum(s, lds)) + a.eps) * UNIT_X;
-    const G* g = (const G*)a.grad + blockIdx.z * a.stride_grad;
+    for (int i = threadIdx.x; i < a.p.parts; i += MUON_THREADS) s += a.sums[blockIdx.z * a.p.parts + i];
+    const double inv = 1.0 / (sqrt(group_sum<MUON_THREADS>(s, lds)) + a.p.eps) * UNIT_X;
+    const G* g = (const G*)a.p.grad + blockIdx.z * a.p.stride_grad;
     _Float16* X = (_Float16*)(a.x + blockIdx.z * a.per);
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
     const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
@@ -106,23 +61,16 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
     for (int y = y0; y < 64; y += MUON_THREADS / 64) {
         const int64_t r = r0 + y, c = c0 + x;
         float v = 0.f;
-        if (r < a.rows && c < a.cols) {
-            float u = grad_at<G>(g, r * a.ld_grad + c);
-            if (a.momentum) {
-                const float m = a.momentum[r * a.ld_momentum + c];
-                u = a.nesterov ? u + a.beta * m : m;
-            }
-            v = (float)((double)u * inv);
-        }
-        if (a.turn) tile[y * 65 + x] = v;
-        else if (r < a.rows && c < a.ld) put(r * a.ld + c, v);
+        if (r < a.p.rows && c < a.p.cols) v = (float)((double)direction_at<G>(a.p, g, r, c) * inv);
+        if (a.p.turn) tile[y * 65 + x] = v;
+        else if (r < a.p.rows && c < a.ld) put(r * a.ld + c, v);
     }
-    if (!a.turn) return;
+    if (!a.p.turn) return;
     __syncthreads();
 #pragma unroll 4
     for (int y = y0; y < 64; y += MUON_THREADS / 64) {
         const int64_t c = c0 + y, r = r0 + x;
-        if (c < a.cols && r < a.ld) put(c * a.ld + r, tile[x * 65 + y]);
+        if (c < a.p.cols && r < a.ld) put(c * a.ld + r, tile[x * 65 + y]);
     }
 }
 
@@ -448,6 +396,43 @@ static int64_t part_numbers(const NsChoice& c, int64_t rows, int64_t cols)
     return c.splits == 1 ? 0 : c.splits * ((rows + s - 1) / s * s) * ((cols + s - 1) / s * s);
 }
 
+int gvq_muon_parts(const MuonMatrix& x)
+{
+    const int64_t n = x.rows * x.cols, parts = (n + 16 * MUON_THREADS - 1) / (16 * MUON_THREADS);
+    return (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
+}
+
+MuonPrep gvq_muon_prep(const MuonArgs& m)
+{
+    MuonPrep p{};
+    p.grad = m.grad; p.ld_grad = m.ld_grad; p.stride_grad = m.stride_grad;
+    p.momentum = m.momentum; p.ld_momentum = m.ld_momentum;
+    p.beta = m.beta; p.nesterov = m.nesterov;
+    p.rows = m.x.rows; p.cols = m.x.cols;
+    p.parts = gvq_muon_parts(m.x);
+    p.eps = m.eps;
+    p.turn = m.x.rows > m.x.cols;
+    return p;
+}
+
+float gvq_muon_coef(const MuonArgs& m, int step, int i)
+{
+    static const double standard[3] = {3.4445, -4.7750, 2.0315};
+    return (float)(m.coef ? m.coef[3 * step + i] : standard[i]);
+}
+
+int gvq_launch_muon_norm(const MuonArgs& m, const MuonPrep& p, double* sums, hipStream_t st)
+{
+    PrepArgs q{};
+    q.p = p;
+    q.sums = sums;
+    const dim3 grid(p.parts, (unsigned)m.x.batch);
+    if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_norm_kernel<unsigned short>), grid, dim3(MUON_THREADS), 0, st, q);
+    else hipLaunchKernelGGL((muon_norm_kernel<float>), grid, dim3(MUON_THREADS), 0, st, q);
+    GVQ_HIP(hipGetLastError());
+    return GVQ_OK;
+}
+
 bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
 {
     if (x.batch < 0 || x.rows < 0 || x.cols < 0 || x.batch > 65535 || x.rows > (1 << 20) || x.cols > (1 << 20)) return false;
@@ -455,16 +440,21 @@ bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
     p->n = x.rows < x.cols ? x.cols : x.rows;
     p->ldn = padded(p->n);
     p->ldm = padded(p->m);
+    p->bytes = 0;
     // a plane stays at 2 GiB, so that both planes of a tile's rows are within 32 bits of each other
     if (p->m * p->ldn > (int64_t)1 << 30) return false;
+    if (gvq_muon_small_takes(x)) {
+        MuonSmallPlan small;
+        p->bytes = gvq_muon_small_plan(x, &small);
+        return true;
+    }
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
     for (int i = 0; i < 2; ++i) p->x[i] = take(p->m * p->ldn * 4);
     p->gram = take(p->m * p->ldm * 4);
     p->poly = take(p->m * p->ldm * 4);
     p->per = at;
-    const int64_t n = x.rows * x.cols, parts = (n + 16 * MUON_THREADS - 1) / (16 * MUON_THREADS);
-    p->parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
+    p->parts = gvq_muon_parts(x);
     at = x.batch * p->per;
     p->sums = take(x.batch * p->parts * (int64_t)sizeof(double));
     p->gram_by = ns_choose(x.batch, p->m, p->m, p->ldn / 32, true);
@@ -536,36 +526,28 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
 {
     MuonPlan p;
     if (!gvq_muon_plan(m.x, &p)) return GVQ_EINVAL;
+    if (gvq_muon_small_takes(m.x)) return gvq_launch_muon_small(m, st);
     const int64_t batch = m.x.batch;
     const bool wide = m.x.rows <= m.x.cols;
     char* w = m.workspace;
     PrepArgs q{};
-    q.grad = m.grad; q.ld_grad = m.ld_grad; q.stride_grad = m.stride_grad;
-    q.momentum = m.momentum; q.ld_momentum = m.ld_momentum;
-    q.beta = m.beta; q.nesterov = m.nesterov;
-    q.rows = m.x.rows; q.cols = m.x.cols;
+    q.p = gvq_muon_prep(m);
     q.sums = (double*)(w + p.sums);
-    q.parts = p.parts;
-    q.eps = m.eps;
-    q.x = w + p.x[0]; q.per = p.per; q.plane = p.m * p.ldn; q.ld = p.ldn; q.turn = !wide;
+    q.x = w + p.x[0]; q.per = p.per; q.plane = p.m * p.ldn; q.ld = p.ldn;
+    int rc = gvq_launch_muon_norm(m, q.p, q.sums, st);
+    if (rc != GVQ_OK) return rc;
     // the padding of X's rows is written too: behind the columns, or behind the rows
-    const int64_t down = wide ? q.rows : p.ldn, across = wide ? p.ldn : q.cols;
-    const dim3 g1(p.parts, (unsigned)batch), g2((unsigned)((across + 63) / 64), (unsigned)((down + 63) / 64), (unsigned)batch);
-    if (m.grad_dtype == GVQ_BF16) {
-        hipLaunchKernelGGL((muon_norm_kernel<unsigned short>), g1, dim3(MUON_THREADS), 0, st, q);
-        hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), g2, dim3(MUON_THREADS), 0, st, q);
-    } else {
-        hipLaunchKernelGGL((muon_norm_kernel<float>), g1, dim3(MUON_THREADS), 0, st, q);
-        hipLaunchKernelGGL((muon_planes_kernel<float>), g2, dim3(MUON_THREADS), 0, st, q);
-    }
+    const int64_t down = wide ? m.x.rows : p.ldn, across = wide ? p.ldn : m.x.cols;
+    const dim3 grid((unsigned)((across + 63) / 64), (unsigned)((down + 63) / 64), (unsigned)batch);
+    if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), grid, dim3(MUON_THREADS), 0, st, q);
+    else hipLaunchKernelGGL((muon_planes_kernel<float>), grid, dim3(MUON_THREADS), 0, st, q);
     GVQ_HIP(hipGetLastError());
     const int mm = (int)p.m, nn = (int)p.n;
     const int64_t es = m.out_dtype == GVQ_BF16 ? 2 : 4;
     const TileOperand gram{w + p.gram, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
     const TileOperand poly{w + p.poly, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
     for (int s = 0; s < m.steps; ++s) {
-        const float a = (float)(m.coef ? m.coef[3 * s] : 3.4445), b = (float)(m.coef ? m.coef[3 * s + 1] : -4.7750),
-                    c = (float)(m.coef ? m.coef[3 * s + 2] : 2.0315);
+        const float a = gvq_muon_coef(m, s, 0), b = gvq_muon_coef(m, s, 1), c = gvq_muon_coef(m, s, 2);
         const TileOperand X{w + p.x[s & 1], mm * p.ldn * 2, p.ldn * 2, mm, nullptr, 0};
         NsArgs n{};
         n.per = p.per;
@@ -578,7 +560,7 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
         n.res = (_Float16*)(w + p.gram);
         n.plane = mm * p.ldm;
         n.ld = p.ldm;
-        int rc = launch_ns<NS_GRAM, float, false>(n, p.gram_by, batch, st);
+        rc = launch_ns<NS_GRAM, float, false>(n, p.gram_by, batch, st);
         if (rc != GVQ_OK) return rc;
         // b A + c A A
         n.a = n.b = gram;

@@ -1,0 +1,53 @@
+// What the Newton-Schulz kernels share on the device: units, splits, the momentum.
+#pragma once
+#include "gvq_muon.h"
+#include "gvq_tile.h"
+
+// Fixed units of the f16 terms: X and its Gram matrix, the polynomial.
+#define UNIT_X 4096.f
+#define UNIT_P 1024.f
+
+__device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo)
+{
+    hi = (_Float16)v;
+    lo = (_Float16)(v - (float)hi);
+}
+
+// Sum over a work-group, in a fixed order; every thread gets it.
+template <int THREADS>
+__device__ __forceinline__ double group_sum(double v, double* lds)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double s = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
+    __syncthreads();
+    return s;
+}
+
+__device__ __forceinline__ float number_at(const float* g, int64_t i) { return g[i]; }
+__device__ __forceinline__ float number_at(const unsigned short* g, int64_t i) { return bf16_to_f32(g[i]); }
+
+// U at row r and column c as the momentum already is.
+template <typename G>
+__device__ __forceinline__ float direction_at(const MuonPrep& a, const G* g, int64_t r, int64_t c)
+{
+    const float u = number_at(g, r * a.ld_grad + c);
+    if (!a.momentum) return u;
+    const float m = a.momentum[r * a.ld_momentum + c];
+    return a.nesterov ? u + a.beta * m : m;
+}
+// ... and with the momentum brought up to date first: M <- beta M + G.
+template <typename G>
+__device__ __forceinline__ float momentum_at(const MuonPrep& a, const G* g, int64_t r, int64_t c)
+{
+    const float u = number_at(g, r * a.ld_grad + c);
+    if (!a.momentum) return u;
+    float* m = a.momentum + r * a.ld_momentum + c;
+    const float v = a.beta * *m + u;
+    *m = v;
+    return a.nesterov ? u + a.beta * v : v;
+}

@@ -91,6 +91,12 @@ struct TileShape {
 
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v* tile_turn_ptr;
+// Four numbers each of one column: 16 lanes read four rows of 16 numbers, lane i four numbers of row i / 4 from column 4 (i % 4) on, and
+// lane i gets column i.
+__device__ __forceinline__ h4 turned4(const void* p)
+{
+    return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile_turn_ptr)p));
+}
 template <typename T>
 __device__ __forceinline__ int tile_exchange(int row)
 {
@@ -185,13 +191,12 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
         } else if constexpr (T::TURNED) {
             // two transposing reads of four rows each; lane i of 16 gets column i of the fragment
             const char* p = st + 2 * GA * 1024 + turn + ((turn_unit ^ ni) << 5);
-            auto four = [&](const char* q) { return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile_turn_ptr)q)); };
             if constexpr (WHICH & 1) {
-                const h4 a = four(p), b = four(p + 8 * T::BN);
+                const h4 a = turned4(p), b = turned4(p + 8 * T::BN);
                 f.hi = h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             }
             if constexpr (WHICH & 2) {
-                const h4 a = four(p + GB * 1024), b = four(p + GB * 1024 + 8 * T::BN);
+                const h4 a = turned4(p + GB * 1024), b = turned4(p + GB * 1024 + 8 * T::BN);
                 f.lo = h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             }
         } else {
