@@ -9,8 +9,22 @@ struct MxProductArgs {
     int nm, nn, band;  // tiles, and how they are swept
     void* out;
     int64_t ld;
-    int accumulate, words;   // words: four neighbouring results are one aligned word
+    int accumulate, words;   // words: rows are aligned to 16 bytes
 };
+
+// A wave hands its results out through its share of LDS, so that rows leave in 16-byte words side by side: straight from the
+// accumulators they would leave in pieces of 32 or 64 bytes, 16 rows at a time.  Rows are padded by one word; fp32 results go in
+// two halves.
+template <typename T, typename OUT>
+struct MxOut {
+    static constexpr int R = T::BM / T::WM / (sizeof(OUT) / 2), C = T::BN / T::WN, PAD = 16 / sizeof(OUT), LD = C + PAD;
+    static constexpr int WAVE = R * LD * sizeof(OUT), ALL = T::WAVES * WAVE;
+    static constexpr int LDS = T::LDS > ALL ? T::LDS : ALL;
+    static_assert(LDS <= 160 * 1024 && WAVE % 16 == 0 && R % 16 == 0, "LDS of a compute unit; whole fragments");
+};
+
+__device__ __forceinline__ void mx_lds4(float* p, f4 v) { *(f4*)p = v; }
+__device__ __forceinline__ void mx_lds4(unsigned short* p, f4 v) { *(u2*)p = u2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
 template <typename T, typename OUT>
 __global__ __launch_bounds__(T::THREADS) void mx_tile_kernel(MxProductArgs a)
@@ -24,16 +38,46 @@ __global__ __launch_bounds__(T::THREADS) void mx_tile_kernel(MxProductArgs a)
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = f4{0.f, 0.f, 0.f, 0.f};
     tile_product<T>(a.a, a.b, tm * T::BM, tn * T::BN, 0, a.steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = tm * T::BM + wave / T::WN * (T::BM / T::WM) + (lane & 15);
-    const int c0 = tn * T::BN + wave % T::WN * (T::BN / T::WN) + 4 * (lane >> 4);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int r0 = tm * T::BM + wave / T::WN * (T::BM / T::WM), c0 = tn * T::BN + wave % T::WN * (T::BN / T::WN);
+    OUT* out = (OUT*)a.out;
+    if (a.words && !a.accumulate) {
+        typedef MxOut<T, OUT> O;
+        constexpr int FRAGS = O::R / 16, PER = 16 / sizeof(OUT), LANES = O::C / PER;   // lanes of a row
+        OUT* w = (OUT*)(lds + wave * O::WAVE);
+        __syncthreads();
+        static_for<0, T::MI / FRAGS>([&](auto half) {
+            constexpr int H = decltype(half)::value * FRAGS;
+#pragma unroll
+            for (int mi = 0; mi < FRAGS; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) mx_lds4(w + (16 * mi + (lane & 15)) * O::LD + 16 * ni + 4 * (lane >> 4), acc[H + mi][ni]);
+            wave_lds_sync();
+#pragma unroll
+            for (int i = 0; i < O::R * LANES / 64; ++i) {
+                const int e = lane + 64 * i, r = e / LANES, c = e % LANES * PER, left = a.b.rows - (c0 + c);
+                if (r0 + 16 * H + r >= a.a.rows) continue;
+                const u4 v = *(const u4*)(w + r * O::LD + c);
+                OUT* to = out + (int64_t)(r0 + 16 * H + r) * a.ld + c0 + c;
+                if (left >= PER) *(u4*)to = v;
+                else
+#pragma unroll
+                    for (int k = 0; k < PER; ++k)
+                        if (k < left) to[k] = w[r * O::LD + c + k];
+            }
+            wave_lds_sync();
+        });
+        return;
+    }
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi) {
-        const int r = r0 + 16 * mi;
+        const int r = r0 + 16 * mi + (lane & 15);
         if (r >= a.a.rows) continue;
-        OUT* row = (OUT*)a.out + (int64_t)r * a.ld;
 #pragma unroll
-        for (int ni = 0; ni < T::NI; ++ni) mx_store4(row + c0 + 16 * ni, a.words != 0, a.b.rows - (c0 + 16 * ni), a.accumulate != 0, acc[mi][ni]);
+        for (int ni = 0; ni < T::NI; ++ni) {
+            const int c = c0 + 16 * ni + 4 * (lane >> 4);
+            mx_store4(out + (int64_t)r * a.ld + c, a.words != 0, a.b.rows - c, a.accumulate != 0, acc[mi][ni]);
+        }
     }
 }
 
@@ -44,30 +88,54 @@ static int launch_tile(MxProductArgs a, hipStream_t st)
     a.nn = (a.b.rows + T::BN - 1) / T::BN;
     if ((int64_t)a.nm * a.nn > 0x7fffffff) return GVQ_EINVAL;
     a.band = 4;
+    constexpr int LDS = MxOut<T, OUT>::LDS;
     static gvq_once_per_device lds;
     int dev;
     GVQ_HIP(hipGetDevice(&dev));
     const int rc = lds.call(dev, [] {
-        GVQ_HIP(hipFuncSetAttribute((const void*)mx_tile_kernel<T, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+        GVQ_HIP(hipFuncSetAttribute((const void*)mx_tile_kernel<T, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
         return (int)GVQ_OK;
     });
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((mx_tile_kernel<T, OUT>), dim3(a.nm * a.nn), dim3(T::THREADS), T::LDS, st, a);
+    hipLaunchKernelGGL((mx_tile_kernel<T, OUT>), dim3(a.nm * a.nn), dim3(T::THREADS), LDS, st, a);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
 
+// Tile shapes and their times, fitted to 20 products (64 to 8192 rows, 1000 to 25088 columns, sums of 500 to 25088) each measured with
+// every shape: what a round of tiles over 256 compute units costs beside its steps, a step, and the work-groups that share a unit.
+struct MxShape {
+    int bm, bn;
+    double start_us, step_us;
+    int per_cu;
+};
+static const MxShape mx_shapes[4] = {{256, 256, 8.0, 0.95, 1}, {256, 128, 2.5, 0.67, 1}, {128, 128, 1.0, 0.39, 1}, {64, 64, 2.0, 0.255, 2}};
+
 template <typename OUT>
 static int launch_product(const MxProductArgs& a, hipStream_t st)
 {
-    const int64_t big = (int64_t)((a.a.rows + 255) / 256) * ((a.b.rows + 255) / 256);
-    if (big >= 192) return launch_tile<TileShape<256, 256, 2, 4, 1, 4>, OUT>(a, st);
-    return launch_tile<TileShape<64, 64, 2, 2, 1, 4>, OUT>(a, st);
+    if (a.steps < 4) return launch_tile<TileShape<64, 64, 2, 2, 1, 4, false, false, true>, OUT>(a, st);
+    int best = 3;
+    double least = 1e300;
+    for (int k = 0; k < 4; ++k) {
+        const MxShape& s = mx_shapes[k];
+        const int64_t tiles = (int64_t)((a.a.rows + s.bm - 1) / s.bm) * ((a.b.rows + s.bn - 1) / s.bn);
+        const double t = (double)((tiles + 256 * s.per_cu - 1) / (256 * s.per_cu)) * (s.start_us + s.step_us * a.steps);
+        if (t < least) { least = t; best = k; }
+    }
+    switch (best) {
+    case 0: return launch_tile<TileShape<256, 256, 2, 4, 1, 4>, OUT>(a, st);
+    case 1: return launch_tile<TileShape<256, 128, 4, 2, 1, 4>, OUT>(a, st);
+    case 2: return launch_tile<TileShape<128, 128, 2, 4, 1, 4>, OUT>(a, st);
+    default: return launch_tile<TileShape<64, 64, 2, 2, 1, 4>, OUT>(a, st);
+    }
 }
 
 int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n,
                          int64_t k, void* out, gvq_dtype_t dtype, int64_t ld, bool accumulate, hipStream_t st)
 {
+    if (m <= GVQ_MX_FEW_ROWS && k > 0)
+        return gvq_launch_mx_few(a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, accumulate, st);
     MxProductArgs a;
     const int64_t row = gvq_mx_row_bytes(k), es = dtype == GVQ_BF16 ? 2 : 4;
     a.a = TileOperand{(const char*)a_codes, 0, row, (int)m, (const char*)a_scales, 0};
@@ -76,7 +144,7 @@ int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* 
     a.out = out;
     a.ld = ld;
     a.accumulate = accumulate;
-    a.words = (((uintptr_t)out | (uintptr_t)(ld * es)) & (uintptr_t)(4 * es - 1)) == 0;
+    a.words = (((uintptr_t)out | (uintptr_t)(ld * es)) & 15) == 0;
     a.nm = a.nn = a.band = 0;
     return dtype == GVQ_BF16 ? launch_product<unsigned short>(a, st) : launch_product<float>(a, st);
 }

@@ -17,15 +17,23 @@ typedef int i8v __attribute__((ext_vector_type(8)));
 // global -> LDS, `voff` bytes behind the wave-uniform `base` for each lane, 16 (or 4) bytes a lane to consecutive places from the
 // wave-uniform byte offset `lds` on.  Inline assembly: the compiler would otherwise wait for every such copy before any LDS read.
 // m0 carries the LDS offset and is named as clobbered on purpose.
+__device__ __forceinline__ const void* in_scalars(const void* p)
+{
+    const uint64_t v = (uint64_t)p;
+    const unsigned int lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (const void*)((uint64_t)hi << 32 | lo);
+}
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_rows_to_lds(const void* base, unsigned int voff, unsigned int lds)
 {
+    base = in_scalars(base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(voff), "s"(lds), "s"(base)
                  : "memory", "m0");
 }
 __device__ __forceinline__ void copy_words_to_lds(const void* base, unsigned int voff, unsigned int lds)
 {
+    base = in_scalars(base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, %2" ::"v"(voff), "s"(lds), "s"(base)
                  : "memory", "m0");
 }
@@ -65,9 +73,11 @@ struct TileFragF16 {
 // each, and a lane gets its eight numbers of one column by two transposing LDS reads.  Their 32-byte units (a fragment's 16 columns of
 // one row) are exchanged within a row so that the eight rows that are read at one time lie in different banks.
 // FLIP: a lane ends with four neighbouring rows of one column instead of four neighbouring columns of one row.
-template <int BM_, int BN_, int WM_, int WN_, int PLANES_, int STAGES_, bool TURNED_ = false, bool FLIP_ = false>
+// Scales come for four steps at a time, 16 bytes of a row, into one of two places (a row's 4 bytes per step cost as many cache lines
+// as its 16 would: 8192 x 4096 x 4096 73 us without them, 101 with): sums of four steps at least, unless NARROW, step by step.
+template <int BM_, int BN_, int WM_, int WN_, int PLANES_, int STAGES_, bool TURNED_ = false, bool FLIP_ = false, bool NARROW_ = false>
 struct TileShape {
-    static constexpr bool TURNED = TURNED_, FLIP = FLIP_;
+    static constexpr bool TURNED = TURNED_, FLIP = FLIP_, WIDE = PLANES_ == 1 && !NARROW_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, PLANES = PLANES_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;             // fragments of a wave
@@ -75,16 +85,20 @@ struct TileShape {
     static constexpr int COPIES = GROUPS / WAVES;
     static constexpr int SCALE_GROUPS = PLANES == 1 ? (BM + BN) / 64 : 0;  // 64 rows' scales each
     static constexpr int SCALE_COPIES = (SCALE_GROUPS + WAVES - 1) / WAVES;
-    static constexpr int STAGE = GROUPS * 1024 + SCALE_GROUPS * 256;
-    static constexpr int LDS = STAGE * STAGES;
+    static constexpr int STAGE = GROUPS * 1024 + (WIDE ? 0 : SCALE_GROUPS * 256);
+    static constexpr int SCALE_PLACE = SCALE_GROUPS * 1024;                // WIDE: two of them behind the stages
+    static constexpr int LDS = STAGE * STAGES + (WIDE ? 2 * SCALE_PLACE : 0);
     static constexpr int RING = (2 * MI) % 3 == 0 ? 3 : 4;                 // row fragments of A in registers
     static constexpr int BSETS = PLANES == 1 ? 2 : 1;                      // sets of column fragments
     static constexpr int UNROLL = BSETS == 2 || MI % RING ? 2 : 1;         // steps after which the registers' roles repeat
     typedef typename std::conditional<PLANES == 1, TileFragMx, TileFragF16>::type Frag;
-    static constexpr int LOADS = COPIES + SCALE_COPIES;                    // of a wave and a step
+    // Of a wave and a step.  WIDE: every fourth step has SCALE_COPIES more, which a wait for the youngest ones' predecessors then
+    // counts in place of younger ones: it waits for a copy or two more than it has to.
+    static constexpr int LOADS = COPIES + (WIDE ? 0 : SCALE_COPIES);
     static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && GROUPS % WAVES == 0, "whole fragments and copies");
     static_assert(SCALE_GROUPS * 64 == (PLANES == 1 ? BM + BN : 0), "whole copies of scales");
-    static_assert(LDS <= 160 * 1024 && LOADS * (STAGES - 1) < 64, "LDS and vmcnt");
+    static_assert(LDS <= 160 * 1024 && (LOADS + SCALE_COPIES) * STAGES < 64, "LDS and vmcnt");
+    static_assert(!WIDE || STAGES % 4 == 0, "a place of scales is free when the step that needs the next one is asked for");
     static_assert(!TURNED || (PLANES == 2 && (NI & (NI - 1)) == 0 && (BN & (BN - 1)) == 0 && BN >= 64), "exchange by exclusive or");
     static_assert(MI >= 2 && (2 * MI) % RING == 0, "rings turn whole in two steps");
 };
@@ -150,6 +164,16 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
     }
     auto issue = [&](int s) {
         const unsigned int to = (unsigned int)(s % T::STAGES) * T::STAGE;
+        if constexpr (T::WIDE) {
+            if ((s & 3) == 0) {
+                const int from = s + 4 <= steps ? s : steps - 4;
+#pragma unroll
+                for (int i = 0; i < T::SCALE_COPIES; ++i) {
+                    const int g = (wave * T::SCALE_COPIES + i) % T::SCALE_GROUPS;
+                    copy_rows_to_lds(sbase[g >= T::BM / 64] + (int64_t)from * 4, soff[i], T::STAGE * T::STAGES + (s >> 2 & 1) * T::SCALE_PLACE + g * 1024);
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < T::COPIES; ++i) {
             const int g = wave * T::COPIES + i;
@@ -161,7 +185,7 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
                 copy_rows_to_lds(base[g >= T::PLANES * GA] + (int64_t)s * TILE_STEP, voff[i], to + g * 1024);
             }
         }
-        if constexpr (T::PLANES == 1) {
+        if constexpr (T::PLANES == 1 && !T::WIDE) {
 #pragma unroll
             for (int i = 0; i < T::SCALE_COPIES; ++i) {
                 const int g = (wave * T::SCALE_COPIES + i) % T::SCALE_GROUPS;
@@ -169,25 +193,35 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
             }
         }
     };
+    // WIDE: the scales of steps s to s + 3, or of the last four
+    auto scales_from = [&](int s) { return (s & ~3) + 4 <= steps ? s & ~3 : steps - 4; };
+    auto scales_at = [&](int s, int row) {
+        if constexpr (T::WIDE)
+            return T::STAGE * T::STAGES + (s >> 2 & 1) * T::SCALE_PLACE + row * 16 + (s - scales_from(s)) * 4;
+        else
+            return (s % T::STAGES) * T::STAGE + T::GROUPS * 1024 + row * 4;
+    };
     const int frag = (lane & 15) * 64 + ((lane >> 4) ^ tile_swizzle((lane >> 2) & 3)) * 16;
     const int turn_row = 8 * (lane >> 4) + ((lane & 15) >> 2);
     const int turn = turn_row * 2 * T::BN + (lane & 3) * 8, turn_unit = (wn * T::NI) ^ tile_exchange<T>(turn_row);
     typedef typename T::Frag Frag;
+    constexpr int SCALE_ROW = T::WIDE ? 16 : 4;
+    const char* lane_scale = lds + (lane >> 4);
     Frag fa[T::RING], fb[T::BSETS][T::NI];
-    auto load_a = [&](const char* st, int mi, Frag& f) {
+    auto load_a = [&](const char* st, const char* sc, int mi, Frag& f) {
         if constexpr (T::PLANES == 1) {
             f.v = *(const u4*)(st + (wm * T::MI + mi) * 1024 + frag);
-            f.k = *(const unsigned char*)(st + T::GROUPS * 1024 + ((wm * T::MI + mi) * 16 + (lane & 15)) * 4 + (lane >> 4));
+            f.k = *(const unsigned char*)(sc + (wm * T::MI + mi) * 16 * SCALE_ROW);
         } else {
             f.hi = *(const h8*)(st + (wm * T::MI + mi) * 1024 + frag);
             f.lo = *(const h8*)(st + (GA + wm * T::MI + mi) * 1024 + frag);
         }
     };
-    auto load_b = [&](const char* st, int ni, Frag& f, auto which) {   // f16: 1 the first term, 2 the second
+    auto load_b = [&](const char* st, const char* sc, int ni, Frag& f, auto which) {   // f16: 1 the first term, 2 the second
         constexpr int WHICH = decltype(which)::value;
         if constexpr (T::PLANES == 1) {
             f.v = *(const u4*)(st + (GA + wn * T::NI + ni) * 1024 + frag);
-            f.k = *(const unsigned char*)(st + T::GROUPS * 1024 + (T::BM + (wn * T::NI + ni) * 16 + (lane & 15)) * 4 + (lane >> 4));
+            f.k = *(const unsigned char*)(sc + (T::BM + (wn * T::NI + ni) * 16) * SCALE_ROW);
         } else if constexpr (T::TURNED) {
             // two transposing reads of four rows each; lane i of 16 gets column i of the fragment
             const char* p = st + 2 * GA * 1024 + turn + ((turn_unit ^ ni) << 5);
@@ -212,9 +246,11 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
         const char* st = lds + (unsigned int)(s % T::STAGES) * T::STAGE;
         const char* next = lds + (unsigned int)((s + 1) % T::STAGES) * T::STAGE;
         const bool more = s + 1 < steps;
+        const char* sc = T::PLANES == 1 ? lane_scale + scales_at(s, lane & 15) : nullptr;
+        const char* next_sc = T::PLANES == 1 ? lane_scale + scales_at(more ? s + 1 : s, lane & 15) : nullptr;
         static_for<0, T::MI>([&](auto c) {
             constexpr int mi = decltype(c)::value;
-            if constexpr (mi + 2 < T::MI) load_a(st, mi + 2, fa[(P * T::MI + mi + 2) % T::RING]);
+            if constexpr (mi + 2 < T::MI) load_a(st, sc, mi + 2, fa[(P * T::MI + mi + 2) % T::RING]);
             if constexpr (mi == T::MI - 2) {
                 if (more) {
                     if (s + T::STAGES <= steps) tile_barrier<T::LOADS * (T::STAGES - 2)>();
@@ -224,9 +260,9 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
                 // (behind the last step: read once more what is there, into registers that nobody looks at)
                 if constexpr (T::BSETS == 2)
 #pragma unroll
-                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[NB][ni], std::integral_constant<int, 3>{});
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, next_sc, ni, fb[NB][ni], std::integral_constant<int, 3>{});
             }
-            if constexpr (mi >= T::MI - 2) load_a(next, mi + 2 - T::MI, fa[(P * T::MI + mi + 2) % T::RING]);
+            if constexpr (mi >= T::MI - 2) load_a(next, next_sc, mi + 2 - T::MI, fa[(P * T::MI + mi + 2) % T::RING]);
             const Frag& a = fa[(P * T::MI + mi) % T::RING];
             if constexpr (T::PLANES == 1) {
 #pragma unroll
@@ -242,7 +278,7 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
                                                                            : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].lo, a.hi, acc[mi][ni], 0, 0, 0);
                 if constexpr (mi == T::MI - 1)
 #pragma unroll
-                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[PB][ni], std::integral_constant<int, 2>{});
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, next_sc, ni, fb[PB][ni], std::integral_constant<int, 2>{});
 #pragma unroll
                 for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = T::FLIP ? __builtin_amdgcn_mfma_f32_16x16x32_f16(a.lo, fb[PB][ni].hi, acc[mi][ni], 0, 0, 0)
                                                                            : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].hi, a.lo, acc[mi][ni], 0, 0, 0);
@@ -251,7 +287,7 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
                                                                            : __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[PB][ni].hi, a.hi, acc[mi][ni], 0, 0, 0);
                 if constexpr (mi == T::MI - 1)
 #pragma unroll
-                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, ni, fb[PB][ni], std::integral_constant<int, 1>{});
+                    for (int ni = 0; ni < T::NI; ++ni) load_b(next, next_sc, ni, fb[PB][ni], std::integral_constant<int, 1>{});
             }
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -260,10 +296,11 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
     for (int s = 0; s < T::STAGES && s < steps; ++s) issue(s);
     if (steps >= T::STAGES) tile_barrier<T::LOADS * (T::STAGES - 1)>();
     else tile_barrier<0>();
+    const char* first_sc = T::PLANES == 1 ? lane_scale + scales_at(0, lane & 15) : nullptr;
 #pragma unroll
-    for (int ni = 0; ni < T::NI; ++ni) load_b(lds, ni, fb[0][ni], std::integral_constant<int, 3>{});
-    load_a(lds, 0, fa[0]);
-    load_a(lds, 1, fa[1]);
+    for (int ni = 0; ni < T::NI; ++ni) load_b(lds, first_sc, ni, fb[0][ni], std::integral_constant<int, 3>{});
+    load_a(lds, first_sc, 0, fa[0]);
+    load_a(lds, first_sc, 1, fa[1]);
     for (int s = 0; s < steps; s += T::UNROLL) {
         step(s, std::integral_constant<int, 0>{});
         if constexpr (T::UNROLL == 2) {
