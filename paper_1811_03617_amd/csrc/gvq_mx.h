@@ -11,6 +11,7 @@ struct MxQuantArgs {
     unsigned char *codes_t, *scales_t;   // blocks along columns (may be null), transposed, rows of ldct bytes
     int64_t ldc, ldct;               // filled in by the launcher, as are:
     int words, noise_words;          // rows are aligned for wide loads
+    int across;                      // tiles of 64 columns
 };
 
 // Bytes of one row of codes: a whole number of 128 columns; the scales take a sixteenth of that.
@@ -30,6 +31,13 @@ int gvq_launch_mx_few(const void* x_codes, const void* x_scales, const void* w_c
 bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x);
 int gvq_launch_mx_few_numbers(const void* x, gvq_dtype_t x_dtype, int64_t ld_x, const void* w_codes, const void* w_scales, int64_t rows,
                               int64_t n, int64_t k, void* out, gvq_dtype_t dtype, int64_t ld_out, hipStream_t st);
+
+// Neighbouring tiles for the work-groups of one XCD, to which they go round robin (8 of them).
+__device__ __forceinline__ int mx_tile_of(int block, int tiles)
+{
+    const int per = tiles >> 3, more = tiles & 7, x = block & 7;
+    return x * per + (x < more ? x : more) + (block >> 3);
+}
 
 // Eight numbers from p, of which `left` are in the matrix (the others are 0); `words`: p is 16-byte aligned.
 __device__ __forceinline__ void mx_load8(const float* p, bool words, int64_t left, float (&v)[8])
@@ -124,9 +132,9 @@ __device__ __forceinline__ float mx_scale(int code)
 
 // One number rounded stochastically: its magnitude lies u steps (1/2, 1 or 2) from 0; up if the fraction of a step is above
 // (z + 1/2) / 256.  Every step here is exact: a multiplication by powers of two, floor, a difference.
-__device__ __forceinline__ unsigned int mx_code_noise(float v, float inv_lo, float inv_hi, unsigned int z)
+__device__ __forceinline__ unsigned int mx_code_noise(float v, float inv, unsigned int z)
 {
-    float t = fminf(fabsf(v) * inv_lo * inv_hi, 6.f);
+    float t = fminf(fabsf(v) * inv, 6.f);
     const float per = t < 2.f ? 2.f : t < 4.f ? 1.f : 0.5f;      // steps in 1
     const float u = t * per, f = floorf(u);
     const float up = (u - f) * 256.f > (float)z + 0.5f ? 1.f : 0.f;
@@ -140,12 +148,10 @@ template <bool NOISE>
 __device__ __forceinline__ unsigned int mx_pack8(const float* v, const unsigned int (&z)[2], int code)
 {
     if constexpr (NOISE) {
-        // 2^(127 - code) in two factors, each a normal number
-        const int e = 127 - code, half = e >> 1;
-        const float lo = __uint_as_float((unsigned int)(half + 127) << 23), hi = __uint_as_float((unsigned int)(e - half + 127) << 23);
+        const float inv = __uint_as_float((unsigned int)(254 - code) << 23);   // 2^(127 - code), for codes of up to 252
         unsigned int q = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q |= mx_code_noise(v[i], lo, hi, z[i >> 2] >> (8 * (i & 3)) & 255u) << (4 * i);
+        for (int i = 0; i < 8; ++i) q |= mx_code_noise(v[i], inv, z[i >> 2] >> (8 * (i & 3)) & 255u) << (4 * i);
         return q;
     } else {
         const float s = mx_scale(code);

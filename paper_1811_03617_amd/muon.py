@@ -8,7 +8,7 @@ import numpy as np
 import torch
 
 from . import gvq
-from .mx import _dtype, _matrix
+from .mx import _check, _dtype, _matrix, _now, _workspace
 
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
@@ -23,25 +23,20 @@ def _coef(coefficients, steps):
     return table, len(table)
 
 
-def _workspace(batch, rows, cols, device):
-    return torch.empty(gvq.gvq_orthogonalize_workspace(batch, rows, cols), dtype=torch.uint8, device=device)
-
-
 def orthogonalize(g, steps=5, coefficients=None, eps=1e-7, dtype=None):
     """g ([rows, cols] or [batch, rows, cols]) with its singular values driven towards 1.  coefficients: (a, b, c) of every step
     instead of `steps` times the default."""
     if g.dim() not in (2, 3):
         raise ValueError(f"g: two or three dimensions are needed, not {g.dim()}")
-    b = g if g.dim() == 3 else g.unsqueeze(0)
-    batch, rows, cols = b.shape
-    code, ld = _matrix(b[0], "g") if batch else (_dtype(g.dtype, "g"), cols)
-    stride = b.stride(0) if batch > 1 else 0
-    if stride < 0:
-        raise ValueError("g: matrices have to lie one behind the other")
+    batch, rows, cols = g.shape if g.dim() == 3 else (1, *g.shape)
+    code, ld, _, _ = _matrix(g if g.dim() == 2 else g[0], "g") if batch else (_dtype(g.dtype, "g"), cols, 0, 0)
+    stride = g.stride(0) if batch > 1 else 0
     out = torch.empty(g.shape, dtype=dtype or g.dtype, device=g.device)
     coef, steps = _coef(coefficients, steps)
-    gvq.gvq_orthogonalize(g, code, batch, rows, cols, ld, stride, coef, steps, eps, out, _dtype(out.dtype, "dtype"), cols, rows * cols,
-                          _workspace(batch, rows, cols, g.device))
+    ws = _workspace(g.device, "gvq_orthogonalize_workspace", batch, rows, cols)
+    _check(gvq.lib().gvq_orthogonalize(g.data_ptr(), code, batch, rows, cols, ld, stride, coef if coef is None else coef.ctypes.data, steps,
+                                       eps, out.data_ptr(), _dtype(out.dtype, "dtype"), cols, rows * cols, ws.data_ptr(), _now()),
+           "gvq_orthogonalize")
     return out
 
 
@@ -49,14 +44,15 @@ def step(weight, grad, buffer, lr, momentum=0.95, weight_decay=0.0, nesterov=Tru
     """One step in place, of buffer (the momentum, float32) and weight (float32 or bfloat16): buffer <- momentum buffer + grad, and the
     weight moves against the orthogonalised buffer (nesterov: grad + momentum buffer).  scale: multiplies lr, sqrt(max(1, rows / cols))
     unless given."""
-    code_w, ld_w = _matrix(weight, "weight")
-    code_g, ld_g = _matrix(grad, "grad")
-    code_m, ld_m = _matrix(buffer, "buffer")
-    rows, cols = weight.shape
-    if grad.shape != weight.shape or buffer.shape != weight.shape or code_m != gvq.F32:
+    code_w, ld_w, rows, cols = _matrix(weight, "weight")
+    code_g, ld_g, rows_g, cols_g = _matrix(grad, "grad")
+    code_b, ld_b, rows_b, cols_b = _matrix(buffer, "buffer")
+    if (rows_g, cols_g) != (rows, cols) or (rows_b, cols_b) != (rows, cols) or code_b != gvq.F32:
         raise ValueError("grad and buffer: the weight's shape is needed, and float32 of the buffer")
     if scale is None:
         scale = max(1.0, rows / max(1, cols)) ** 0.5
     coef, steps = _coef(coefficients, steps)
-    gvq.gvq_muon_step(weight, code_w, ld_w, grad, code_g, ld_g, buffer, ld_m, rows, cols, lr, momentum, weight_decay, int(nesterov), scale,
-                      coef, steps, eps, _workspace(1, rows, cols, weight.device))
+    ws = _workspace(weight.device, "gvq_orthogonalize_workspace", 1, rows, cols)
+    _check(gvq.lib().gvq_muon_step(weight.data_ptr(), code_w, ld_w, grad.data_ptr(), code_g, ld_g, buffer.data_ptr(), ld_b, rows, cols, lr,
+                                   momentum, weight_decay, int(nesterov), scale, coef if coef is None else coef.ctypes.data, steps, eps,
+                                   ws.data_ptr(), _now()), "gvq_muon_step")
