@@ -23,7 +23,7 @@ int gvq_launch_mx_dequantize(const void* codes, const void* scales, int64_t rows
 // out = A B^T (+ out): A [m][k], B [n][k] in codes and scales.
 int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n,
                          int64_t k, void* out, gvq_dtype_t dtype, int64_t ld, bool accumulate, hipStream_t st);
-// ... of at most GVQ_MX_FEW_ROWS rows of A; of at most 16 rows of numbers, aligned to 16 bytes, quantised on the way
+// ... of at most GVQ_MX_FEW_ROWS rows of A; of at most 4 rows of numbers, aligned to 16 bytes, quantised on the way
 // (gvq_mx_few.hip).
 #define GVQ_MX_FEW_ROWS 16
 int gvq_launch_mx_few(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, int64_t rows, int64_t n,

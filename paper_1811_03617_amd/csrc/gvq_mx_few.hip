@@ -1,10 +1,10 @@
 // Products of at most 16 rows with a 4-bit matrix, y = x W^T: what there is to move is W, once.
 //
-// A work-group has 16 rows of W, its 16 waves take the sum in turns of 256 numbers (128 bytes of every row), and each lane reads
-// its operands straight into registers: row lane % 16, 16 bytes of codes and their scale.  Their loads run two turns ahead of the
-// products.  Rows of x in numbers are quantised on the way: the 32 numbers that a lane needs are one block, so the lane finds its
-// scale and packs its codes alone, without LDS and without a launch of its own.
-// The waves' sums are added in the order of the waves.
+// A work-group has 16 rows of W, its 16 waves take the sum in turns of 512 numbers (256 bytes of every row), and each lane reads
+// its operands straight into registers: row lane % 16, 16 bytes of codes a step, and four steps' scales in one word.  The loads run
+// a turn ahead of the products, with no branch around any of them (or every load would be waited for).  Up to four rows of x are
+// quantised on the way: the 32 numbers that a lane needs are one block, so the lane finds its scale and packs its codes alone, without
+// LDS and without a launch of its own.  More rows come in codes.
 #include "gvq_mx.h"
 #include "gvq_tile.h"
 
@@ -22,14 +22,14 @@ struct MxFewArgs {
     int accumulate, words;
 };
 
-// A block of 32 numbers as it lies in memory, or its codes and scale.
+// A block of 32 numbers as it lies in memory.
 template <typename X>
 struct FewBlock;
 
 template <>
 struct FewBlock<float> {
     u4 v[8];
-    __device__ __forceinline__ void load(const float* p, const char*)
+    __device__ __forceinline__ void load(const float* p)
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = *(const u4*)(p + 4 * i);
@@ -62,7 +62,7 @@ struct FewBlock<float> {
 template <>
 struct FewBlock<unsigned short> {
     u4 v[4];
-    __device__ __forceinline__ void load(const unsigned short* p, const char*)
+    __device__ __forceinline__ void load(const unsigned short* p)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = *(const u4*)(p + 8 * i);
@@ -98,93 +98,144 @@ struct FewBlock<unsigned short> {
     }
 };
 
-template <>
-struct FewBlock<unsigned char> {
-    u4 v;
-    int k;
-    __device__ __forceinline__ void load(const unsigned char* p, const char* s)
-    {
-        v = *(const u4*)p;
-        k = *(const unsigned char*)s;
-    }
-    __device__ __forceinline__ void pack(u4& q, int& code) const { q = v; code = k; }
-};
 __device__ __forceinline__ i8v few_operand(const u4& q) { return i8v{(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0}; }
 
-// X: float or unsigned short (bf16): numbers; unsigned char: codes.  16 rows at most.
-template <typename X, typename OUT>
-__global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(MxFewArgs a)
+struct MxScales4 {
+    unsigned int v[4];
+} __attribute__((aligned(4)));
+
+// The waves' sums of 16 rows of W, a lane four neighbouring results of one row of x, added in the order of the waves.
+template <typename OUT>
+__device__ __forceinline__ void few_out(const MxFewArgs& a, int n0, int wave, int lane, const f4& acc, f4 (*sums)[64])
 {
-    constexpr bool CODES = sizeof(X) == 1;
-    constexpr int TURN = sizeof(X) == 4 ? 1 : 2;   // steps of 128 numbers a wave takes at a time: 32 registers of numbers at most
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave != 0) return;
+    f4 v = acc;
+#pragma unroll
+    for (int i = 1; i < FEW_WAVES; ++i) v += sums[i][lane];
+    const int r = lane & 15, c = n0 + 4 * (lane >> 4);
+    if (r < a.rows && c < a.n) mx_store4((OUT*)a.out + (int64_t)r * a.ld_out + c, a.words != 0, a.n - c, a.accumulate != 0, v);
+}
+
+// At most four rows of numbers.  A wave packs the blocks of four steps at once, lane 16 b + 4 k + r that of row r, step k and block b
+// (alone they would fill a quarter of the lanes or less), and turns the lanes by 4 k for step k's product, where only the first
+// four of sixteen matter.  One row of 25088 numbers in bf16 to 4096: with the blocks of each step packed on their own 22 us, so
+// 15, of which W's bytes would take 9 to 11 alone.
+// Lane i of 16 gets what lane (i + N) % 16 has.
+template <int N>
+__device__ __forceinline__ unsigned int turn_lanes(unsigned int v)
+{
+    if constexpr (N == 0) return v;
+    else return (unsigned int)__builtin_amdgcn_mov_dpp((int)v, 0x120 + 16 - N, 0xf, 0xf, true);   // row_ror
+}
+
+template <typename X, typename OUT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void mx_four_kernel(MxFewArgs a)
+{
     __shared__ f4 sums[FEW_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int n0 = blockIdx.x * 16, b = lane >> 4, wr = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
+    const int64_t lds = a.ldw >> 4;
     const char* w = a.w + wr * a.ldw + 16 * b;
-    const char* ws = a.w_scales + wr * (a.ldw >> 4) + b;
-    const int64_t xr = (lane & 15) < a.rows ? lane & 15 : a.rows - 1;
-    const X* x = (const X*)a.x + xr * a.ld + (CODES ? 16 * b : 32 * b);
-    const char* xs = CODES ? a.x_scales + xr * (a.ld >> 4) + b : nullptr;
+    const char* ws = a.w_scales + wr * lds;
+    const int xr = lane & 3, kk = lane >> 2 & 3;
+    const X* x = (const X*)a.x + (int64_t)(xr < a.rows ? xr : a.rows - 1) * a.ld + 32 * b;
     f4 acc = {0.f, 0.f, 0.f, 0.f};
-    // Turn t of this wave: TURN steps from s0 + t FEW_WAVES TURN on; what is asked for behind the last one is the last one once
-    // more, and not multiplied.  Only whole steps of numbers: a branch around a load would have every load waited for.
-    const int steps = CODES ? a.steps : a.k / 128, s0 = wave * TURN;
-    const int turns = steps > s0 ? (steps - s0 + FEW_WAVES * TURN - 1) / (FEW_WAVES * TURN) : 0;
-    u4 q[2][TURN];
-    int k[2][TURN];
-    FewBlock<X> blocks[2][TURN];
+    // A turn is four whole steps of numbers; this wave has the turns wave, wave + FEW_WAVES, ..  What is asked for behind the last
+    // one is the last one once more.
+    const int whole = a.k / 128, turns_all = whole / 4;
+    const int turns = turns_all > wave ? (turns_all - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
+    u4 q[2][4];
+    MxScales4 k[2];
+    FewBlock<X> block[2];
     auto ask = [&](int t, int set) {
+        const int turn = t < turns ? wave + t * FEW_WAVES : wave + (turns - 1) * FEW_WAVES;
+        const int64_t s = 4 * (int64_t)turn;
+        block[set].load(x + (s + kk) * 128);
 #pragma unroll
-        for (int i = 0; i < TURN; ++i) {
-            const int next = s0 + t * (FEW_WAVES * TURN) + i, s = next < steps ? next : steps - 1;
-            q[set][i] = stream_load((const u4*)(w + (int64_t)s * TILE_STEP));
-            k[set][i] = *(const unsigned char*)(ws + (int64_t)s * 4);
-            blocks[set][i].load(x + (int64_t)s * (CODES ? TILE_STEP : 128), CODES ? xs + (int64_t)s * 4 : nullptr);
-        }
+        for (int i = 0; i < 4; ++i) q[set][i] = stream_load((const u4*)(w + (s + i) * TILE_STEP));
+        k[set] = *(const MxScales4*)(ws + s * 4);
     };
-    auto multiply = [&](const u4& wq, int wk, const FewBlock<X>& block) {
+    auto take = [&](int set) {
         u4 xq;
         int xk;
-        block.pack(xq, xk);
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(few_operand(wq), few_operand(xq), acc, 4, 4, 0, wk, 0, xk);
-    };
-    auto take = [&](int t, int set) {
-#pragma unroll
-        for (int i = 0; i < TURN; ++i)
-            if (s0 + t * (FEW_WAVES * TURN) + i < steps) multiply(q[set][i], k[set][i], blocks[set][i]);
+        block[set].pack(xq, xk);
+        static_for<0, 4>([&](auto c) {
+            constexpr int i = decltype(c)::value;
+            const u4 y = {turn_lanes<4 * i>(xq[0]), turn_lanes<4 * i>(xq[1]), turn_lanes<4 * i>(xq[2]), turn_lanes<4 * i>(xq[3])};
+            const int yk = (int)turn_lanes<4 * i>((unsigned int)xk);
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(few_operand(q[set][i]), few_operand(y), acc, 4, 4, 0,
+                                                                   (int)(k[set].v[i] >> (8 * b)), 0, yk);
+        });
     };
     if (turns > 0) ask(0, 0);
     for (int t = 0; t < turns; t += 2) {
         ask(t + 1, 1);
-        take(t, 0);
+        take(0);
         if (t + 1 >= turns) break;
         ask(t + 2, 0);
-        take(t + 1, 1);
+        take(1);
     }
-    if constexpr (!CODES)
-        if (steps < a.steps && wave == FEW_WAVES - 1) {   // what is left of the last step
-            FewBlock<X> block;
-            block.load_some(x + (int64_t)steps * 128, a.k - steps * 128 - 32 * b);
-            multiply(*(const u4*)(w + (int64_t)steps * TILE_STEP), *(const unsigned char*)(ws + (int64_t)steps * 4), block);
-        }
-    sums[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0) {
-        f4 v = acc;
-#pragma unroll
-        for (int i = 1; i < FEW_WAVES; ++i) v += sums[i][lane];
-        const int r = lane & 15, c = n0 + 4 * b;
-        if (r < a.rows && c < a.n) mx_store4((OUT*)a.out + (int64_t)r * a.ld_out + c, a.words != 0, a.n - c, a.accumulate != 0, v);
+    // what is left: up to three whole steps and a part of one, a wave each
+    const int rest = 4 * turns_all + (FEW_WAVES - 1 - wave);
+    if (rest < a.steps) {
+        FewBlock<X> last;
+        last.load_some(x + (int64_t)rest * 128, a.k - rest * 128 - 32 * b);
+        u4 xq;
+        int xk;
+        last.pack(xq, xk);
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(few_operand(*(const u4*)(w + (int64_t)rest * TILE_STEP)), few_operand(xq), acc, 4, 4, 0,
+                                                               *(const unsigned char*)(ws + (int64_t)rest * 4 + b), 0, xk);
     }
+    few_out<OUT>(a, n0, wave, lane, acc, sums);
 }
 
-template <typename X, typename OUT>
-static int launch_few(const MxFewArgs& a, hipStream_t st)
+// Rows of codes, up to 16: a turn is four steps here too, both operands' scales a word.
+template <typename OUT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(MxFewArgs a)
 {
-    const dim3 grid((a.n + 15) / 16), threads(64 * FEW_WAVES);
-    hipLaunchKernelGGL((mx_few_kernel<X, OUT>), grid, threads, 0, st, a);
-    GVQ_HIP(hipGetLastError());
-    return GVQ_OK;
+    __shared__ f4 sums[FEW_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int n0 = blockIdx.x * 16, b = lane >> 4, wr = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
+    const int64_t lds = a.ldw >> 4, xr = (lane & 15) < a.rows ? lane & 15 : a.rows - 1;
+    const char *w = a.w + wr * a.ldw + 16 * b, *x = (const char*)a.x + xr * a.ldw + 16 * b;
+    const char *ws = a.w_scales + wr * lds, *xs = a.x_scales + xr * lds;
+    f4 acc = {0.f, 0.f, 0.f, 0.f};
+    const int turns_all = a.steps / 4, turns = turns_all > wave ? (turns_all - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
+    u4 q[2][4], y[2][4];
+    MxScales4 k[2], yk[2];
+    auto ask = [&](int t, int set) {
+        const int turn = t < turns ? wave + t * FEW_WAVES : wave + (turns - 1) * FEW_WAVES;
+        const int64_t s = 4 * (int64_t)turn;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            q[set][i] = stream_load((const u4*)(w + (s + i) * TILE_STEP));
+            y[set][i] = *(const u4*)(x + (s + i) * TILE_STEP);
+        }
+        k[set] = *(const MxScales4*)(ws + s * 4);
+        yk[set] = *(const MxScales4*)(xs + s * 4);
+    };
+    auto take = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(few_operand(q[set][i]), few_operand(y[set][i]), acc, 4, 4, 0,
+                                                                   (int)(k[set].v[i] >> (8 * b)), 0, (int)(yk[set].v[i] >> (8 * b)));
+    };
+    if (turns > 0) ask(0, 0);
+    for (int t = 0; t < turns; t += 2) {
+        ask(t + 1, 1);
+        take(0);
+        if (t + 1 >= turns) break;
+        ask(t + 2, 0);
+        take(1);
+    }
+    const int rest = 4 * turns_all + (FEW_WAVES - 1 - wave);   // up to three more steps, a wave each
+    if (rest < a.steps)
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            few_operand(*(const u4*)(w + (int64_t)rest * TILE_STEP)), few_operand(*(const u4*)(x + (int64_t)rest * TILE_STEP)), acc, 4, 4, 0,
+            *(const unsigned char*)(ws + (int64_t)rest * 4 + b), 0, *(const unsigned char*)(xs + (int64_t)rest * 4 + b));
+    few_out<OUT>(a, n0, wave, lane, acc, sums);
 }
 
 static MxFewArgs few_args(const void* w_codes, const void* w_scales, int64_t rows, int64_t n, int64_t k, void* out, gvq_dtype_t dtype,
@@ -201,17 +252,25 @@ static MxFewArgs few_args(const void* w_codes, const void* w_scales, int64_t row
     return a;
 }
 
+template <typename K>
+static int launch_few(K kernel, const MxFewArgs& a, hipStream_t st)
+{
+    hipLaunchKernelGGL(kernel, dim3((a.n + 15) / 16), dim3(64 * FEW_WAVES), 0, st, a);
+    GVQ_HIP(hipGetLastError());
+    return GVQ_OK;
+}
+
 int gvq_launch_mx_few(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, int64_t rows, int64_t n,
                       int64_t k, void* out, gvq_dtype_t dtype, int64_t ld_out, bool accumulate, hipStream_t st)
 {
     MxFewArgs a = few_args(w_codes, w_scales, rows, n, k, out, dtype, ld_out, accumulate);
     a.x = x_codes; a.x_scales = (const char*)x_scales; a.ld = a.ldw;
-    return dtype == GVQ_BF16 ? launch_few<unsigned char, unsigned short>(a, st) : launch_few<unsigned char, float>(a, st);
+    return dtype == GVQ_BF16 ? launch_few(mx_few_kernel<unsigned short>, a, st) : launch_few(mx_few_kernel<float>, a, st);
 }
 
 bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x)
 {
-    return rows <= 16 && (((uintptr_t)x | (uintptr_t)(ld_x * (x_dtype == GVQ_BF16 ? 2 : 4))) & 15) == 0;
+    return rows <= 4 && (((uintptr_t)x | (uintptr_t)(ld_x * (x_dtype == GVQ_BF16 ? 2 : 4))) & 15) == 0;
 }
 
 int gvq_launch_mx_few_numbers(const void* x, gvq_dtype_t x_dtype, int64_t ld_x, const void* w_codes, const void* w_scales, int64_t rows,
@@ -220,6 +279,6 @@ int gvq_launch_mx_few_numbers(const void* x, gvq_dtype_t x_dtype, int64_t ld_x, 
     MxFewArgs a = few_args(w_codes, w_scales, rows, n, k, out, dtype, ld_out, false);
     a.x = x; a.ld = ld_x;
     if (x_dtype == GVQ_BF16)
-        return dtype == GVQ_BF16 ? launch_few<unsigned short, unsigned short>(a, st) : launch_few<unsigned short, float>(a, st);
-    return dtype == GVQ_BF16 ? launch_few<float, unsigned short>(a, st) : launch_few<float, float>(a, st);
+        return dtype == GVQ_BF16 ? launch_few(mx_four_kernel<unsigned short, unsigned short>, a, st) : launch_few(mx_four_kernel<unsigned short, float>, a, st);
+    return dtype == GVQ_BF16 ? launch_few(mx_four_kernel<float, unsigned short>, a, st) : launch_few(mx_four_kernel<float, float>, a, st);
 }
