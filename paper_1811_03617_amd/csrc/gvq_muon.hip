@@ -18,7 +18,23 @@ struct PrepArgs {
     char* x;             // planes of the first matrix, `per` bytes further for each next one
     int64_t per, plane;  // plane: numbers
     int64_t ld;
+    int tx, words;       // threads side by side, as a power of two; four neighbouring numbers are aligned words
 };
+
+// Four neighbouring numbers of a row a thread, 1 << tx threads side by side and rows under each other; `at(r, c)` for every such
+// four.  Runs of rows and columns are handed out one after the other; 32-bit indices (a 64-bit division for each number
+// took as long as its memory).
+template <typename F>
+__device__ __forceinline__ void for_fours(const PrepArgs& a, int cols, F at)
+{
+    const int across = 1 << a.tx, down = MUON_THREADS >> a.tx, rows = (int)a.p.rows;
+    const int chunks = (cols + 4 * across - 1) / (4 * across), units = (rows + down - 1) / down * chunks;
+    const int x = 4 * (threadIdx.x & (across - 1)), y = threadIdx.x >> a.tx;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int g = u / chunks, r = g * down + y, c = (u - g * chunks) * 4 * across + x;
+        if (r < rows && c < cols) at(r, c);
+    }
+}
 
 // M <- beta M + G, and the sum of squares of U, in float64 (squares of fp32 numbers are exact there and do not overflow).
 template <typename G>
@@ -27,50 +43,102 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_norm_kernel(PrepArgs a)
     __shared__ double lds[MUON_THREADS / 64];
     const G* g = (const G*)a.p.grad + blockIdx.y * a.p.stride_grad;
     double s = 0;
-    const int64_t n = a.p.rows * a.p.cols, step = (int64_t)gridDim.x * MUON_THREADS;
-    for (int64_t i = (int64_t)blockIdx.x * MUON_THREADS + threadIdx.x; i < n; i += step) {
-        const int64_t r = i / a.p.cols, c = i - r * a.p.cols;
-        const float u = momentum_at<G>(a.p, g, r, c);
-        s += (double)u * u;
-    }
+    const int cols = (int)a.p.cols;
+    for_fours(a, cols, [&](int r, int c) {
+        float u[4];
+        if (a.words && c + 4 <= cols) {
+            four_numbers(g + r * a.p.ld_grad + c, u);
+            if (a.p.momentum) {
+                f4* m = (f4*)(a.p.momentum + r * a.p.ld_momentum + c);
+                const f4 v = a.p.beta * *m + f4{u[0], u[1], u[2], u[3]};
+                *m = v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = a.p.nesterov ? u[i] + a.p.beta * v[i] : v[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = c + i < cols ? momentum_at<G>(a.p, g, r, c + i) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += (double)u[i] * u[i];
+    });
     s = group_sum<MUON_THREADS>(s, lds);
     if (threadIdx.x == 0) a.sums[blockIdx.y * a.p.parts + blockIdx.x] = s;
 }
 
-// U / (|U| + eps) into the two planes of X, with zeros behind the last column: 64 x 64 numbers a work-group, through LDS if X is
-// the transpose.
+template <typename G>
+__device__ __forceinline__ double scale_to_x(const PrepArgs& a, int matrix, double* lds)
+{
+    double s = 0;
+    for (int i = threadIdx.x; i < a.p.parts; i += MUON_THREADS) s += a.sums[matrix * a.p.parts + i];
+    return 1.0 / (sqrt(group_sum<MUON_THREADS>(s, lds)) + a.p.eps) * UNIT_X;
+}
+
+// U / (|U| + eps) into the two planes of X, with zeros behind the last column.
 template <typename G>
 __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
 {
     __shared__ double lds[MUON_THREADS / 64];
+    const double inv = scale_to_x<G>(a, blockIdx.y, lds);
+    const G* g = (const G*)a.p.grad + blockIdx.y * a.p.stride_grad;
+    _Float16* X = (_Float16*)(a.x + blockIdx.y * a.per);
+    const int cols = (int)a.p.cols;
+    for_fours(a, (int)a.ld, [&](int r, int c) {
+        float u[4];
+        if (a.words && c + 4 <= cols) {
+            four_numbers(g + r * a.p.ld_grad + c, u);
+            if (a.p.momentum) {
+                const f4 m = *(const f4*)(a.p.momentum + r * a.p.ld_momentum + c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = a.p.nesterov ? u[i] + a.p.beta * m[i] : m[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = c + i < cols ? direction_at<G>(a.p, g, r, c + i) : 0.f;
+        }
+        h4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            _Float16 h, l;
+            split_f16(c + i < cols ? (float)((double)u[i] * inv) : 0.f, h, l);
+            hi[i] = h; lo[i] = l;
+        }
+        *(h4*)(X + r * a.ld + c) = hi;
+        *(h4*)(X + a.plane + r * a.ld + c) = lo;
+    });
+}
+
+// The same where X is the transpose: 64 x 64 numbers a work-group, through LDS.
+template <typename G>
+__global__ __launch_bounds__(MUON_THREADS) void muon_turn_kernel(PrepArgs a)
+{
+    __shared__ double lds[MUON_THREADS / 64];
     __shared__ float tile[64 * 65];
-    double s = 0;
-    for (int i = threadIdx.x; i < a.p.parts; i += MUON_THREADS) s += a.sums[blockIdx.z * a.p.parts + i];
-    const double inv = 1.0 / (sqrt(group_sum<MUON_THREADS>(s, lds)) + a.p.eps) * UNIT_X;
+    const double inv = scale_to_x<G>(a, blockIdx.z, lds);
     const G* g = (const G*)a.p.grad + blockIdx.z * a.p.stride_grad;
     _Float16* X = (_Float16*)(a.x + blockIdx.z * a.per);
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
     const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
-    auto put = [&](int64_t at, float v) {
-        _Float16 hi, lo;
-        split_f16(v, hi, lo);
-        X[at] = hi;
-        X[a.plane + at] = lo;
-    };
-#pragma unroll 4
-    for (int y = y0; y < 64; y += MUON_THREADS / 64) {
-        const int64_t r = r0 + y, c = c0 + x;
-        float v = 0.f;
-        if (r < a.p.rows && c < a.p.cols) v = (float)((double)direction_at<G>(a.p, g, r, c) * inv);
-        if (a.p.turn) tile[y * 65 + x] = v;
-        else if (r < a.p.rows && c < a.ld) put(r * a.ld + c, v);
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int64_t r = r0 + y0 + 4 * i, c = c0 + x;
+        const bool in = r < a.p.rows && c < a.p.cols;
+        const float u = direction_at<G>(a.p, g, r < a.p.rows ? r : a.p.rows - 1, c < a.p.cols ? c : a.p.cols - 1);
+        v[i] = in ? (float)((double)u * inv) : 0.f;
     }
-    if (!a.p.turn) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tile[(y0 + 4 * i) * 65 + x] = v[i];
     __syncthreads();
 #pragma unroll 4
     for (int y = y0; y < 64; y += MUON_THREADS / 64) {
         const int64_t c = c0 + y, r = r0 + x;
-        if (c < a.p.cols && r < a.ld) put(c * a.ld + r, tile[x * 65 + y]);
+        if (c < a.p.cols && r < a.ld) {
+            _Float16 hi, lo;
+            split_f16(tile[x * 65 + y], hi, lo);
+            X[c * a.ld + r] = hi;
+            X[a.plane + c * a.ld + r] = lo;
+        }
     }
 }
 
@@ -421,9 +489,21 @@ float gvq_muon_coef(const MuonArgs& m, int step, int i)
     return (float)(m.coef ? m.coef[3 * step + i] : standard[i]);
 }
 
-int gvq_launch_muon_norm(const MuonArgs& m, const MuonPrep& p, double* sums, hipStream_t st)
+static PrepArgs prep_args(const MuonArgs& m)
 {
     PrepArgs q{};
+    q.p = gvq_muon_prep(m);
+    q.tx = 2;
+    while (q.tx < 8 && (4 << q.tx) < m.x.cols) ++q.tx;
+    const uintptr_t es = m.grad_dtype == GVQ_BF16 ? 2 : 4;
+    q.words = ((((uintptr_t)m.grad | (uintptr_t)m.ld_grad * es | (uintptr_t)m.stride_grad * es) & (4 * es - 1)) |
+               (((uintptr_t)m.momentum | (uintptr_t)m.ld_momentum * 4) & 15)) == 0;
+    return q;
+}
+
+int gvq_launch_muon_norm(const MuonArgs& m, const MuonPrep& p, double* sums, hipStream_t st)
+{
+    PrepArgs q = prep_args(m);
     q.p = p;
     q.sums = sums;
     const dim3 grid(p.parts, (unsigned)m.x.batch);
@@ -530,17 +610,22 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
     const int64_t batch = m.x.batch;
     const bool wide = m.x.rows <= m.x.cols;
     char* w = m.workspace;
-    PrepArgs q{};
-    q.p = gvq_muon_prep(m);
+    PrepArgs q = prep_args(m);
     q.sums = (double*)(w + p.sums);
     q.x = w + p.x[0]; q.per = p.per; q.plane = p.m * p.ldn; q.ld = p.ldn;
     int rc = gvq_launch_muon_norm(m, q.p, q.sums, st);
     if (rc != GVQ_OK) return rc;
-    // the padding of X's rows is written too: behind the columns, or behind the rows
-    const int64_t down = wide ? m.x.rows : p.ldn, across = wide ? p.ldn : m.x.cols;
-    const dim3 grid((unsigned)((across + 63) / 64), (unsigned)((down + 63) / 64), (unsigned)batch);
-    if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), grid, dim3(MUON_THREADS), 0, st, q);
-    else hipLaunchKernelGGL((muon_planes_kernel<float>), grid, dim3(MUON_THREADS), 0, st, q);
+    // (the padding of X's rows is written too)
+    const dim3 threads(MUON_THREADS);
+    if (wide) {
+        const dim3 grid((unsigned)(p.parts), (unsigned)batch);
+        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), grid, threads, 0, st, q);
+        else hipLaunchKernelGGL((muon_planes_kernel<float>), grid, threads, 0, st, q);
+    } else {
+        const dim3 grid((unsigned)((m.x.cols + 63) / 64), (unsigned)((p.ldn + 63) / 64), (unsigned)batch);
+        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_turn_kernel<unsigned short>), grid, threads, 0, st, q);
+        else hipLaunchKernelGGL((muon_turn_kernel<float>), grid, threads, 0, st, q);
+    }
     GVQ_HIP(hipGetLastError());
     const int mm = (int)p.m, nn = (int)p.n;
     const int64_t es = m.out_dtype == GVQ_BF16 ? 2 : 4;

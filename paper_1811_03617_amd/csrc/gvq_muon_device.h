@@ -31,6 +31,22 @@ __device__ __forceinline__ double group_sum(double v, double* lds)
 __device__ __forceinline__ float number_at(const float* g, int64_t i) { return g[i]; }
 __device__ __forceinline__ float number_at(const unsigned short* g, int64_t i) { return bf16_to_f32(g[i]); }
 
+__device__ __forceinline__ void four_numbers(const float* p, float (&u)[4])   // from an aligned place
+{
+    const f4 v = *(const f4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = v[i];
+}
+__device__ __forceinline__ void four_numbers(const unsigned short* p, float (&u)[4])
+{
+    const u2 v = *(const u2*)p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        u[2 * i] = __uint_as_float(v[i] << 16);
+        u[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+}
+
 // U at row r and column c as the momentum already is.
 template <typename G>
 __device__ __forceinline__ float direction_at(const MuonPrep& a, const G* g, int64_t r, int64_t c)

@@ -98,7 +98,7 @@ struct TileShape {
     static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && GROUPS % WAVES == 0, "whole fragments and copies");
     static_assert(SCALE_GROUPS * 64 == (PLANES == 1 ? BM + BN : 0), "whole copies of scales");
     static_assert(LDS <= 160 * 1024 && (LOADS + SCALE_COPIES) * STAGES < 64, "LDS and vmcnt");
-    static_assert(!WIDE || STAGES % 4 == 0, "a place of scales is free when the step that needs the next one is asked for");
+    static_assert(!WIDE || STAGES <= 4, "a place of scales is free when the step that needs the next one is asked for");
     static_assert(!TURNED || (PLANES == 2 && (NI & (NI - 1)) == 0 && (BN & (BN - 1)) == 0 && BN >= 64), "exchange by exclusive or");
     static_assert(MI >= 2 && (2 * MI) % RING == 0, "rings turn whole in two steps");
 };
