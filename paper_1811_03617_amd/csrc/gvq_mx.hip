@@ -5,7 +5,9 @@
 // 0, 1/2, 1, 3/2, 2, 3, 4, 6 (ties to the even code, above 6 to 6) with its sign in front.  The conversion instruction does the
 // division, the rounding and the saturation; it agrees with that definition on all 65536 bf16 numbers and on fp32 numbers around
 // every tie, at scales from the smallest to the largest, so rounding here is exact: nothing is lost but what the format loses.
-// Bound: memory.  A matrix is read once; both directions' blocks come out of the same pass, the columns' ones through LDS.
+// Bound: memory, and with random bytes the 20 instructions that each of a number's two roundings takes.  A matrix is read once; both
+// directions' blocks come out of the same pass, the columns' ones through LDS.  Rows of 8192 x 4096 bf16 numbers 16.6 us (5.1 TB/s),
+// columns of 4096 x 25088 59 (4.4), both ways of 8191 x 4093 fp32 numbers with random bytes 83 (2.5), back into fp32 27 (5.6).
 #include "gvq_mx.h"
 
 #define MXQ_THREADS 256
