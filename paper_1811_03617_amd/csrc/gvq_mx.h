@@ -23,12 +23,13 @@ int gvq_launch_mx_dequantize(const void* codes, const void* scales, int64_t rows
 // out = A B^T (+ out): A [m][k], B [n][k] in codes and scales.
 int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n,
                          int64_t k, void* out, gvq_dtype_t dtype, int64_t ld, bool accumulate, hipStream_t st);
-// ... of at most GVQ_MX_FEW_ROWS rows of A; of at most 4 rows of numbers, aligned to 16 bytes, quantised on the way
-// (gvq_mx_few.hip).
-#define GVQ_MX_FEW_ROWS 16
-int gvq_launch_mx_few(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, int64_t rows, int64_t n,
+// About how many us that takes.
+double gvq_mx_product_time(int64_t m, int64_t n, int64_t k);
+// The same without LDS, `tiles` (1 or 2) times 16 rows of A a work-group; of at most 4 rows of numbers, aligned to 16 bytes and quantised on
+// the way, where that is the faster way (gvq_mx_few.hip).
+int gvq_launch_mx_few(int tiles, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, int64_t rows, int64_t n,
                       int64_t k, void* out, gvq_dtype_t dtype, int64_t ld_out, bool accumulate, hipStream_t st);
-bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x);
+bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k);
 int gvq_launch_mx_few_numbers(const void* x, gvq_dtype_t x_dtype, int64_t ld_x, const void* w_codes, const void* w_scales, int64_t rows,
                               int64_t n, int64_t k, void* out, gvq_dtype_t dtype, int64_t ld_out, hipStream_t st);
 

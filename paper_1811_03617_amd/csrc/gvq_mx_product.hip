@@ -113,18 +113,34 @@ struct MxShape {
 };
 static const MxShape mx_shapes[4] = {{256, 256, 8.0, 0.95, 1}, {256, 128, 2.5, 0.67, 1}, {128, 128, 1.0, 0.39, 1}, {64, 64, 2.0, 0.255, 2}};
 
+// The time of the fastest shape, and which it is.
+static double tile_time(int64_t m, int64_t n, int64_t steps, int& best)
+{
+    double least = 1e300;
+    for (int k = 0; k < 4; ++k) {
+        const MxShape& s = mx_shapes[k];
+        const int64_t tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
+        const double t = (double)((tiles + 256 * s.per_cu - 1) / (256 * s.per_cu)) * (s.start_us + s.step_us * steps);
+        if (t < least) { least = t; best = k; }
+    }
+    return least;
+}
+
+// The kernels without LDS (gvq_mx_few.hip), `tiles` times 16 rows of A and 16 of B a work-group: rounds over 256 compute units again.  Fitted to
+// 120 products of 17 to 500 rows, 512 to 4096 columns and sums of 256 to 25088, where the better of the two is up to four times faster than any tile
+// (77 x 1000 x 4096 5.9 us and 11.5, 48 x 512 x 25088 14.4 and 56) and up to four times slower where work-groups are many.
+static double few_time(int64_t m, int64_t n, int64_t steps, int tiles)
+{
+    const int64_t groups = ((m + 16 * tiles - 1) / (16 * tiles)) * ((n + 15) / 16);
+    return 1.5 + (double)((groups + 255) / 256) * (tiles == 1 ? 0.45 + 0.06 * steps : 0.3 + 0.096 * steps);
+}
+
 template <typename OUT>
 static int launch_product(const MxProductArgs& a, hipStream_t st)
 {
     if (a.steps < 4) return launch_tile<TileShape<64, 64, 2, 2, 1, 4, false, false, true>, OUT>(a, st);
     int best = 3;
-    double least = 1e300;
-    for (int k = 0; k < 4; ++k) {
-        const MxShape& s = mx_shapes[k];
-        const int64_t tiles = (int64_t)((a.a.rows + s.bm - 1) / s.bm) * ((a.b.rows + s.bn - 1) / s.bn);
-        const double t = (double)((tiles + 256 * s.per_cu - 1) / (256 * s.per_cu)) * (s.start_us + s.step_us * a.steps);
-        if (t < least) { least = t; best = k; }
-    }
+    tile_time(a.a.rows, a.b.rows, a.steps, best);
     switch (best) {
     case 0: return launch_tile<TileShape<256, 256, 2, 4, 1, 4>, OUT>(a, st);
     case 1: return launch_tile<TileShape<256, 128, 4, 2, 1, 4>, OUT>(a, st);
@@ -133,11 +149,30 @@ static int launch_product(const MxProductArgs& a, hipStream_t st)
     }
 }
 
+// few: times 16 rows of A a work-group without LDS, 0: tiles.
+struct MxWay {
+    int few;
+    double us;
+};
+static MxWay way_of(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t steps = gvq_mx_row_bytes(k) / TILE_STEP;
+    int shape;
+    const double tile = tile_time(m, n, steps, shape), one = few_time(m, n, steps, 1), two = few_time(m, n, steps, 2);
+    if (one <= two && one < tile) return {1, one};
+    return two < tile ? MxWay{2, two} : MxWay{0, tile};
+}
+
+double gvq_mx_product_time(int64_t m, int64_t n, int64_t k) { return way_of(m, n, k).us; }
+
 int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n,
                          int64_t k, void* out, gvq_dtype_t dtype, int64_t ld, bool accumulate, hipStream_t st)
 {
-    if (m <= GVQ_MX_FEW_ROWS && k > 0)
-        return gvq_launch_mx_few(a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, accumulate, st);
+    if (k > 0) {
+        const MxWay way = way_of(m, n, k);
+        if (way.few)
+            return gvq_launch_mx_few(way.few, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, accumulate, st);
+    }
     MxProductArgs a;
     const int64_t row = gvq_mx_row_bytes(k), es = dtype == GVQ_BF16 ? 2 : 4;
     a.a = TileOperand{(const char*)a_codes, 0, row, (int)m, (const char*)a_scales, 0};

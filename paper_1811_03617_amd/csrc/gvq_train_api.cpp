@@ -79,7 +79,7 @@ int gvq_mx_linear(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, 
     if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(y_dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16) ||
         !aligned(workspace, 16))
         return GVQ_EALIGN;
-    if (n_in > 0 && gvq_mx_few_numbers_takes(x, dtype, rows, ld_x))
+    if (n_in > 0 && gvq_mx_few_numbers_takes(x, dtype, rows, ld_x, n_out, n_in))
         return gvq_launch_mx_few_numbers(x, dtype, ld_x, w_codes, w_scales, rows, n_out, n_in, y, y_dtype, ld_y, (hipStream_t)stream);
     char* w = (char*)workspace;
     char* ws = w + up256(codes_of(rows, n_in));
