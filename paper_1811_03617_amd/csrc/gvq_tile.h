@@ -22,7 +22,9 @@ typedef int i8v __attribute__((ext_vector_type(8)));
 
 // global -> LDS, `voff` bytes behind the wave-uniform `base` for each lane, 16 (or 4) bytes a lane to consecutive places from the
 // wave-uniform byte offset `lds` on.  Inline assembly: the compiler would otherwise wait for every such copy before any LDS read.
-// m0 carries the LDS offset and is named as clobbered on purpose.
+// m0 carries the LDS offset and is named as clobbered on purpose.  The compiler keeps `base` in vector registers where it likes and
+// reads it into scalar ones right before the copy; a scalar register that a vector instruction wrote may be an address five wait
+// states later at the earliest, and the compiler puts no such waits in front of inline assembly: the five are s_mov and s_nop 3.
 __device__ __forceinline__ const void* in_scalars(const void* p)
 {
     const uint64_t v = (uint64_t)p;
@@ -34,13 +36,13 @@ __device__ __forceinline__ const void* in_scalars(const void* p)
 __device__ __forceinline__ void copy_rows_to_lds(const void* base, unsigned int voff, unsigned int lds)
 {
     base = in_scalars(base);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(voff), "s"(lds), "s"(base)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(voff), "s"(lds), "s"(base)
                  : "memory", "m0");
 }
 __device__ __forceinline__ void copy_words_to_lds(const void* base, unsigned int voff, unsigned int lds)
 {
     base = in_scalars(base);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, %2" ::"v"(voff), "s"(lds), "s"(base)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, %2" ::"v"(voff), "s"(lds), "s"(base)
                  : "memory", "m0");
 }
 #pragma clang diagnostic pop
