@@ -246,7 +246,7 @@ constexpr int ns_lds()
 template <typename T, int KIND, typename OUT, bool SPLIT>
 __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
 {
-    extern __shared__ char lds[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr bool SYM = KIND == NS_GRAM || KIND == NS_POLY;
     const int tiles = SYM ? a.nm * (a.nm + 1) / 2 : a.nm * a.nn;
     int tm, tn, split = 0, step0 = 0, steps = a.steps;
@@ -368,7 +368,7 @@ template <int KIND, typename OUT, bool TURN>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a)
 {
     constexpr bool SYM = KIND == NS_GRAM || KIND == NS_POLY;
-    __shared__ float tile[32 * 36];
+    __shared__ __attribute__((aligned(16))) float tile[32 * 36];
     int tm, tn;
     if (SYM) triangle_at(blockIdx.x, tm, tn);
     else { tm = blockIdx.x / a.nn; tn = blockIdx.x - tm * a.nn; }

@@ -208,7 +208,7 @@ __device__ __forceinline__ void results(const MuonSmallArgs& a, OUT* out, int R,
 template <typename G, typename OUT, int WIDTH>
 __global__ __launch_bounds__(MS_THREADS) void muon_one_kernel(MuonSmallArgs a, MuonCoef coef)
 {
-    extern __shared__ char lds[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ double red[MS_THREADS / 64];
     const int cols = (a.n + 31) & ~31, ld = cols + 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Slab X = {(_Float16*)lds, MS_M * ld, ld};
@@ -314,7 +314,7 @@ __device__ __forceinline__ void slab_words(const MuonSmallArgs& a, int cols, L l
 template <typename G, typename OUT, bool FIRST, bool LAST>
 __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
 {
-    extern __shared__ char lds[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ double red[MS_THREADS / 64];
     constexpr int LD = MS_SLAB + 8, TILES = MS_SLAB / 128;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

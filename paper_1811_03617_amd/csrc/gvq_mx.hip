@@ -52,8 +52,8 @@ __device__ __forceinline__ int mx_place(int r, int c) { return r * 64 + (c ^ (16
 template <typename T, bool NOISE, bool ROWS>
 __global__ __launch_bounds__(MXQ_THREADS) void mx_both_kernel(MxQuantArgs a)
 {
-    __shared__ float tile[128 * 64];
-    __shared__ unsigned char dust[NOISE ? 128 * 64 : 16];
+    __shared__ __attribute__((aligned(16))) float tile[128 * 64];
+    __shared__ __attribute__((aligned(16))) unsigned char dust[NOISE ? 128 * 64 : 16];
     const int t = mx_tile_of(blockIdx.x, gridDim.x);
     const int64_t r0 = (int64_t)(t / a.across) * 128, c0 = (int64_t)(t % a.across) * 64;
     const bool whole = r0 + 128 <= a.rows && c0 + 64 <= a.cols;

@@ -31,7 +31,7 @@ __device__ __forceinline__ void mx_lds4(unsigned short* p, f4 v) { *(u2*)p = u2{
 template <typename T, typename OUT>
 __global__ __launch_bounds__(T::THREADS) void mx_tile_kernel(MxProductArgs a)
 {
-    extern __shared__ char lds[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     int tm, tn;
     tile_at(tile_of_block(blockIdx.x, a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
     f4 acc[T::MI][T::NI];

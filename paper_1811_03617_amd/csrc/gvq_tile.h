@@ -47,6 +47,12 @@ __device__ __forceinline__ void copy_words_to_lds(const void* base, unsigned int
 }
 #pragma clang diagnostic pop
 
+// Where a copy's destination lies among the work-group's LDS: `p` is not always the first of it.
+__device__ __forceinline__ unsigned int lds_offset(const char* p)
+{
+    return (unsigned int)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+
 // All but the youngest N copies of this wave have arrived and its LDS reads are done; then the other waves' too.
 template <int N>
 __device__ __forceinline__ void tile_barrier()
@@ -127,13 +133,14 @@ __device__ __forceinline__ int tile_exchange(int row)
 
 // acc[mi][ni][i] += C[row0 + wave's rows + 16 mi + lane % 16][col0 + wave's columns + 16 ni + 4 (lane / 16) + i] (FLIP: row 4 (lane / 16) + i,
 // column lane % 16), over the steps [step0, step0 + steps) of the sum.  Four neighbouring columns a lane come from giving the matrix
-// instruction the operands in exchanged roles.
+// instruction the operands in exchanged roles.  lds: T::LDS bytes, aligned to 16.
 template <typename T>
 __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOperand& B, int row0, int col0, int step0, int steps,
                                              char* lds, f4 (&acc)[T::MI][T::NI])
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave / T::WN, wn = wave % T::WN;
+    const unsigned int lds0 = lds_offset(lds);
     const char* base[2] = {A.p + (int64_t)row0 * A.ld + (int64_t)step0 * TILE_STEP,
                            T::TURNED ? B.p + (int64_t)step0 * 32 * B.ld + (int64_t)col0 * 2
                                      : B.p + (int64_t)col0 * B.ld + (int64_t)step0 * TILE_STEP};
@@ -171,14 +178,15 @@ __device__ __forceinline__ void tile_product(const TileOperand& A, const TileOpe
         }
     }
     auto issue = [&](int s) {
-        const unsigned int to = (unsigned int)(s % T::STAGES) * T::STAGE;
+        const unsigned int to = lds0 + (unsigned int)(s % T::STAGES) * T::STAGE;
         if constexpr (T::WIDE) {
             if ((s & 3) == 0) {
                 const int from = s + 4 <= steps ? s : steps - 4;
 #pragma unroll
                 for (int i = 0; i < T::SCALE_COPIES; ++i) {
                     const int g = (wave * T::SCALE_COPIES + i) % T::SCALE_GROUPS;
-                    copy_rows_to_lds(sbase[g >= T::BM / 64] + (int64_t)from * 4, soff[i], T::STAGE * T::STAGES + (s >> 2 & 1) * T::SCALE_PLACE + g * 1024);
+                    copy_rows_to_lds(sbase[g >= T::BM / 64] + (int64_t)from * 4, soff[i],
+                                     lds0 + T::STAGE * T::STAGES + (s >> 2 & 1) * T::SCALE_PLACE + g * 1024);
                 }
             }
         }
