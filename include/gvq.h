@@ -316,8 +316,12 @@ int gvq_mx_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t
  * Newton-Schulz orthogonalisation of `batch` matrices [rows][cols], `stride` elements apart (out: stride_out): X = g / (|g|_F + eps),
  * then `steps` times X <- a X + (b A + c A A) X, A = X X^T (of the shorter side; at most GVQ_MAX_STEPS), which drives every singular value
  * towards 1 and keeps the singular vectors.  coef: host array [steps][3] of a, b, c, or NULL for 3.4445, -4.7750, 2.0315 in every step.
- * Products of 22-bit numbers with fp32 sums, about fp32's accuracy, for |X| < 16, |b A + c A A| < 64 (entries; the
- * default polynomial keeps them below 1.3 and 7).  A zero matrix gives zero (with eps = 0: NaN); an infinity or a NaN makes its whole matrix NaN.  At most 2^30 numbers
+ * Products of 22-bit numbers with fp32 sums: about fp32's accuracy in the 2-norm of the result, whatever |g|_F and eps are.  In every step singular values
+ * have to stay below 4 and the entries of b A + c A A below 64 (the default polynomial keeps them below 1.21 and 2.9): entries of X or A from 16 on or
+ * of the polynomial from 64 on become NaN, and with them the whole matrix (from the last step's polynomial on only their rows, of a tall matrix columns).
+ * X is kept down to 2^-36 of the norm that it starts with: a row a millionth of the others' size ends up to a thousandth of itself off, where fp32
+ * products end a millionth off.  A zero matrix
+ * gives zero (with eps = 0: NaN); an infinity or a NaN makes its whole matrix NaN.  At most 2^30 numbers
  * (rows and columns rounded up to 32) and 2^20 rows or columns per matrix, 65535 matrices.  out may be g.
  */
 int64_t gvq_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols);

@@ -1,6 +1,7 @@
 // Newton-Schulz orthogonalisation and the Muon step: launchers (host side).
 #pragma once
 #include "gvq_internal.h"
+#include "gvq_muon_plan.h"
 
 struct MuonMatrix {
     int64_t batch, rows, cols;
@@ -17,6 +18,7 @@ struct MuonPlan {   // where things lie in a workspace, in bytes
     int64_t x[2], gram, poly;     // of one matrix: two planes each
     int64_t per;                  // bytes of one matrix's planes
     int64_t sums, parts_at;       // partial sums of squares; partial products
+    int64_t factors;              // of every step, GVQ_MAX_STEPS a matrix
     int64_t bytes;                // of the whole workspace
     int parts;                    // partial sums of squares of a matrix
     NsChoice gram_by, poly_by, step_by;
@@ -59,14 +61,20 @@ struct MuonPrep {
     int turn;            // more rows than columns: X is the transpose
 };
 MuonPrep gvq_muon_prep(const MuonArgs& a);
-float gvq_muon_coef(const MuonArgs& a, int step, int i);
+// The coefficients, and the steps' factors of a matrix whose norm is far above eps.
+struct MuonCoef {
+    float v[GVQ_MAX_STEPS][3];
+    NsFactors whole[GVQ_MAX_STEPS];
+    int steps;
+};
+MuonCoef gvq_muon_coef(const MuonArgs& a);
 int gvq_muon_parts(const MuonMatrix& x);
 // M <- beta M + G and the sums of squares of U, `p.parts` per matrix.
 int gvq_launch_muon_norm(const MuonArgs& a, const MuonPrep& p, double* sums, hipStream_t st);
 
 // Matrices with at most 64 rows or columns (gvq_muon_small.hip).
 struct MuonSmallPlan {
-    int64_t m, n, ldn, run, groups, per, x, grams[2], sums, bytes;
+    int64_t m, n, ldn, run, groups, per, x, grams[2], sums, factors, bytes;
     int parts;
     bool one;            // in one work-group, without a workspace
 };

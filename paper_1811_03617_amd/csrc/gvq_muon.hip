@@ -5,7 +5,8 @@
 //
 // Precision.  The steps multiply small singular values by a = 3.4 each, 485 in all, and what rounding adds to X along such a
 // direction grows with them: numbers kept in bf16 end 1 to 7 % off (2-norm, planted low rank the worst), in f16 0.1 to 0.9 %.
-// So X, A and the polynomial are kept as two f16 terms, 22 bits, in fixed units of 2^-12 (X, A) and 2^-10 (the polynomial), and
+// So X, A and the polynomial are kept as two f16 terms, 22 bits, in units chosen by the matrix's norm and the coefficients
+// (gvq_muon_plan.h; an ordinary matrix: 2^-12 for X and A, 2^-10 for the polynomial), and
 // every product is hi hi + hi lo + lo hi in fp32 sums: as exact as fp32 products (1.0 to 1.15 times their error), at a third of
 // the f16 matrix pipe's rate, which is three times what the fp32 pipe reaches (153 TFLOP/s of library products).
 //
@@ -23,6 +24,7 @@ struct PrepArgs {
     int64_t per, plane;  // plane: numbers
     int64_t ld;
     int tx, words;       // threads side by side, as a power of two; four neighbouring numbers are aligned words
+    NsFactors* factors;  // [batch][GVQ_MAX_STEPS]
 };
 
 // Four neighbouring numbers of a row a thread, 1 << tx threads side by side and rows under each other; `at(r, c)` for every such
@@ -70,20 +72,22 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_norm_kernel(PrepArgs a)
     if (threadIdx.x == 0) a.sums[blockIdx.y * a.p.parts + blockIdx.x] = s;
 }
 
-template <typename G>
-__device__ __forceinline__ double scale_to_x(const PrepArgs& a, int matrix, double* lds)
+// The matrix's scale; `first`, one of its work-groups, leaves its factors.
+__device__ __forceinline__ double scale_of(const PrepArgs& a, const MuonCoef& coef, int matrix, bool first, double* lds)
 {
-    double s = 0;
+    double s = 0, r;
     for (int i = threadIdx.x; i < a.p.parts; i += MUON_THREADS) s += a.sums[matrix * a.p.parts + i];
-    return 1.0 / (sqrt(group_sum<MUON_THREADS>(s, lds)) + a.p.eps) * UNIT_X;
+    const double inv = scale_to_x(group_sum<MUON_THREADS>(s, lds), a.p.eps, r);
+    if (first) leave_factors(coef, r, a.factors + matrix * GVQ_MAX_STEPS);
+    return inv;
 }
 
 // U / (|U| + eps) into the two planes of X, with zeros behind the last column.
 template <typename G>
-__global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
+__global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a, MuonCoef coef)
 {
     __shared__ double lds[MUON_THREADS / 64];
-    const double inv = scale_to_x<G>(a, blockIdx.y, lds);
+    const double inv = scale_of(a, coef, blockIdx.y, blockIdx.x == 0, lds);
     const G* g = (const G*)a.p.grad + blockIdx.y * a.p.stride_grad;
     _Float16* X = (_Float16*)(a.x + blockIdx.y * a.per);
     const int cols = (int)a.p.cols;
@@ -114,11 +118,11 @@ __global__ __launch_bounds__(MUON_THREADS) void muon_planes_kernel(PrepArgs a)
 
 // The same where X is the transpose: 64 x 64 numbers a work-group, through LDS.
 template <typename G>
-__global__ __launch_bounds__(MUON_THREADS) void muon_turn_kernel(PrepArgs a)
+__global__ __launch_bounds__(MUON_THREADS) void muon_turn_kernel(PrepArgs a, MuonCoef coef)
 {
     __shared__ double lds[MUON_THREADS / 64];
     __shared__ float tile[64 * 65];
-    const double inv = scale_to_x<G>(a, blockIdx.z, lds);
+    const double inv = scale_of(a, coef, blockIdx.z, blockIdx.x == 0 && blockIdx.y == 0, lds);
     const G* g = (const G*)a.p.grad + blockIdx.z * a.p.stride_grad;
     _Float16* X = (_Float16*)(a.x + blockIdx.z * a.per);
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
@@ -154,8 +158,7 @@ struct NsArgs {
     int steps, nm, nn, band;   // steps of 32 numbers of the sum; tiles, and how they are swept
     int rows, cols;            // of the result
     int64_t per;
-    float scale;               // of the sum, in units of the result
-    float ca, cb;              // POLY: result = ca old + cb sum; STEP, LAST: ca old + sum
+    const NsFactors* f;        // this step's of the first matrix, GVQ_MAX_STEPS further for each next one (not GRAM)
     const _Float16* old;       // POLY: A, STEP and LAST: X
     _Float16* res;             // result (not LAST)
     int64_t plane, ld;         // of old and res, in numbers
@@ -202,10 +205,9 @@ __device__ __forceinline__ void last_store4<unsigned short>(unsigned short* p, b
 // not as a I to the polynomial, which would save reading X a second time: in the product it would be the largest term by far of a
 // sum that is rounded every 32 numbers (1024 x 1024 of planted low rank: 2.5e-5 off instead of 1.1e-5).
 template <int KIND, bool FLIP>
-__device__ __forceinline__ f4 ns_value4(const NsArgs& a, const _Float16* old, int r, int c, f4 v)
+__device__ __forceinline__ f4 ns_value4(const NsArgs& a, const NsFactors& f, const _Float16* old, int r, int c, f4 v)
 {
-    v *= a.scale;
-    if (KIND == NS_GRAM) return v;
+    if (KIND == NS_GRAM) return v * NS_GRAM_SCALE;
     f4 o;
     if (!FLIP) {
         const h4 hi = *(const h4*)(old + r * a.ld + c), lo = *(const h4*)(old + a.plane + r * a.ld + c);
@@ -215,7 +217,13 @@ __device__ __forceinline__ f4 ns_value4(const NsArgs& a, const _Float16* old, in
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = r + i < a.rows ? (float)old[(r + i) * a.ld + c] + (float)old[a.plane + (r + i) * a.ld + c] : 0.f;
     }
-    return a.ca * o + (KIND == NS_POLY ? a.cb * v : v);
+    return KIND == NS_POLY ? f.pa * o + f.pc * v : f.sa * o + f.ss * v;
+}
+template <int KIND>
+__device__ __forceinline__ NsFactors ns_factors_of(const NsArgs& a, int matrix)
+{
+    if (KIND == NS_GRAM) return NsFactors{};
+    return a.f[matrix * GVQ_MAX_STEPS];
 }
 
 // Upper triangle of tiles, column by column: column tn holds the tiles (0 .. tn, tn), tn (tn + 1) / 2 of them before it.
@@ -264,6 +272,7 @@ __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
         tile_at(tile_of_block(blockIdx.x, tiles), a.nm, a.nn, a.band, tm, tn);
     }
     const int64_t off = blockIdx.y * a.per;
+    const NsFactors f = SPLIT ? NsFactors{} : ns_factors_of<KIND>(a, blockIdx.y);   // (read here, they are there when the sums are)
     TileOperand A = a.a, B = a.b;
     A.p += off;
     B.p += off;
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
             for (int ni = 0; ni < T::NI; ++ni) {
                 const int r = rw + 16 * mi + (T::FLIP ? 4 * (lane >> 4) : lane & 15), c = cw + 16 * ni + (T::FLIP ? lane & 15 : 4 * (lane >> 4));
                 if (r >= a.rows || c >= a.cols) continue;
-                const f4 v = ns_value4<KIND, T::FLIP>(a, old, r, c, acc[mi][ni]) * (1.f / UNIT_X);
+                const f4 v = ns_value4<KIND, T::FLIP>(a, f, old, r, c, acc[mi][ni]) * f.out;
                 OUT* to = T::FLIP ? out + (int64_t)c * a.ld_out + r : out + (int64_t)r * a.ld_out + c;
                 last_store4<OUT>(to, a.words != 0, T::FLIP ? a.rows - r : a.cols - c, a.update, a.keep, a.rate, v);
             }
@@ -311,7 +320,7 @@ __global__ __launch_bounds__(T::THREADS) void ns_tile_kernel(NsArgs a)
             for (int ni = 0; ni < T::NI; ++ni) {
                 const int r = rw + 16 * mi + (lane & 15), c = cw + 16 * ni + 4 * (lane >> 4);
                 f4 v = {0.f, 0.f, 0.f, 0.f};
-                if (r < a.rows && c < a.ld) v = ns_value4<KIND, false>(a, old, r, c, acc[mi][ni]);
+                if (r < a.rows && c < a.ld) v = ns_value4<KIND, false>(a, f, old, r, c, acc[mi][ni]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (c + i >= a.cols) v[i] = 0.f;
@@ -374,16 +383,17 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a)
     else { tm = blockIdx.x / a.nn; tn = blockIdx.x - tm * a.nn; }
     const int64_t off = blockIdx.y * a.per;
     const int y = threadIdx.x >> 3, x = 4 * (threadIdx.x & 7), r = tm * 32 + y, c = tn * 32 + x;
+    const NsFactors f = ns_factors_of<KIND>(a, blockIdx.y);
     const float* p = a.parts + (int64_t)blockIdx.y * a.splits * a.part + r * a.ld_part + c;
     f4 v = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < a.splits; ++s) v += *(const f4*)(p + s * a.part);
     const _Float16* old = (const _Float16*)((const char*)a.old + off);
     const bool in = r < a.rows && c < a.ld;
-    if (in) v = ns_value4<KIND, false>(a, old, r, c, v);
+    if (in) v = ns_value4<KIND, false>(a, f, old, r, c, v);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (!in || c + i >= a.cols) v[i] = 0.f;
-    if (KIND == NS_LAST) v *= 1.f / UNIT_X;
+    if (KIND == NS_LAST) v *= f.out;
     if (KIND == NS_LAST && !TURN) {
         if (in && c < a.cols)
             last_store4<OUT>((OUT*)a.out + blockIdx.y * a.stride_out + (int64_t)r * a.ld_out + c, a.words != 0, a.cols - c, a.update, a.keep, a.rate, v);
@@ -487,10 +497,15 @@ MuonPrep gvq_muon_prep(const MuonArgs& m)
     return p;
 }
 
-float gvq_muon_coef(const MuonArgs& m, int step, int i)
+MuonCoef gvq_muon_coef(const MuonArgs& m)
 {
     static const double standard[3] = {3.4445, -4.7750, 2.0315};
-    return (float)(m.coef ? m.coef[3 * step + i] : standard[i]);
+    MuonCoef c{};
+    c.steps = m.steps;
+    for (int t = 0; t < m.steps; ++t)
+        for (int i = 0; i < 3; ++i) c.v[t][i] = (float)(m.coef ? m.coef[3 * t + i] : standard[i]);
+    ns_factors(c.v[0], c.steps, 1.0, c.whole);
+    return c;
 }
 
 static PrepArgs prep_args(const MuonArgs& m)
@@ -541,6 +556,7 @@ bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
     p->parts = gvq_muon_parts(x);
     at = x.batch * p->per;
     p->sums = take(x.batch * p->parts * (int64_t)sizeof(double));
+    p->factors = take(x.batch * GVQ_MAX_STEPS * (int64_t)sizeof(NsFactors));
     p->gram_by = ns_choose(x.batch, p->m, p->m, p->ldn / 32, true);
     p->poly_by = ns_choose(x.batch, p->m, p->m, p->ldm / 32, true);
     p->step_by = ns_choose(x.batch, p->m, p->n, p->ldm / 32, false);
@@ -617,18 +633,20 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
     PrepArgs q = prep_args(m);
     q.sums = (double*)(w + p.sums);
     q.x = w + p.x[0]; q.per = p.per; q.plane = p.m * p.ldn; q.ld = p.ldn;
+    q.factors = (NsFactors*)(w + p.factors);
+    const MuonCoef coef = gvq_muon_coef(m);
     int rc = gvq_launch_muon_norm(m, q.p, q.sums, st);
     if (rc != GVQ_OK) return rc;
     // (the padding of X's rows is written too)
     const dim3 threads(MUON_THREADS);
     if (wide) {
         const dim3 grid((unsigned)(p.parts), (unsigned)batch);
-        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), grid, threads, 0, st, q);
-        else hipLaunchKernelGGL((muon_planes_kernel<float>), grid, threads, 0, st, q);
+        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_planes_kernel<unsigned short>), grid, threads, 0, st, q, coef);
+        else hipLaunchKernelGGL((muon_planes_kernel<float>), grid, threads, 0, st, q, coef);
     } else {
         const dim3 grid((unsigned)((m.x.cols + 63) / 64), (unsigned)((p.ldn + 63) / 64), (unsigned)batch);
-        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_turn_kernel<unsigned short>), grid, threads, 0, st, q);
-        else hipLaunchKernelGGL((muon_turn_kernel<float>), grid, threads, 0, st, q);
+        if (m.grad_dtype == GVQ_BF16) hipLaunchKernelGGL((muon_turn_kernel<unsigned short>), grid, threads, 0, st, q, coef);
+        else hipLaunchKernelGGL((muon_turn_kernel<float>), grid, threads, 0, st, q, coef);
     }
     GVQ_HIP(hipGetLastError());
     const int mm = (int)p.m, nn = (int)p.n;
@@ -636,16 +654,15 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
     const TileOperand gram{w + p.gram, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
     const TileOperand poly{w + p.poly, mm * p.ldm * 2, p.ldm * 2, mm, nullptr, 0};
     for (int s = 0; s < m.steps; ++s) {
-        const float a = gvq_muon_coef(m, s, 0), b = gvq_muon_coef(m, s, 1), c = gvq_muon_coef(m, s, 2);
         const TileOperand X{w + p.x[s & 1], mm * p.ldn * 2, p.ldn * 2, mm, nullptr, 0};
         NsArgs n{};
         n.per = p.per;
         n.parts = (float*)(w + p.parts_at);
+        n.f = q.factors + s;
         // A = X X^T
         n.a = n.b = X;
         n.steps = (int)(p.ldn / 32);
         n.rows = n.cols = mm;
-        n.scale = 1.f / UNIT_X;   // (x UNIT_X)(x UNIT_X) -> A UNIT_X
         n.res = (_Float16*)(w + p.gram);
         n.plane = mm * p.ldm;
         n.ld = p.ldm;
@@ -654,9 +671,6 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
         // b A + c A A
         n.a = n.b = gram;
         n.steps = (int)(p.ldm / 32);
-        n.scale = UNIT_P / (UNIT_X * UNIT_X);
-        n.ca = b * (UNIT_P / UNIT_X);
-        n.cb = c;
         n.old = (const _Float16*)(w + p.gram);
         n.res = (_Float16*)(w + p.poly);
         rc = launch_ns<NS_POLY, float, false>(n, p.poly_by, batch, st);
@@ -667,8 +681,6 @@ int gvq_launch_muon(const MuonArgs& m, hipStream_t st)
         n.b.rows = nn;
         n.b.depth = mm;
         n.cols = nn;
-        n.scale = 1.f / UNIT_P;
-        n.ca = a;
         n.old = (const _Float16*)(w + p.x[s & 1]);
         n.plane = mm * p.ldn;
         n.ld = p.ldn;

@@ -3,9 +3,8 @@
 #include "gvq_muon.h"
 #include "gvq_tile.h"
 
-// Fixed units of the f16 terms: X and its Gram matrix, the polynomial.
-#define UNIT_X 4096.f
-#define UNIT_P 1024.f
+// A from sums of products of X (both in their units, see gvq_muon_plan.h).
+#define NS_GRAM_SCALE (1.f / (1 << NS_X_BITS))
 
 __device__ __forceinline__ void split_f16(float v, _Float16& hi, _Float16& lo)
 {
@@ -26,6 +25,23 @@ __device__ __forceinline__ double group_sum(double v, double* lds)
     for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
     __syncthreads();
     return s;
+}
+
+// From the sum of U's squares: what U is multiplied with to become X in its units.  r: |X|.
+__device__ __forceinline__ double scale_to_x(double squares, double eps, double& r)
+{
+    const double norm = sqrt(squares), inv = 1.0 / (norm + eps);
+    r = norm * inv;
+    return ldexp(inv, NS_X_BITS + (ns_is_whole(r) ? 0 : ns_unit_x(r)));
+}
+// The factors of a matrix's steps, by a whole work-group; `to` may be read behind a barrier (or by the next launch).
+__device__ __forceinline__ void leave_factors(const MuonCoef& coef, double r, NsFactors* to)
+{
+    if (ns_is_whole(r)) {
+        if (threadIdx.x < coef.steps) to[threadIdx.x] = coef.whole[threadIdx.x];
+    } else if (threadIdx.x == 0) {
+        ns_factors(coef.v[0], coef.steps, r, to);
+    }
 }
 
 __device__ __forceinline__ float number_at(const float* g, int64_t i) { return g[i]; }

@@ -1,0 +1,96 @@
+// The units in which the Newton-Schulz steps keep their numbers.  Plain C++: nothing here needs HIP.
+#pragma once
+#include <cmath>
+
+#if defined(__HIPCC__)
+#define NS_BOTH __host__ __device__ inline
+#else
+#define NS_BOTH inline
+#endif
+
+// X, A = X X^T and the polynomial P = b A + c A A are kept as two f16 terms per number, 22 bits down to a smallest step and up to 65504:
+// X in units of 2^-(12 + k), A in 2^-(12 + 2 k), P in 2^-(10 + j).  With k = j = 0, the ordinary case, that is |X| and |A| below 16, which singular values
+// below 4 keep, and |P| below 64; what goes beyond becomes NaN.  Small numbers would lose their last bits (of |U| = 1e-11 beside eps = 1e-7
+// 3e-5, of 1e-13 all but three digits), so k and j follow the numbers' bounds downwards: singular values are at most the
+// Frobenius norm r = |U| / (|U| + eps) at the start and the largest |a s + b s^3 + c s^5| over [0, S] behind a step from at most S; A's entries are
+// at most S^2, P's the largest |b x + c x^2| over [0, S^2].  Never upwards: a bound that is far above the numbers themselves, as behind coefficients that
+// would let X grow, would cost the bits that it is to save.
+#define NS_X_BITS 12
+#define NS_P_BITS 10
+
+// The largest |a s + b s^3 + c s^5| for s from 0 to S: at S or where the derivative a + 3 b x + 5 c x^2, x = s^2, is 0.
+NS_BOTH double ns_step_bound(double a, double b, double c, double S)
+{
+    auto at = [=](double x) { return std::fabs(std::sqrt(x) * (a + x * (b + x * c))); };
+    const double top = S * S;
+    double most = at(top);
+    auto look = [&](double x) {
+        if (x > 0.0 && x < top) {
+            const double v = at(x);
+            most = v > most ? v : most;
+        }
+    };
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    if (d >= 0.0) {
+        const double q = -0.5 * (3.0 * b + (b < 0.0 ? -std::sqrt(d) : std::sqrt(d)));
+        if (c != 0.0) look(q / (5.0 * c));
+        if (q != 0.0) look(a / q);
+    }
+    return most;
+}
+// The largest |b x + c x^2| for x from 0 to S^2.
+NS_BOTH double ns_poly_bound(double b, double c, double S)
+{
+    const double top = S * S;
+    double most = std::fabs(top * (b + top * c));
+    if (c != 0.0) {
+        const double x = -b / (2.0 * c);
+        if (x > 0.0 && x < top && std::fabs(0.5 * b * x) > most) most = std::fabs(0.5 * b * x);
+    }
+    return most;
+}
+
+// k for a bound S: 0 above 1/2, otherwise S 2^k is in [1/2, 1).
+NS_BOTH int ns_unit_x(double S)
+{
+    if (!(S > 0.0 && S <= 0.5)) return 0;
+    int e;
+    std::frexp(S, &e);
+    return -e;
+}
+// j for a bound B: 0 from 1/16 on and for B = 0, otherwise B 2^j is in [1, 2).
+NS_BOTH int ns_unit_p(double B)
+{
+    if (!(B > 0.0 && B < 0.0625)) return 0;
+    int e;
+    std::frexp(B, &e);
+    return 1 - e;
+}
+
+// What a step's kernels multiply with: P = pa A + pc (A A), X' = sa X + ss (P X), all in their units; out X' is the result.
+struct NsFactors {
+    float pa, pc, sa, ss, out;
+};
+
+// Norms above this share of |U| + eps are taken for all of it: the usual case, for which the factors are known beforehand.
+#define NS_WHOLE 0.5
+
+NS_BOTH bool ns_is_whole(double r) { return !(r > 0.0 && r <= NS_WHOLE); }   // (NaN: whatever the factors are, X is NaN; 0: X is 0)
+
+// Factors of all steps from singular values of at most S.  coef: [steps][3].
+NS_BOTH void ns_factors(const float* coef, int steps, double S, NsFactors* f)
+{
+    int k = ns_unit_x(S);
+    for (int t = 0; t < steps; ++t) {
+        const double a = coef[3 * t], b = coef[3 * t + 1], c = coef[3 * t + 2];
+        const int j = ns_unit_p(ns_poly_bound(b, c, S));
+        S = ns_step_bound(a, b, c, S);
+        const int next = t + 1 < steps ? ns_unit_x(S) : k;
+        f[t].pa = (float)std::ldexp(b, NS_P_BITS + j - NS_X_BITS - 2 * k);
+        f[t].pc = (float)std::ldexp(c, NS_P_BITS + j - 2 * NS_X_BITS - 4 * k);
+        f[t].sa = (float)std::ldexp(a, next - k);
+        f[t].ss = (float)std::ldexp(1.0, next - k - NS_P_BITS - j);
+        f[t].out = (float)std::ldexp(1.0, -NS_X_BITS - next);
+        k = next;
+    }
+}

@@ -21,7 +21,7 @@ struct MuonSmallArgs {
     int m, n;
     int steps;
     const double* sums;            // of squares, [matrix][parts]: slabs only
-    float abc[3];                  // slabs: this step's polynomial
+    NsFactors* factors;            // slabs: this step's of the first matrix (FIRST: all of them), GVQ_MAX_STEPS further for each next one
     _Float16* x;                   // slabs: planes of the first matrix, `per` bytes further for each next one
     int64_t per, plane, ldn;
     float *from, *to;              // slabs: partial Gram matrices, [matrix][group][64][64]
@@ -30,9 +30,6 @@ struct MuonSmallArgs {
     int64_t ld_out, stride_out;
     int update;
     float keep, rate;
-};
-struct MuonCoef {
-    float v[GVQ_MAX_STEPS][3];
 };
 
 // Two planes in LDS, `plane` numbers apart, rows of ld.
@@ -103,8 +100,8 @@ __device__ __forceinline__ void gram_add(const Slab& X, int cols, int m, Sum3 (&
     }
 }
 
-// P = b A + c A A from the planes of A (units of 1 / UNIT_X; P in 1 / UNIT_P).
-__device__ __forceinline__ void poly(const Slab& A, const Slab& P, int m, float b, float c)
+// P = b A + c A A from the planes of A.
+__device__ __forceinline__ void poly(const Slab& A, const Slab& P, int m, const NsFactors& f)
 {
     const int lane = threadIdx.x & 63;
     Sum3 acc[2];
@@ -114,7 +111,7 @@ __device__ __forceinline__ void poly(const Slab& A, const Slab& P, int m, float 
     for (int t = 0; t < 2; ++t) {
         if (r + 32 * t >= m || q >= m) continue;
         const int row = r + 32 * t + (lane & 15), col = q + 4 * (lane >> 4);
-        put4(P, row, col, b * (UNIT_P / UNIT_X) * get4(A, row, col) + c * (UNIT_P / (UNIT_X * UNIT_X)) * acc[t].value());
+        put4(P, row, col, f.pa * get4(A, row, col) + f.pc * acc[t].value());
     }
 }
 
@@ -133,7 +130,7 @@ struct PolyFrags {
 
 // a X + P X for the column tiles wave, wave + 8, .. of a slab of `cols` columns: TILES of them at most, four row tiles each.
 template <int TILES>
-__device__ __forceinline__ void step(const Slab& X, const PolyFrags& P, int cols, int m, float a, f4 (&v)[TILES][4])
+__device__ __forceinline__ void step(const Slab& X, const PolyFrags& P, int cols, int m, const NsFactors& f, f4 (&v)[TILES][4])
 {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
 #pragma unroll
@@ -151,7 +148,7 @@ __device__ __forceinline__ void step(const Slab& X, const PolyFrags& P, int cols
                 if (16 * r < m && 32 * k < m) acc[r].add(P.hi[k][r], P.lo[k][r], bh[k], bl[k]);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (16 * r < m) v[t][r] = a * get4(X, 16 * r + (lane & 15), c + 4 * (lane >> 4)) + acc[r].value() * (1.f / UNIT_P);
+            if (16 * r < m) v[t][r] = f.sa * get4(X, 16 * r + (lane & 15), c + 4 * (lane >> 4)) + f.ss * acc[r].value();
     }
 }
 
@@ -210,6 +207,7 @@ __global__ __launch_bounds__(MS_THREADS) void muon_one_kernel(MuonSmallArgs a, M
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ double red[MS_THREADS / 64];
+    __shared__ NsFactors factors[GVQ_MAX_STEPS];
     const int cols = (a.n + 31) & ~31, ld = cols + 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Slab X = {(_Float16*)lds, MS_M * ld, ld};
     const Slab A = {(_Float16*)lds + 2 * MS_M * ld, MS_M * MS_LDM, MS_LDM}, P = {A.hi + 2 * MS_M * MS_LDM, MS_M * MS_LDM, MS_LDM};
@@ -228,7 +226,9 @@ __global__ __launch_bounds__(MS_THREADS) void muon_one_kernel(MuonSmallArgs a, M
                     s += (double)u * u;
                     F[a.p.turn ? c * ld + r : r * ld + c] = u;
                 });
-    const double inv = 1.0 / (sqrt(group_sum<MS_THREADS>(s, red)) + a.p.eps) * UNIT_X;   // (its barriers are behind all of F)
+    double norm;
+    const double inv = scale_to_x(group_sum<MS_THREADS>(s, red), a.p.eps, norm);   // (its barriers are behind all of F)
+    leave_factors(coef, norm, factors);
     // wave w has the rows w, w + 8, ..
     constexpr int ACROSS = WIDTH / 64;
     float v[MS_M / 8][ACROSS];
@@ -260,16 +260,17 @@ __global__ __launch_bounds__(MS_THREADS) void muon_one_kernel(MuonSmallArgs a, M
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = 16 * (wave >> 2) + 32 * i, c = 16 * (wave & 3);
-            if (r < m && c < m) put4(A, r + (lane & 15), c + 4 * (lane >> 4), acc[i].value() * (1.f / UNIT_X));
+            if (r < m && c < m) put4(A, r + (lane & 15), c + 4 * (lane >> 4), acc[i].value() * NS_GRAM_SCALE);
         }
+        const NsFactors f = factors[t];
         __syncthreads();
-        poly(A, P, m, coef.v[t][1], coef.v[t][2]);
+        poly(A, P, m, f);
         __syncthreads();
         constexpr int TILES = (WIDTH + 127) / 128;
         f4 x[TILES][4];
         PolyFrags frags;
         frags.load(P, m);
-        step<TILES>(X, frags, cols, m, coef.v[t][0], x);
+        step<TILES>(X, frags, cols, m, f, x);
         __syncthreads();
         const bool last = t + 1 == a.steps;
 #pragma unroll
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(MS_THREADS) void muon_one_kernel(MuonSmallArgs a, M
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * r + (lane & 15);
                 if (16 * r >= m) continue;
-                if (last) *(f4*)(F + row * ld + c) = x[i][r] * (1.f / UNIT_X);
+                if (last) *(f4*)(F + row * ld + c) = x[i][r] * f.out;
                 else put4(X, row, c, x[i][r]);
             }
         }
@@ -309,10 +310,12 @@ __device__ __forceinline__ void slab_words(const MuonSmallArgs& a, int cols, L l
     }
 }
 
+struct MuonNone {};
+
 // FIRST: U / (|U| + eps) into the planes and its part of A.  Otherwise a step, the result if LAST.
 // LDS: the planes of a slab of MS_SLAB columns (fp32 numbers of the same rows on the way out), those of A and P.
 template <typename G, typename OUT, bool FIRST, bool LAST>
-__global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
+__global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a, typename std::conditional<FIRST, MuonCoef, MuonNone>::type coef)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ double red[MS_THREADS / 64];
@@ -326,10 +329,14 @@ __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
     OUT* out = (OUT*)a.out + blockIdx.y * a.stride_out;
     _Float16* gx = (_Float16*)((char*)a.x + blockIdx.y * a.per);
     double inv = 0;
-    if (FIRST) {
-        double s = 0;
+    NsFactors* fs = a.factors + blockIdx.y * GVQ_MAX_STEPS;
+    NsFactors f{};
+    if (!FIRST) f = *fs;
+    if constexpr (FIRST) {
+        double s = 0, norm;
         for (int i = threadIdx.x; i < a.p.parts; i += MS_THREADS) s += a.sums[blockIdx.y * a.p.parts + i];
-        inv = 1.0 / (sqrt(group_sum<MS_THREADS>(s, red)) + a.p.eps) * UNIT_X;
+        inv = scale_to_x(group_sum<MS_THREADS>(s, red), a.p.eps, norm);
+        if (blockIdx.x == 0) leave_factors(coef, norm, fs);
     } else {
         const float* p = a.from + (int64_t)blockIdx.y * groups * MS_M * MS_M;
         f4 v[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
@@ -340,10 +347,10 @@ __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = 4 * (threadIdx.x + i * MS_THREADS);
-            put4(A, e / MS_M, e % MS_M, v[i] * (1.f / UNIT_X));
+            put4(A, e / MS_M, e % MS_M, v[i] * NS_GRAM_SCALE);
         }
         __syncthreads();
-        poly(A, P, m, a.abc[1], a.abc[2]);
+        poly(A, P, m, f);
     }
     Sum3 acc[2];
     PolyFrags frags;
@@ -379,7 +386,7 @@ __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
         __syncthreads();
         if (!FIRST) {
             f4 x[TILES][4];
-            step<TILES>(X, frags, cols, m, a.abc[0], x);
+            step<TILES>(X, frags, cols, m, f, x);
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < TILES; ++i) {
@@ -389,7 +396,7 @@ __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a)
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * r + (lane & 15);
                     if (16 * r >= m) continue;
-                    if (LAST) *(f4*)(F + row * LD + c) = x[i][r] * (1.f / UNIT_X);
+                    if (LAST) *(f4*)(F + row * LD + c) = x[i][r] * f.out;
                     else put4(X, row, c, x[i][r]);
                 }
             }
@@ -444,6 +451,7 @@ int64_t gvq_muon_small_plan(const MuonMatrix& x, MuonSmallPlan* p)
     for (int i = 0; i < 2; ++i) p->grams[i] = take(x.batch * p->groups * MS_M * MS_M * 4);
     p->parts = gvq_muon_parts(x);
     p->sums = take(x.batch * p->parts * (int64_t)sizeof(double));
+    p->factors = take(x.batch * GVQ_MAX_STEPS * (int64_t)sizeof(NsFactors));
     return p->bytes = at;
 }
 
@@ -472,12 +480,13 @@ static int launch_one(const MuonSmallArgs& a, const MuonCoef& coef, int64_t batc
 }
 
 template <typename G, typename OUT, bool FIRST, bool LAST>
-static int launch_slab(const MuonSmallArgs& a, int64_t groups, int64_t batch, hipStream_t st)
+static int launch_slab(const MuonSmallArgs& a, const typename std::conditional<FIRST, MuonCoef, MuonNone>::type& coef, int64_t groups, int64_t batch,
+                       hipStream_t st)
 {
     static gvq_once_per_device once;
     const int rc = raise_lds(once, muon_slab_kernel<G, OUT, FIRST, LAST>, lds_of(MS_SLAB));
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((muon_slab_kernel<G, OUT, FIRST, LAST>), dim3((unsigned)groups, (unsigned)batch), dim3(MS_THREADS), lds_of(MS_SLAB), st, a);
+    hipLaunchKernelGGL((muon_slab_kernel<G, OUT, FIRST, LAST>), dim3((unsigned)groups, (unsigned)batch), dim3(MS_THREADS), lds_of(MS_SLAB), st, a, coef);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
@@ -499,13 +508,14 @@ static int launch_small(const MuonArgs& m, MuonSmallArgs a, const MuonSmallPlan&
     a.run = (int)p.run;
     a.slab = (int)padded((p.run + (p.run + MS_SLAB - 1) / MS_SLAB - 1) / ((p.run + MS_SLAB - 1) / MS_SLAB));
     a.to = (float*)(w + p.grams[0]);
-    if (rc == GVQ_OK) rc = launch_slab<G, float, true, false>(a, p.groups, m.x.batch, st);
+    a.factors = (NsFactors*)(w + p.factors);
+    if (rc == GVQ_OK) rc = launch_slab<G, float, true, false>(a, coef, p.groups, m.x.batch, st);
     for (int t = 0; t < m.steps && rc == GVQ_OK; ++t) {
-        for (int i = 0; i < 3; ++i) a.abc[i] = coef.v[t][i];
+        a.factors = (NsFactors*)(w + p.factors) + t;
         a.from = (float*)(w + p.grams[t & 1]);
         a.to = (float*)(w + p.grams[(t + 1) & 1]);
-        rc = t + 1 < m.steps ? launch_slab<float, float, false, false>(a, p.groups, m.x.batch, st)
-                             : launch_slab<float, OUT, false, true>(a, p.groups, m.x.batch, st);
+        rc = t + 1 < m.steps ? launch_slab<float, float, false, false>(a, {}, p.groups, m.x.batch, st)
+                             : launch_slab<float, OUT, false, true>(a, {}, p.groups, m.x.batch, st);
     }
     return rc;
 }
@@ -522,9 +532,7 @@ int gvq_launch_muon_small(const MuonArgs& m, hipStream_t st)
     a.steps = m.steps;
     a.out = m.out; a.ld_out = m.ld_out; a.stride_out = m.stride_out;
     a.update = m.update; a.keep = m.keep; a.rate = m.rate;
-    MuonCoef coef{};
-    for (int t = 0; t < m.steps; ++t)
-        for (int i = 0; i < 3; ++i) coef.v[t][i] = gvq_muon_coef(m, t, i);
+    const MuonCoef coef = gvq_muon_coef(m);
     if (m.grad_dtype == GVQ_BF16)
         return m.out_dtype == GVQ_BF16 ? launch_small<unsigned short, unsigned short>(m, a, p, coef, st) : launch_small<unsigned short, float>(m, a, p, coef, st);
     return m.out_dtype == GVQ_BF16 ? launch_small<float, unsigned short>(m, a, p, coef, st) : launch_small<float, float>(m, a, p, coef, st);
