@@ -7,11 +7,6 @@ struct MuonMatrix {
     int64_t batch, rows, cols;
 };
 
-// Which tiles a product takes, and in how many parts its sum is cut.
-struct NsChoice {
-    int shape = 0, splits = 1;
-};
-
 struct MuonPlan {   // where things lie in a workspace, in bytes
     int64_t m, n;                 // shorter and longer side: X is kept as m rows of n numbers
     int64_t ldn, ldm;             // padded row lengths in numbers

@@ -428,56 +428,6 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a)
     }
 }
 
-static int64_t padded(int64_t n) { return (n + 31) / 32 * 32; }
-
-// Tile shapes: 256, 128 and 64 on both sides, and 192 for products whose operands both run along the sum.  The times are fitted to 43
-// products (64 to 4096 rows, 64 to 16384 columns) each measured with every shape and up to 8 parts: what they pick is the fastest or
-// at most 4 % (of the iteration) behind it.
-struct NsShape {
-    int size;
-    double step_us, start_us;   // of one work-group on a compute unit: a step, and what a tile costs beside its steps
-    int per_cu;                 // work-groups that share a compute unit (step_us is that of the pair)
-};
-static const NsShape ns_shapes[4] = {{256, 1.7, 9.0, 1}, {192, 1.08, 4.5, 1}, {128, 0.62, 3.3, 1}, {64, 0.48, 2.9, 2}};
-
-// Rounds of tiles over 256 compute units, with the sum cut in up to 8 parts where there are few tiles.  The parts go by one
-// matrix alone: the tiles' shape does not change a result's bits, the parts do, and a matrix has the same result in every batch.
-static double ns_time(const NsShape& s, int64_t batch, int64_t rows, int64_t cols, int64_t steps, int splits, bool sym)
-{
-    const int64_t nm = (rows + s.size - 1) / s.size, nn = (cols + s.size - 1) / s.size;
-    const int64_t tiles = batch * (sym ? nm * (nm + 1) / 2 : nm * nn) * splits;
-    const int64_t rounds = (tiles + 256 * s.per_cu - 1) / (256 * s.per_cu);
-    const double join = splits > 1 ? 10.0 + 0.56e-6 * batch * rows * cols * (splits + 1) * (sym ? 0.5 : 1.0) : 0.0;
-    return rounds * (s.start_us + s.step_us * ((steps + splits - 1) / splits)) + join;
-}
-
-static NsChoice ns_choose(int64_t batch, int64_t rows, int64_t cols, int64_t steps, bool sym)
-{
-    NsChoice best;
-    double least = 1e300;
-    for (int splits = 1; splits <= 8 && (splits == 1 || splits * 2 <= steps); ++splits)
-        for (int k = 0; k < 4; ++k) {
-            if (k == 1 && !sym) continue;
-            const double t = ns_time(ns_shapes[k], 1, rows, cols, steps, splits, sym);
-            if (t < least) { least = t; best.shape = k; best.splits = splits; }
-        }
-    if (batch > 1) {
-        least = 1e300;
-        for (int k = 0; k < 4; ++k) {
-            if (k == 1 && !sym) continue;
-            const double t = ns_time(ns_shapes[k], batch, rows, cols, steps, best.splits, sym);
-            if (t < least) { least = t; best.shape = k; }
-        }
-    }
-    return best;
-}
-
-static int64_t part_numbers(const NsChoice& c, int64_t rows, int64_t cols)
-{
-    const int64_t s = ns_shapes[c.shape].size;
-    return c.splits == 1 ? 0 : c.splits * ((rows + s - 1) / s * s) * ((cols + s - 1) / s * s);
-}
-
 int gvq_muon_parts(const MuonMatrix& x)
 {
     const int64_t n = x.rows * x.cols, parts = (n + 16 * MUON_THREADS - 1) / (16 * MUON_THREADS);
@@ -537,8 +487,8 @@ bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
     if (x.batch < 0 || x.rows < 0 || x.cols < 0 || x.batch > 65535 || x.rows > (1 << 20) || x.cols > (1 << 20)) return false;
     p->m = x.rows < x.cols ? x.rows : x.cols;
     p->n = x.rows < x.cols ? x.cols : x.rows;
-    p->ldn = padded(p->n);
-    p->ldm = padded(p->m);
+    p->ldn = ns_padded(p->n);
+    p->ldm = ns_padded(p->m);
     p->bytes = 0;
     // a plane stays at 2 GiB, so that both planes of a tile's rows are within 32 bits of each other
     if (p->m * p->ldn > (int64_t)1 << 30) return false;
@@ -557,11 +507,10 @@ bool gvq_muon_plan(const MuonMatrix& x, MuonPlan* p)
     at = x.batch * p->per;
     p->sums = take(x.batch * p->parts * (int64_t)sizeof(double));
     p->factors = take(x.batch * GVQ_MAX_STEPS * (int64_t)sizeof(NsFactors));
-    p->gram_by = ns_choose(x.batch, p->m, p->m, p->ldn / 32, true);
-    p->poly_by = ns_choose(x.batch, p->m, p->m, p->ldm / 32, true);
-    p->step_by = ns_choose(x.batch, p->m, p->n, p->ldm / 32, false);
-    int64_t most = part_numbers(p->gram_by, p->m, p->m);
-    const int64_t b = part_numbers(p->poly_by, p->m, p->m), c = part_numbers(p->step_by, p->m, p->n);
+    const NsWays ways = ns_ways(x.batch, p->m, p->n);
+    p->gram_by = ways.gram; p->poly_by = ways.poly; p->step_by = ways.step;
+    int64_t most = ns_part_numbers(p->gram_by, p->m, p->m);
+    const int64_t b = ns_part_numbers(p->poly_by, p->m, p->m), c = ns_part_numbers(p->step_by, p->m, p->n);
     most = most > b ? most : b;
     most = most > c ? most : c;
     p->parts_at = take(x.batch * most * (int64_t)sizeof(float));
@@ -587,13 +536,10 @@ static int launch_tiles(const NsArgs& a, int64_t batch, hipStream_t st)
     return GVQ_OK;
 }
 
+// The parts of a sum, and their join.
 template <typename T, int KIND, typename OUT, bool TURN>
-static int launch_shape(NsArgs a, int64_t batch, hipStream_t st)
+static int launch_parts(NsArgs a, int64_t batch, hipStream_t st)
 {
-    a.nm = (a.rows + T::BM - 1) / T::BM;
-    a.nn = (a.cols + T::BN - 1) / T::BN;
-    a.band = 4;
-    if (a.splits == 1) return launch_tiles<T, KIND, OUT, false>(a, batch, st);
     a.ld_part = (int64_t)a.nn * T::BN;
     a.part = a.ld_part * a.nm * T::BM;
     // (the parts of LAST lie as those of STEP: what a transpose needs is the join's to do)
@@ -606,6 +552,17 @@ static int launch_shape(NsArgs a, int64_t batch, hipStream_t st)
     hipLaunchKernelGGL((ns_join_kernel<KIND, OUT, TURN>), dim3((unsigned)tiles, (unsigned)batch), dim3(256), 0, st, a);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
+}
+
+template <typename T, int KIND, typename OUT, bool TURN>
+static int launch_shape(NsArgs a, int64_t batch, hipStream_t st)
+{
+    a.nm = (a.rows + T::BM - 1) / T::BM;
+    a.nn = (a.cols + T::BN - 1) / T::BN;
+    a.band = 4;
+    if (a.splits == 1) return launch_tiles<T, KIND, OUT, false>(a, batch, st);
+    if constexpr (ns_in_parts(T::BM, KIND == NS_GRAM)) return launch_parts<T, KIND, OUT, TURN>(a, batch, st);
+    return GVQ_EINVAL;
 }
 
 template <int KIND, typename OUT, bool TURN>

@@ -1,6 +1,7 @@
-// The units in which the Newton-Schulz steps keep their numbers.  Plain C++: nothing here needs HIP.
+// The units in which the Newton-Schulz steps keep their numbers, and the tiles that their products take.  Plain C++: nothing here needs HIP.
 #pragma once
 #include <cmath>
+#include <cstdint>
 
 #if defined(__HIPCC__)
 #define NS_BOTH __host__ __device__ inline
@@ -93,4 +94,73 @@ NS_BOTH void ns_factors(const float* coef, int steps, double S, NsFactors* f)
         f[t].out = (float)std::ldexp(1.0, -NS_X_BITS - next);
         k = next;
     }
+}
+
+// ---- tiles ------------------------------------------------------------------------------------------------------------
+
+inline int64_t ns_padded(int64_t n) { return (n + 31) / 32 * 32; }
+
+// Which tiles a product takes, and in how many parts its sum is cut.
+struct NsChoice {
+    int shape = 0, splits = 1;
+};
+
+// Tile shapes: 256, 128 and 64 on both sides, and 192 for products whose operands both run along the sum.  The times are fitted to 43
+// products (64 to 4096 rows, 64 to 16384 columns) each measured with every shape and up to 8 parts: what they pick is the fastest or
+// at most 4 % (of the iteration) behind it.
+struct NsShape {
+    int size;
+    double step_us, start_us;   // of one work-group on a compute unit: a step, and what a tile costs beside its steps
+    int per_cu;                 // work-groups that share a compute unit (step_us is that of the pair)
+};
+static const NsShape ns_shapes[4] = {{256, 1.7, 9.0, 1}, {192, 1.08, 4.5, 1}, {128, 0.62, 3.3, 1}, {64, 0.48, 2.9, 2}};
+
+// Whether tiles of a size come in parts: 64 x 64 for the Gram matrix of long rows alone (no size has them the fastest way elsewhere).
+constexpr bool ns_in_parts(int size, bool gram) { return gram || size > 64; }
+
+// Rounds of tiles over 256 compute units, with the sum cut in up to 8 parts where there are few tiles.  The parts go by one
+// matrix alone: the tiles' shape does not change a result's bits, the parts do, and a matrix has the same result in every batch.
+inline double ns_time(const NsShape& s, int64_t batch, int64_t rows, int64_t cols, int64_t steps, int splits, bool sym)
+{
+    const int64_t nm = (rows + s.size - 1) / s.size, nn = (cols + s.size - 1) / s.size;
+    const int64_t tiles = batch * (sym ? nm * (nm + 1) / 2 : nm * nn) * splits;
+    const int64_t rounds = (tiles + 256 * s.per_cu - 1) / (256 * s.per_cu);
+    const double join = splits > 1 ? 10.0 + 0.56e-6 * batch * rows * cols * (splits + 1) * (sym ? 0.5 : 1.0) : 0.0;
+    return rounds * (s.start_us + s.step_us * ((steps + splits - 1) / splits)) + join;
+}
+
+// sym: a symmetric product; gram: X X^T.
+inline NsChoice ns_choose(int64_t batch, int64_t rows, int64_t cols, int64_t steps, bool sym, bool gram)
+{
+    NsChoice best;
+    double least = 1e300;
+    auto look = [&](int64_t of, int k, int splits) {
+        if ((k == 1 && !sym) || (splits > 1 && !ns_in_parts(ns_shapes[k].size, gram))) return;
+        const double t = ns_time(ns_shapes[k], of, rows, cols, steps, splits, sym);
+        if (t < least) { least = t; best.shape = k; best.splits = splits; }
+    };
+    for (int splits = 1; splits <= 8 && (splits == 1 || splits * 2 <= steps); ++splits)
+        for (int k = 0; k < 4; ++k) look(1, k, splits);
+    if (batch > 1) {
+        const int splits = best.splits;
+        least = 1e300;
+        for (int k = 0; k < 4; ++k) look(batch, k, splits);
+    }
+    return best;
+}
+
+// The three products of a step for X of m rows and n columns, m <= n.
+struct NsWays {
+    NsChoice gram, poly, step;
+};
+inline NsWays ns_ways(int64_t batch, int64_t m, int64_t n)
+{
+    return {ns_choose(batch, m, m, ns_padded(n) / 32, true, true), ns_choose(batch, m, m, ns_padded(m) / 32, true, false),
+            ns_choose(batch, m, n, ns_padded(m) / 32, false, false)};
+}
+
+inline int64_t ns_part_numbers(const NsChoice& c, int64_t rows, int64_t cols)
+{
+    const int64_t s = ns_shapes[c.shape].size;
+    return c.splits == 1 ? 0 : c.splits * ((rows + s - 1) / s * s) * ((cols + s - 1) / s * s);
 }

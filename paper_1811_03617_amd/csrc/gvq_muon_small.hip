@@ -423,14 +423,12 @@ __global__ __launch_bounds__(MS_THREADS) void muon_slab_kernel(MuonSmallArgs a, 
 
 // ---- launchers ------------------------------------------------------------------------------------------------------------
 
-static int64_t padded(int64_t n) { return (n + 31) / 32 * 32; }
-
 bool gvq_muon_small_takes(const MuonMatrix& x) { return (x.rows < x.cols ? x.rows : x.cols) <= MS_M; }
 
 // Columns of a work-group.
 static int64_t small_run(int64_t n)
 {
-    const int64_t run = padded((n + MS_GROUPS - 1) / MS_GROUPS);
+    const int64_t run = ns_padded((n + MS_GROUPS - 1) / MS_GROUPS);
     return run < 128 ? 128 : run;
 }
 
@@ -443,7 +441,7 @@ int64_t gvq_muon_small_plan(const MuonMatrix& x, MuonSmallPlan* p)
     if (p->one) return p->bytes;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
-    p->ldn = padded(p->n);
+    p->ldn = ns_padded(p->n);
     p->run = small_run(p->n);
     p->groups = (p->n + p->run - 1) / p->run;
     p->per = p->m * p->ldn * 4;
@@ -474,7 +472,7 @@ static int launch_one(const MuonSmallArgs& a, const MuonCoef& coef, int64_t batc
     static gvq_once_per_device once;
     const int rc = raise_lds(once, muon_one_kernel<G, OUT, WIDTH>, lds_of(WIDTH));
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((muon_one_kernel<G, OUT, WIDTH>), dim3((unsigned)batch), dim3(MS_THREADS), lds_of((int)padded(a.n)), st, a, coef);
+    hipLaunchKernelGGL((muon_one_kernel<G, OUT, WIDTH>), dim3((unsigned)batch), dim3(MS_THREADS), lds_of((int)ns_padded(a.n)), st, a, coef);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
@@ -506,7 +504,7 @@ static int launch_small(const MuonArgs& m, MuonSmallArgs a, const MuonSmallPlan&
     a.plane = p.m * p.ldn;
     a.ldn = p.ldn;
     a.run = (int)p.run;
-    a.slab = (int)padded((p.run + (p.run + MS_SLAB - 1) / MS_SLAB - 1) / ((p.run + MS_SLAB - 1) / MS_SLAB));
+    a.slab = (int)ns_padded((p.run + (p.run + MS_SLAB - 1) / MS_SLAB - 1) / ((p.run + MS_SLAB - 1) / MS_SLAB));
     a.to = (float*)(w + p.grams[0]);
     a.factors = (NsFactors*)(w + p.factors);
     if (rc == GVQ_OK) rc = launch_slab<G, float, true, false>(a, coef, p.groups, m.x.batch, st);

@@ -23,7 +23,7 @@ def _run(tmp_path, body):
 RANDOM = r"""
 static unsigned seed = 1;
 static double rnd() { return seed = seed * 1664525u + 1013904223u, (seed >> 8) / 16777216.0; }
-static double coefficient() { return rnd() < 0.2 ? 0.0 : (rnd() - 0.5) * std::exp(6.0 * rnd()); }
+[[maybe_unused]] static double coefficient() { return rnd() < 0.2 ? 0.0 : (rnd() - 0.5) * std::exp(6.0 * rnd()); }
 """
 
 
@@ -107,3 +107,30 @@ int main()
     return ns_unit_x(NAN) || ns_unit_x(INFINITY) || ns_unit_x(0.0) || ns_unit_p(NAN) || ns_unit_p(INFINITY) ? 3 : 0;
 }
 """)
+
+
+def test_the_sizes_that_are_run_take_every_way(tmp_path):
+    """Each size of _muon_ways.py is computed as it says there, and together they reach everything that the rule can pick: over many sizes it picks
+    nothing else."""
+    from _muon_ways import PICKED, WAYS
+    out = _run(tmp_path, "#include <initializer_list>\nstatic const int sizes[][3] = {" + ", ".join("{%d, %d, %d}" % k for k in WAYS) + "};\n" + RANDOM + r"""
+static void tell(int64_t b, int64_t m, int64_t n)
+{
+    const NsWays w = ns_ways(b, m, n);
+    for (const NsChoice& c : {w.gram, w.poly, w.step}) printf("%d %d ", ns_shapes[c.shape].size, c.splits > 1);
+    printf("\n");
+}
+int main()
+{
+    for (auto& s : sizes) tell(s[0], s[1], s[2]);
+    for (int i = 0; i < 20000; ++i) {
+        const int64_t m = 65 + (int64_t)std::exp(8.5 * rnd()), n = m + (int64_t)std::exp(10.5 * rnd()), b = rnd() < 0.5 ? 1 : 1 + (int64_t)std::exp(4.0 * rnd());
+        tell(b, m, n);
+    }
+}
+""")
+    ways = [tuple((int(v[i]), v[i + 1] == "1") for i in (0, 2, 4)) for v in (line.split() for line in out.splitlines())]
+    assert dict(zip(WAYS, ways)) == WAYS
+    for kind in range(3):
+        assert {w[kind] for w in WAYS.values()} == PICKED[kind]
+        assert {w[kind] for w in ways} <= PICKED[kind]
