@@ -3,6 +3,7 @@
 // 273, into fp32 313 (411 MB of results, 80 us alone).  A round of 256 x 256 tiles costs 8 us beside its steps, most of it
 // results that all compute units write at one time.
 #include "gvq_mx.h"
+#include "gvq_mx_plan.h"
 #include "gvq_tile.h"
 
 struct MxProductArgs {
@@ -104,84 +105,35 @@ static int launch_tile(MxProductArgs a, hipStream_t st)
     return GVQ_OK;
 }
 
-// Tile shapes and their times, fitted to 20 products (64 to 8192 rows, 1000 to 25088 columns, sums of 500 to 25088) each measured with
-// every shape: what a round of tiles over 256 compute units costs beside its steps, a step, and the work-groups that share a unit.
-struct MxShape {
-    int bm, bn;
-    double start_us, step_us;
-    int per_cu;
-};
-static const MxShape mx_shapes[4] = {{256, 256, 8.0, 0.95, 1}, {256, 128, 2.5, 0.67, 1}, {128, 128, 1.0, 0.39, 1}, {64, 64, 2.0, 0.255, 2}};
-
-// The time of the fastest shape, and which it is.
-static double tile_time(int64_t m, int64_t n, int64_t steps, int& best)
-{
-    double least = 1e300;
-    for (int k = 0; k < 4; ++k) {
-        const MxShape& s = mx_shapes[k];
-        const int64_t tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
-        const double t = (double)((tiles + 256 * s.per_cu - 1) / (256 * s.per_cu)) * (s.start_us + s.step_us * steps);
-        if (t < least) { least = t; best = k; }
-    }
-    return least;
-}
-
-// The kernels without LDS (gvq_mx_few.hip), `tiles` times 16 rows of A and 16 of B a work-group: rounds over 256 compute units again.  Fitted to
-// 120 products of 17 to 500 rows, 512 to 4096 columns and sums of 256 to 25088, where the better of the two is up to four times faster than any tile
-// (77 x 1000 x 4096 5.9 us and 11.5, 48 x 512 x 25088 14.4 and 56) and up to four times slower where work-groups are many.
-static double few_time(int64_t m, int64_t n, int64_t steps, int tiles)
-{
-    const int64_t groups = ((m + 16 * tiles - 1) / (16 * tiles)) * ((n + 15) / 16);
-    return 1.5 + (double)((groups + 255) / 256) * (tiles == 1 ? 0.45 + 0.06 * steps : 0.3 + 0.096 * steps);
-}
-
 template <typename OUT>
-static int launch_product(const MxProductArgs& a, hipStream_t st)
+static int launch_product(const MxProductArgs& a, int shape, hipStream_t st)
 {
-    if (a.steps < 4) return launch_tile<TileShape<64, 64, 2, 2, 1, 4, false, false, true>, OUT>(a, st);
-    int best = 3;
-    tile_time(a.a.rows, a.b.rows, a.steps, best);
-    switch (best) {
+    switch (shape) {
     case 0: return launch_tile<TileShape<256, 256, 2, 4, 1, 4>, OUT>(a, st);
     case 1: return launch_tile<TileShape<256, 128, 4, 2, 1, 4>, OUT>(a, st);
     case 2: return launch_tile<TileShape<128, 128, 2, 4, 1, 4>, OUT>(a, st);
-    default: return launch_tile<TileShape<64, 64, 2, 2, 1, 4>, OUT>(a, st);
+    case 3: return launch_tile<TileShape<64, 64, 2, 2, 1, 4>, OUT>(a, st);
+    default: return launch_tile<TileShape<64, 64, 2, 2, 1, 4, false, false, true>, OUT>(a, st);
     }
 }
 
-// few: times 16 rows of A a work-group without LDS, 0: tiles.
-struct MxWay {
-    int few;
-    double us;
-};
-static MxWay way_of(int64_t m, int64_t n, int64_t k)
-{
-    const int64_t steps = gvq_mx_row_bytes(k) / TILE_STEP;
-    int shape;
-    const double tile = tile_time(m, n, steps, shape), one = few_time(m, n, steps, 1), two = few_time(m, n, steps, 2);
-    if (one <= two && one < tile) return {1, one};
-    return two < tile ? MxWay{2, two} : MxWay{0, tile};
-}
-
-double gvq_mx_product_time(int64_t m, int64_t n, int64_t k) { return way_of(m, n, k).us; }
+double gvq_mx_product_time(int64_t m, int64_t n, int64_t k) { return mx_way(m, n, gvq_mx_row_bytes(k) / TILE_STEP).us; }
 
 int gvq_launch_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, int64_t m, int64_t n,
                          int64_t k, void* out, gvq_dtype_t dtype, int64_t ld, bool accumulate, hipStream_t st)
 {
-    if (k > 0) {
-        const MxWay way = way_of(m, n, k);
-        if (way.few)
-            return gvq_launch_mx_few(way.few, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, accumulate, st);
-    }
+    const int64_t row = gvq_mx_row_bytes(k), es = dtype == GVQ_BF16 ? 2 : 4, steps = row / TILE_STEP;
+    const MxWay way = steps > 0 ? mx_way(m, n, steps) : mx_tiles(m, n, steps);
+    if (way.few)
+        return gvq_launch_mx_few(way.few, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, accumulate, st);
     MxProductArgs a;
-    const int64_t row = gvq_mx_row_bytes(k), es = dtype == GVQ_BF16 ? 2 : 4;
     a.a = TileOperand{(const char*)a_codes, 0, row, (int)m, (const char*)a_scales, 0};
     a.b = TileOperand{(const char*)b_codes, 0, row, (int)n, (const char*)b_scales, 0};
-    a.steps = (int)(row / TILE_STEP);
+    a.steps = (int)steps;
     a.out = out;
     a.ld = ld;
     a.accumulate = accumulate;
     a.words = (((uintptr_t)out | (uintptr_t)(ld * es)) & 15) == 0;
     a.nm = a.nn = a.band = 0;
-    return dtype == GVQ_BF16 ? launch_product<unsigned short>(a, st) : launch_product<float>(a, st);
+    return dtype == GVQ_BF16 ? launch_product<unsigned short>(a, way.shape, st) : launch_product<float>(a, way.shape, st);
 }
