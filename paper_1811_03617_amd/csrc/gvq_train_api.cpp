@@ -102,15 +102,16 @@ int gvq_mx_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t
                            gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate,
                            void* workspace, void* stream)
 {
-    if (!is_dtype(dtype) || !is_dtype(dx_dtype) || !is_dtype(dw_dtype) || !in_range(rows) || !in_range(n_in) || !in_range(n_out))
+    if (!is_dtype(dtype) || (dx && !is_dtype(dx_dtype)) || (dw && !is_dtype(dw_dtype)) || !in_range(rows) || !in_range(n_in) || !in_range(n_out))
         return GVQ_EINVAL;
     if (ld_dy < n_out || (noise && noise_ld < n_out) || (dx && ld_dx < n_in) || (dw && (ld_x < n_in || ld_dw < n_in))) return GVQ_EINVAL;
     if (n_in == 0 || (rows == 0 && n_out == 0)) return GVQ_OK;
     if (!dx && !dw) return GVQ_EINVAL;
     const bool some = rows > 0 && n_out > 0;
     if (some && (!dy || !workspace || (dx && (!wt_codes || !wt_scales)) || (dw && !x))) return GVQ_EINVAL;
-    if (!aligned(dy, size_of(dtype)) || !aligned(x, size_of(dtype)) || !aligned(dx, size_of(dx_dtype)) || !aligned(dw, size_of(dw_dtype)) ||
-        !aligned(wt_codes, 16) || !aligned(wt_scales, 16) || !aligned(workspace, 16))
+    if (!aligned(dy, size_of(dtype)) || !aligned(workspace, 16) ||
+        (dx && (!aligned(dx, size_of(dx_dtype)) || !aligned(wt_codes, 16) || !aligned(wt_scales, 16))) ||
+        (dw && (!aligned(dw, size_of(dw_dtype)) || !aligned(x, size_of(dtype)))))
         return GVQ_EALIGN;
     char* at = (char*)workspace;
     auto take = [&](int64_t bytes) { char* was = at; at += up256(bytes); return was; };

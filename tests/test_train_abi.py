@@ -94,3 +94,16 @@ def test_muon_refusals():
         args = list(ok2)
         args[k] = v
         assert g(*args) == gvq.EALIGN, k
+
+
+def test_a_gradient_that_is_not_wanted_asks_for_nothing():
+    """What only dw needs (x, its type) is not looked at without dw, and what only dx needs (the weight) not without dx.  Sizes without elements: nothing runs."""
+    f = L.gvq_mx_linear_backward
+    odd, none = A + 1, 7          # an address of no type, a type that there is not
+    assert f(A, 8, odd, 0, gvq.F32, 0, 64, 8, None, 0, A, A, A, gvq.F32, 64, None, none, 0, 0, A, None) == gvq.OK
+    assert f(A, 0, A, 64, gvq.F32, 8, 64, 0, None, 0, odd, odd, None, none, 0, A, gvq.F32, 64, 0, A, None) == gvq.OK
+    # and with them as before
+    assert f(A, 8, odd, 64, gvq.F32, 0, 64, 8, None, 0, A, A, A, gvq.F32, 64, A, gvq.F32, 64, 0, A, None) == gvq.EALIGN
+    assert f(A, 0, A, 64, gvq.F32, 8, 64, 0, None, 0, odd, A, A, gvq.F32, 64, A, gvq.F32, 64, 0, A, None) == gvq.EALIGN
+    assert f(A, 8, A, 64, gvq.F32, 0, 64, 8, None, 0, A, A, A, gvq.F32, 64, A, none, 64, 0, A, None) == gvq.EINVAL
+    assert f(A, 8, A, 64, gvq.F32, 0, 64, 8, None, 0, A, A, A, none, 64, None, gvq.F32, 64, 0, A, None) == gvq.EINVAL
