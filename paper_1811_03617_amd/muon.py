@@ -2,13 +2,14 @@
 
     muon.step(weight, grad, buffer, lr=0.02)     # in place
 
-Everything runs on the device's current stream; the workspace of a call comes from PyTorch's allocator on that stream.
+Everything runs on the device's current stream; the workspace of a call comes from PyTorch's allocator on that stream.  No gradient is
+recorded: `orthogonalize` refuses a tensor that needs one, `step` is an optimiser's and takes weights that do.
 """
 import numpy as np
 import torch
 
 from . import gvq
-from .mx import _check, _dtype, _matrix, _now, _workspace
+from .mx import _check, _dtype, _matrix, _no_graph, _now, _workspace
 
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
@@ -26,6 +27,7 @@ def _coef(coefficients, steps):
 def orthogonalize(g, steps=5, coefficients=None, eps=1e-7, dtype=None):
     """g ([rows, cols] or [batch, rows, cols]) with its singular values driven towards 1.  coefficients: (a, b, c) of every step
     instead of `steps` times the default."""
+    _no_graph(g, "g")
     if g.dim() not in (2, 3):
         raise ValueError(f"g: two or three dimensions are needed, not {g.dim()}")
     batch, rows, cols = g.shape if g.dim() == 3 else (1, *g.shape)

@@ -5,7 +5,8 @@
     dx, dw = mx.linear_backward(dy, x, qt, noise=noise)
 
 Tensors are two-dimensional, float32 or bfloat16, with neighbouring elements of a row next to each other; everything runs on the
-device's current stream, and what a call allocates comes from PyTorch's allocator on that stream.
+device's current stream, and what a call allocates comes from PyTorch's allocator on that stream.  No call records a gradient: one whose
+result would need it is refused (wrap linear and linear_backward in a torch.autograd.Function, where gradients are off).
 """
 import functools
 from typing import NamedTuple
@@ -48,6 +49,11 @@ def _matrix(t, name):
     if (cols > 1 and s1 != 1) or (rows > 1 and s0 < cols):
         raise ValueError(f"{name}: neighbouring elements of a row have to be next to each other, and rows must not overlap")
     return code, (s0 if rows > 1 else cols), rows, cols
+
+
+def _no_graph(t, name):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: needs a gradient, which this call does not record (detach it, or switch gradients off)")
 
 
 def _noise(t, rows, cols):
@@ -153,6 +159,7 @@ def matmul(a, b, dtype=torch.float32, out=None, accumulate=False):
 
 def linear(x, w, dtype=None):
     """Q(x) W^T for a weight of n_out rows and n_in columns; the result's dtype is x's unless given."""
+    _no_graph(x, "x")
     code, ld, rows, n_in = _matrix(x, "x")
     n_out = w.rows
     codes, scales = _stored(w, "w", n_out, n_in)
