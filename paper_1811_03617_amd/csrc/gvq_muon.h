@@ -33,7 +33,7 @@ struct MuonArgs {
     const double* coef;              // host [steps][3], null: the default
     int steps;
     double eps;
-    void* out;                       // decay == null ? the result : the weight
+    void* out;                       // the result, or the weight that it updates
     gvq_dtype_t out_dtype;
     int64_t ld_out, stride_out;
     int update;                      // 0: out = X, 1: out = keep * out - rate * X
@@ -71,7 +71,7 @@ int gvq_launch_muon_norm(const MuonArgs& a, const MuonPrep& p, double* sums, hip
 struct MuonSmallPlan {
     int64_t m, n, ldn, run, groups, per, x, grams[2], sums, factors, bytes;
     int parts;
-    bool one;            // in one work-group, without a workspace
+    bool one;            // in one work-group, which does not look at its workspace (256 bytes all the same)
 };
 bool gvq_muon_small_takes(const MuonMatrix& x);
 int64_t gvq_muon_small_plan(const MuonMatrix& x, MuonSmallPlan* p);   // bytes of the workspace

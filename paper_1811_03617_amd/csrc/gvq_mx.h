@@ -33,13 +33,6 @@ bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, 
 int gvq_launch_mx_few_numbers(const void* x, gvq_dtype_t x_dtype, int64_t ld_x, const void* w_codes, const void* w_scales, int64_t rows,
                               int64_t n, int64_t k, void* out, gvq_dtype_t dtype, int64_t ld_out, hipStream_t st);
 
-// Neighbouring tiles for the work-groups of one XCD, to which they go round robin (8 of them).
-__device__ __forceinline__ int mx_tile_of(int block, int tiles)
-{
-    const int per = tiles >> 3, more = tiles & 7, x = block & 7;
-    return x * per + (x < more ? x : more) + (block >> 3);
-}
-
 // Eight numbers from p, of which `left` are in the matrix (the others are 0); `words`: p is 16-byte aligned.
 __device__ __forceinline__ void mx_load8(const float* p, bool words, int64_t left, float (&v)[8])
 {

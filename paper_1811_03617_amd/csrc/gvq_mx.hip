@@ -9,6 +9,7 @@
 // directions' blocks come out of the same pass, the columns' ones through LDS.  Rows of 8192 x 4096 bf16 numbers 16.6 us (5.1 TB/s),
 // columns of 4096 x 25088 59 (4.4), both ways of 8191 x 4093 fp32 numbers with random bytes 83 (2.5), back into fp32 27 (5.6).
 #include "gvq_mx.h"
+#include "gvq_tile.h"
 
 #define MXQ_THREADS 256
 
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(MXQ_THREADS) void mx_both_kernel(MxQuantArgs a)
 {
     __shared__ __attribute__((aligned(16))) float tile[128 * 64];
     __shared__ __attribute__((aligned(16))) unsigned char dust[NOISE ? 128 * 64 : 16];
-    const int t = mx_tile_of(blockIdx.x, gridDim.x);
+    const int t = tile_of_block(blockIdx.x, gridDim.x);
     const int64_t r0 = (int64_t)(t / a.across) * 128, c0 = (int64_t)(t % a.across) * 64;
     const bool whole = r0 + 128 <= a.rows && c0 + 64 <= a.cols;
     if (whole && a.words) {
