@@ -7,12 +7,12 @@
 // direction grows with them: numbers kept in bf16 end 1 to 7 % off (2-norm, planted low rank the worst), in f16 0.1 to 0.9 %.
 // So X, A and the polynomial are kept as two f16 terms, 22 bits, in units chosen by the matrix's norm and the coefficients
 // (gvq_muon_plan.h; an ordinary matrix: 2^-12 for X and A, 2^-10 for the polynomial), and
-// every product is hi hi + hi lo + lo hi in fp32 sums: as exact as fp32 products (1.0 to 1.15 times their error), at a third of
+// every product is hi hi + hi lo + lo hi in fp32 sums: as exact as fp32 products (0.6 to 1.4 times their error), at a third of
 // the f16 matrix pipe's rate, which is three times what the fp32 pipe reaches (153 TFLOP/s of library products).
 //
 // A step is three products: A (half of it, mirrored), b A + c A A (half of it), and a X + P X.  Bound: the matrix pipe's power where
-// matrices are large (4096 x 4096 in fp32 193 + 198 + 331 us a step), launches, half-filled rounds of tiles and the bytes of X where they
-// are not (5 of 512 x 4608 36 + 6 + 11 + 67, 1000 x 4096 20 + 5 + 15 + 36).
+// matrices are large (4096 x 4096 in fp32 196 + 200 + 338 us a step), launches, half-filled rounds of tiles and the bytes of X where they
+// are not (5 of 512 x 4608 36 + 6 + 11 + 67, 1000 x 4096 21 + 5 + 16 + 38).
 #include "gvq_muon_device.h"
 
 #define MUON_THREADS 256

@@ -5,8 +5,8 @@
 // ones are cut into up to MS_GROUPS runs of columns, a launch per step: every work-group adds up the partial Gram matrices of the
 // launch before, makes the polynomial for itself (a 64 x 64 product), takes its columns through the step and leaves its part of
 // the next Gram matrix.  Same numbers and products as in gvq_muon.hip: two f16 terms, three products, fp32 sums.
-// Bound: latency, from barrier to barrier, and at many columns the LDS, whose fragments every tile reads for itself.  64 x 27 15 us,
-// 64 x 384 61, 64 x 4096 89, 64 x 25088 215 (one launch per product: 68, 99, 129, 251).
+// Bound: latency, from barrier to barrier, and at many columns the LDS, whose fragments every tile reads for itself, on the 32 compute units that
+// have columns.  64 x 27 16 us, 64 x 384 59, 64 x 4096 87, 64 x 25088 208 (one launch per product: 68, 99, 129, 251).
 #include "gvq_muon_device.h"
 
 #define MS_THREADS 512

@@ -2,13 +2,15 @@
 // to move it.
 //
 // A work-group has 16 rows of W, its 16 waves take the sum in turns of 512 numbers (256 bytes of every row), and each lane reads
-// its operands straight into registers: row lane % 16, 16 bytes of codes a step, and four steps' scales in one word.  The loads run
-// a turn ahead of the products, with no branch around any of them (or every load would be waited for), and go through the caches: an
+// its operands straight into registers: row lane % 16, 16 bytes of codes a step, and four steps' scales in one word.  A turn's loads are
+// asked for before the products of the turn before, with no branch around any of them (or every load would be waited for); where that
+// would take more registers than two work-groups of a unit have (64 a lane), the compiler moves them back to their own turn and a wave waits for them
+// there: all but the fp32 kernel of one to four rows (127 registers) are built so, and rely on the unit's other waves.  Loads go through the caches: an
 // instruction takes half a line of each of 16 rows, the next one the other half (with loads past the caches 16 x 512 x 25088 17.8 us, so
-// 14.2).  Up to four rows of x are quantised on the way: the 32 numbers that a lane needs are one block, so the lane finds its scale and
+// 13.6).  Up to four rows of x are quantised on the way: the 32 numbers that a lane needs are one block, so the lane finds its scale and
 // packs its codes alone, without LDS and without a launch of its own.  More rows come in codes, 16 or 32 to a work-group.
-// Bound: a compute unit's loads, 33 bytes a ns of codes each, and a turn's latency at the beginning and the end.
-// 77 x 1000 x 4096 6 us, 1 x 4096 x 25088 (54.6 MB) 13.3.
+// Bound: a compute unit's loads, 33 bytes a ns of codes each, and a turn's latency at the beginning and the end, in the products of codes also between.
+// 77 x 1000 x 4096 6 us, 1 x 4096 x 25088 (54.6 MB) 10.9.
 #include "gvq_mx.h"
 #include "gvq_tile.h"
 
@@ -127,7 +129,7 @@ __device__ __forceinline__ void few_out(const MxFewArgs& a, int r0, int n0, int 
 // At most four rows of numbers.  A wave packs the blocks of four steps at once, lane 16 b + 4 k + r that of row r, step k and block b
 // (alone they would fill a quarter of the lanes or less), and turns the lanes by 4 k for step k's product, where only the first
 // four of sixteen matter.  One row of 25088 numbers in bf16 to 4096: with the blocks of each step packed on their own 22 us, so
-// 13, of which W's bytes would take 10 to 11 alone.
+// 11, which is what W's bytes take alone.
 // Lane i of 16 gets what lane (i + N) % 16 has.
 template <int N>
 __device__ __forceinline__ unsigned int turn_lanes(unsigned int v)
@@ -294,8 +296,9 @@ int gvq_launch_mx_few(int tiles, const void* x_codes, const void* x_scales, cons
 }
 
 // Numbers are packed by every work-group again, which costs little with one row of bf16 and most with four of fp32: rounds as for codes
-// (gvq_mx_product.hip), fitted to 20 layers of 1 and 4 rows.  The other way is a launch that packs them once, 4 us, and the
-// product of codes (4 rows of 4096 fp32 numbers to 25088 here 47 us, there 24; one row of 25088 bf16 numbers to 4096 here 13.3, there 16.5).
+// (gvq_mx_plan.h), fitted to 20 layers of 1 and 4 rows.  The other way is a launch that packs them once, 4 us, and the
+// product of codes (4 rows of 4096 fp32 numbers to 25088 here 47 us, there 17; one row of 25088 bf16 numbers to 4096 here 11.2, there 13.6).  Of 32 layers measured
+// both ways 28 take the faster one or lose less than 6 %; the others lose up to a quarter (4 fp32 rows of 4096 to 4096 8.1 us for 6.5).
 bool gvq_mx_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k)
 {
     const bool bf16 = x_dtype == GVQ_BF16;

@@ -1,6 +1,6 @@
 // Products of 4-bit microscaled matrices, C = A B^T, on the scaled 4-bit matrix pipe (v_mfma_scale_f32_16x16x128_f8f6f4: exact
-// products of codes, scaled per block of 32, fp32 sums).  8192 x 4096 x 4096 into bf16 88 us (3.1 PFLOP/s), 4096 x 25088 x 4096 into bf16
-// 273, into fp32 313 (411 MB of results, 80 us alone).  A round of 256 x 256 tiles costs 8 us beside its steps, most of it
+// products of codes, scaled per block of 32, fp32 sums).  8192 x 4096 x 4096 into bf16 80 to 88 us (3.1 to 3.4 PFLOP/s), 4096 x 25088 x 4096 into bf16
+// 259 to 275, into fp32 308 to 315 (411 MB of results, 80 us alone), by the box.  A round of 256 x 256 tiles costs 8 us beside its steps, most of it
 // results that all compute units write at one time.
 #include "gvq_mx.h"
 #include "gvq_mx_plan.h"

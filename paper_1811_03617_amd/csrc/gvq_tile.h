@@ -9,8 +9,8 @@
 // What bounds it.  4 bits, 256 x 256: LDS, of which a step's 1024 cycles of products need 96 KB of fragments, 33 KB of copies in and
 // 24 reads of scales a wave; 8192 x 8192 x 8192 3.7 PFLOP/s of the 8.0 that the pipe does alone.  f16, three products: power, the
 // clock falls to 1.9 GHz with the pipe two thirds busy; a step of 4096 x 4096 x 4096 1.25 to 1.3 PFLOP/s where the library's f16 product of
-// 8192 x 8192 x 8192 does 1.24.  256 x 256 is the largest tile whose sums leave registers for fragments (128 of 256), eight waves of
-// 128 x 64 because four of 128 x 128 have their sums copied back and forth (four times slower).
+// 8192 x 8192 x 8192 does 1.24.  256 x 256 is the largest tile whose sums leave registers for fragments (128 of 256; the f16 kernels that hand
+// planes out keep 24 to 26 more in scratch), eight waves of 128 x 64 because four of 128 x 128 have their sums copied back and forth (four times slower).
 #pragma once
 #include "gvq_device.h"
 
