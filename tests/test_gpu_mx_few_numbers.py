@@ -77,3 +77,25 @@ def test_fp32_numbers_around_every_tie(mx, n):
         b[:, 15] = 7 * s      # each block's scale is s
         rows.append(b)
     _through_a_layer(mx, np.concatenate(rows), torch.float32, n)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4])
+@pytest.mark.parametrize("n", [512, 100])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_nan_stays_in_its_row_and_column(mx, rows, n, dtype):
+    """An infinity or a NaN makes its block NaN, and with it its row of the result, of the weight its column; the others are as without it."""
+    g = torch.Generator().manual_seed(n)
+    x, w = torch.randn(rows, n, generator=g).to(dtype).to(DEV), torch.randn(70, n, generator=g).to(DEV)
+    clean = mx.linear(x, mx.quantize(w), torch.float32)
+    assert bool(torch.isfinite(clean).all())
+    for value in (float("nan"), float("inf"), float("-inf")):
+        for at in (0, n - 1):
+            bad_x, bad_w = x.clone(), w.clone()
+            bad_x[rows - 1, at] = value
+            bad_w[11, at] = value
+            got = mx.linear(bad_x, mx.quantize(bad_w), torch.float32)
+            want = clean.clone()
+            want[rows - 1] = float("nan")
+            want[:, 11] = float("nan")
+            assert torch.equal(torch.isnan(got), torch.isnan(want))
+            assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
