@@ -339,6 +339,86 @@ int gvq_muon_step(void* weight, gvq_dtype_t weight_dtype, int64_t ld_weight, con
                   int nesterov, double scale, const double* coef, int steps, double eps, void* workspace, void* stream);
 
 /*
+ * ---- 8-bit layers, the gated block made of them, and the loss that fits a network to a teacher ----
+ *
+ * Conventions of the 4-bit layers above: no handle, the caller owns every buffer and workspace, sizes up to GVQ_MX_MAX, and up to GVQ_I8_MAX_SUM
+ * along the axis that a product sums (its whole numbers fit 32 bits).
+ */
+#define GVQ_I8_MAX_SUM 131072   /* longest sum of 8-bit products (2^17) */
+#define GVQ_MAX_TOP 1024        /* most entries of a teacher's list */
+typedef enum { GVQ_SILU = 0, GVQ_GELU = 1 } gvq_activation_t;   /* g / (1 + e^-g); g Phi(g), Phi the normal distribution */
+
+/*
+ * Matrices in 8-bit integers.  A row's numbers share one scale: m its largest magnitude (at least 2^-100), each is kept as the nearest
+ * integer to x fl(127/m), halves to the even one, and stands for that integer times fl(m/127) (fl: one rounding to fp32).  A row that
+ * holds an infinity or a NaN is NaN throughout (codes 0, scale NaN).
+ *   codes  : [rows][128 ceil(cols/128)] bytes, -127 to 127, 0 behind the last column; 16-byte aligned;
+ *   scales : float [rows]; 16-byte aligned.
+ * x [rows][cols] -> its rows (codes, scales) and / or its columns (codes_t, scales_t: the matrix of x's transpose, a scale for each column);
+ * either pair may be NULL, and without the second one so may the workspace (gvq_i8_quantize_workspace bytes).
+ */
+int64_t gvq_i8_code_bytes(int64_t rows, int64_t cols);
+int64_t gvq_i8_quantize_workspace(int64_t rows, int64_t cols);
+int gvq_i8_quantize(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld, void* codes, float* scales, void* codes_t,
+                    float* scales_t, void* workspace, void* stream);
+
+/* The values that codes and scales stand for, rounded to out_dtype. */
+int gvq_i8_dequantize(const void* codes, const float* scales, int64_t rows, int64_t cols, void* out, gvq_dtype_t out_dtype, int64_t ld,
+                      void* stream);
+
+/*
+ * out [m][n] = A B^T (accumulate != 0: out + A B^T), A [m][k] and B [n][k] with a scale for each row.  The integers' sum is exact; it is
+ * rounded to fp32, multiplied by the product of both scales, and rounded to out_dtype.
+ */
+int gvq_i8_matmul(const void* a_codes, const float* a_scales, const void* b_codes, const float* b_scales, int64_t m, int64_t n, int64_t k,
+                  void* out, gvq_dtype_t out_dtype, int64_t ld, int accumulate, void* stream);
+
+/*
+ * A layer with an 8-bit weight: y [rows][n_out] = Q(x) W^T, a scale for each row of x (token) and of W (channel).  Any number of rows,
+ * from one token on.  Its gradients: dx [rows][n_in] = Q(dy) Q(W^T)^T, wt_codes and wt_scales W's transpose ([n_in][n_out], the second pair of
+ * gvq_i8_quantize); dw [n_out][n_in] = Q(dy^T) Q(x^T)^T (accumulate != 0: added to dw).  dx or dw may be NULL; what only it
+ * needs is then not looked at.
+ */
+int64_t gvq_i8_linear_workspace(int64_t rows, int64_t n_in);
+int gvq_i8_linear(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales,
+                  int64_t n_out, void* y, gvq_dtype_t y_dtype, int64_t ld_y, void* workspace, void* stream);
+int64_t gvq_i8_linear_backward_workspace(int64_t rows, int64_t n_in, int64_t n_out);
+int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
+                           int64_t n_out, const void* wt_codes, const float* wt_scales, void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw,
+                           gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate, void* workspace, void* stream);
+
+/*
+ * A gated block's first half: h [rows][n] = act(g) u, [g | u] = Q(x) W^T, W [2 n][n_in] with the gate's rows first.  Workspace:
+ * gvq_i8_linear_workspace(rows, n_in).  gvq_i8_gated_gradient: from dh the gradient of the sums, dg [rows][2 n] = [dh u act'(g) | dh act(g)] in x's type, g
+ * and u computed anew (the same workspace).  gvq_i8_gated_backward: that, and then the gradients of a layer of 2 n outputs whose dy it is, as
+ * gvq_i8_linear_backward gives them: dx, and dw [2 n][n_in]; wt is the transpose of all of W ([n_in][2 n]).
+ */
+int gvq_i8_gated(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales, int64_t n,
+                 gvq_activation_t activation, void* h, gvq_dtype_t h_dtype, int64_t ld_h, void* workspace, void* stream);
+int gvq_i8_gated_gradient(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t n,
+                          const void* w_codes, const float* w_scales, gvq_activation_t activation, void* dg, int64_t ld_dg, void* workspace,
+                          void* stream);
+int64_t gvq_i8_gated_backward_workspace(int64_t rows, int64_t n_in, int64_t n);
+int gvq_i8_gated_backward(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t n,
+                          const void* w_codes, const float* w_scales, const void* wt_codes, const float* wt_scales, gvq_activation_t activation,
+                          void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate,
+                          void* workspace, void* stream);
+
+/*
+ * A student's logits z [rows][vocab] against a teacher's largest ones, a [rows][n_top] at the places index [rows][n_top] (int64).  With
+ * p = softmax(a / t) over the row's entries and q = softmax(z / t) over the whole row, t the temperature (0.001 to 1000):
+ *   loss[row] = w t^2 sum_j p_j (log p_j - log q[index_j]),   grad[row][v] = w t (q[v] - sum of p_j with index_j = v),
+ * the gradient of the sum of all losses, in z's type.  An entry whose index is outside [0, vocab) is absent (-1, say, in rows of fewer entries);
+ * entries of one index add up.  weight: w of each row, or NULL for 1.  A row of weight 0 or without entries has loss 0 and gradient 0,
+ * whatever its logits hold.  Logits of -inf have q = 0; a row that holds +inf, a NaN or nothing but -inf is NaN.  grad may be NULL, or
+ * the logits themselves (with ld_grad = ld).  n_top is at most GVQ_MAX_TOP.
+ */
+int64_t gvq_distill_workspace(int64_t rows, int64_t vocab, int64_t n_top);
+int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* top, gvq_dtype_t top_dtype,
+                const int64_t* index, int64_t n_top, int64_t ld_top, int64_t ld_index, const float* weight, double temperature, float* loss,
+                void* grad, int64_t ld_grad, void* workspace, void* stream);
+
+/*
  * Text for a status code.  For GVQ_EHIP the text includes the message of the most recent
  * failed HIP call in this process.  The pointer stays valid until the next call.
  */

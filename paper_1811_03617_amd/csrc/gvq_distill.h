@@ -1,0 +1,22 @@
+// A teacher's top logits against a student's softmax: arguments and the launcher's declaration.
+#pragma once
+#include "gvq_device.h"
+
+struct DistillArgs {
+    const void* logits;       // [rows][vocab]
+    int64_t rows, ld;
+    int vocab;
+    const void* top;          // [rows][n_top]
+    int top_bf16;
+    int64_t ld_top;
+    const int64_t* index;     // [rows][n_top]; outside [0, vocab): the entry is absent
+    int64_t ld_index;
+    int n_top;
+    const float* weight;      // [rows] or null: ones
+    float t, log2_t;          // temperature t, log2(e) / t
+    float* loss;              // [rows]
+    void* grad;               // [rows][vocab] or null
+    int64_t ld_grad;
+};
+
+int gvq_launch_distill(const DistillArgs& a, gvq_dtype_t dtype, void* workspace, hipStream_t st);

@@ -1,0 +1,51 @@
+"""The divergence of a teacher's top logits from a student's softmax, and its gradient (include/gvq.h, `gvq_distill`).
+
+    losses, dlogits = distill.loss_and_gradient(logits, top, index, temperature=2.0, weight=weight)
+
+For every row, with p = softmax(top / t) over the row's entries and q = softmax(logits / t) over all of the row:
+loss = w t^2 sum_j p_j (log p_j - log q[index_j]), gradient = w t (q - p at its places).  Everything runs on the device's current
+stream.  No call records a gradient: `loss` refuses logits that need one, `loss_and_gradient` gives it.
+"""
+import torch
+
+from . import gvq
+from .mx import _check, _matrix, _no_graph, _now, _workspace, _device
+
+
+def _run(logits, top, index, temperature, weight, grad, want):
+    code, ld, rows, vocab = _matrix(logits, "logits")
+    code_top, ld_top, rows_top, n = _matrix(top, "top")
+    if rows_top != rows or tuple(index.shape) != (rows, n) or index.dtype != torch.int64 or not index.is_cuda or index.get_device() != _device():
+        raise ValueError("top and index: a row for each of logits' rows, of one length, and int64 of the index, are needed")
+    s0, s1 = index.stride()
+    if (n > 1 and s1 != 1) or (rows > 1 and s0 < n):
+        raise ValueError("index: neighbouring elements of a row have to be next to each other, and rows must not overlap")
+    if weight is not None and (weight.dtype != torch.float32 or tuple(weight.shape) != (rows,) or not weight.is_contiguous() or not weight.is_cuda
+                               or weight.get_device() != _device()):
+        raise ValueError(f"weight: float32 of shape ({rows},), contiguous, on the current GPU is needed")
+    ld_grad = vocab
+    if want:
+        if grad is None:
+            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        code_g, ld_grad, rows_g, cols_g = _matrix(grad, "out")
+        if (rows_g, cols_g) != (rows, vocab) or code_g != code:
+            raise ValueError("out: the shape and dtype of logits are needed")
+    losses = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    ws = _workspace(logits.device, "gvq_distill_workspace", rows, vocab, n)
+    _check(gvq.lib().gvq_distill(logits.data_ptr(), code, rows, vocab, ld, top.data_ptr(), code_top, index.data_ptr(), n, ld_top,
+                                 s0 if rows > 1 else n, None if weight is None else weight.data_ptr(), temperature, losses.data_ptr(),
+                                 grad.data_ptr() if want else None, ld_grad, ws.data_ptr(), _now()), "gvq_distill")
+    return losses, grad
+
+
+def loss(logits, top, index, temperature=1.0, weight=None):
+    """Every row's loss, float32.  logits [rows, vocab], top [rows, n] the teacher's largest logits and index [rows, n] (int64) where they
+    are; an index outside the vocabulary (-1, say) is no entry.  weight: float32 [rows], or 1; a row of weight 0 is not looked at."""
+    _no_graph(logits, "logits")
+    return _run(logits, top, index, temperature, weight, None, False)[0]
+
+
+def loss_and_gradient(logits, top, index, temperature=1.0, weight=None, out=None):
+    """(every row's loss, gradient of their sum by the logits in the logits' dtype).  out: where the gradient goes, the logits themselves
+    if they are needed no more."""
+    return _run(logits, top, index, temperature, weight, out, True)

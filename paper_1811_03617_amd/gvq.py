@@ -18,6 +18,9 @@ STATIC_MAX_SLICES = 1 << 21
 MAX_D = 1024
 MX_MAX = 1 << 22
 MAX_STEPS = 64
+I8_MAX_SUM = 131072
+MAX_TOP = 1024
+SILU, GELU = 0, 1
 
 _lib = None
 
@@ -76,8 +79,20 @@ def lib():
         f64 = C.c_double
         L.gvq_orthogonalize.argtypes = [vp, i32, i64, i64, i64, i64, i64, vp, i32, f64, vp, i32, i64, i64, vp, vp]
         L.gvq_muon_step.argtypes = [vp, i32, i64, vp, i32, i64, vp, i64, i64, i64, f64, f64, f64, i32, f64, vp, i32, f64, vp, vp]
+        L.gvq_i8_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+        L.gvq_i8_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+        L.gvq_i8_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i32, i64, i32, vp]
+        L.gvq_i8_linear.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp, vp]
+        L.gvq_i8_linear_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, vp, vp, i32, i64, vp, i32, i64, i32, vp, vp]
+        L.gvq_i8_gated.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp, vp]
+        L.gvq_i8_gated_gradient.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, vp, i32, vp, i64, vp, vp]
+        L.gvq_i8_gated_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, vp, vp, vp, i32, vp, i32, i64, vp, i32, i64, i32,
+                                            vp, vp]
+        L.gvq_distill.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i64, i64, i64, vp, f64, vp, vp, i64, vp, vp]
         for name, n in (("gvq_mx_code_bytes", 2), ("gvq_mx_scale_bytes", 2), ("gvq_mx_linear_workspace", 2),
-                        ("gvq_mx_linear_backward_workspace", 3), ("gvq_orthogonalize_workspace", 3)):
+                        ("gvq_mx_linear_backward_workspace", 3), ("gvq_orthogonalize_workspace", 3), ("gvq_i8_code_bytes", 2),
+                        ("gvq_i8_quantize_workspace", 2), ("gvq_i8_linear_workspace", 2), ("gvq_i8_linear_backward_workspace", 3),
+                        ("gvq_i8_gated_backward_workspace", 3), ("gvq_distill_workspace", 3)):
             getattr(L, name).argtypes = [i64] * n
             getattr(L, name).restype = i64
         for name in ("gvq_basis_create", "gvq_basis_destroy", "gvq_fit_basis", "gvq_fit_status",
@@ -86,7 +101,8 @@ def lib():
                      "gvq_select_k", "gvq_compress_segment", "gvq_decompress_segment", "gvq_flatten_conv",
                      "gvq_unflatten_conv", "gvq_fit_basis_first_slice", "gvq_local_loss_static", "gvq_mx_quantize",
                      "gvq_mx_dequantize", "gvq_mx_matmul", "gvq_mx_linear", "gvq_mx_linear_backward", "gvq_orthogonalize",
-                     "gvq_muon_step"):
+                     "gvq_muon_step", "gvq_i8_quantize", "gvq_i8_dequantize", "gvq_i8_matmul", "gvq_i8_linear", "gvq_i8_linear_backward",
+                     "gvq_i8_gated", "gvq_i8_gated_gradient", "gvq_i8_gated_backward", "gvq_distill"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -361,3 +377,76 @@ class Basis:
         U = np.ascontiguousarray(U, dtype=np.float32).reshape(self.B, self.d, self.k)
         mu = np.ascontiguousarray(mu, dtype=np.float32).reshape(self.B, self.d)
         _check(lib().gvq_basis_import(self._h, U.ctypes.data, mu.ctypes.data), "gvq_basis_import")
+
+
+def gvq_i8_code_bytes(rows, cols):
+    return _size(lib().gvq_i8_code_bytes(rows, cols), "gvq_i8_code_bytes")
+
+
+def gvq_i8_quantize_workspace(rows, cols):
+    return _size(lib().gvq_i8_quantize_workspace(rows, cols), "gvq_i8_quantize_workspace")
+
+
+def gvq_i8_quantize(x, dtype, rows, cols, ld, codes, scales, codes_t, scales_t, workspace, stream=None):
+    _check(lib().gvq_i8_quantize(_ptr(x), dtype, rows, cols, ld, _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t), _ptr(workspace),
+                                 _stream(stream)), "gvq_i8_quantize")
+
+
+def gvq_i8_dequantize(codes, scales, rows, cols, out, out_dtype, ld, stream=None):
+    _check(lib().gvq_i8_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), out_dtype, ld, _stream(stream)), "gvq_i8_dequantize")
+
+
+def gvq_i8_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, out_dtype, ld, accumulate=False, stream=None):
+    _check(lib().gvq_i8_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, _ptr(out), out_dtype, ld, accumulate,
+                               _stream(stream)), "gvq_i8_matmul")
+
+
+def gvq_i8_linear_workspace(rows, n_in):
+    return _size(lib().gvq_i8_linear_workspace(rows, n_in), "gvq_i8_linear_workspace")
+
+
+def gvq_i8_linear(x, dtype, rows, n_in, ld_x, w_codes, w_scales, n_out, y, y_dtype, ld_y, workspace, stream=None):
+    _check(lib().gvq_i8_linear(_ptr(x), dtype, rows, n_in, ld_x, _ptr(w_codes), _ptr(w_scales), n_out, _ptr(y), y_dtype, ld_y, _ptr(workspace),
+                               _stream(stream)), "gvq_i8_linear")
+
+
+def gvq_i8_linear_backward_workspace(rows, n_in, n_out):
+    return _size(lib().gvq_i8_linear_backward_workspace(rows, n_in, n_out), "gvq_i8_linear_backward_workspace")
+
+
+def gvq_i8_linear_backward(dy, ld_dy, x, ld_x, dtype, rows, n_in, n_out, wt_codes, wt_scales, dx, dx_dtype, ld_dx, dw, dw_dtype, ld_dw,
+                           accumulate, workspace, stream=None):
+    _check(lib().gvq_i8_linear_backward(_ptr(dy), ld_dy, _ptr(x), ld_x, dtype, rows, n_in, n_out, _ptr(wt_codes), _ptr(wt_scales), _ptr(dx),
+                                        dx_dtype, ld_dx, _ptr(dw), dw_dtype, ld_dw, accumulate, _ptr(workspace), _stream(stream)),
+           "gvq_i8_linear_backward")
+
+
+def gvq_i8_gated(x, dtype, rows, n_in, ld_x, w_codes, w_scales, n, activation, h, h_dtype, ld_h, workspace, stream=None):
+    _check(lib().gvq_i8_gated(_ptr(x), dtype, rows, n_in, ld_x, _ptr(w_codes), _ptr(w_scales), n, activation, _ptr(h), h_dtype, ld_h,
+                              _ptr(workspace), _stream(stream)), "gvq_i8_gated")
+
+
+def gvq_i8_gated_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, dg, ld_dg, workspace, stream=None):
+    _check(lib().gvq_i8_gated_gradient(_ptr(dh), ld_dh, _ptr(x), ld_x, dtype, rows, n_in, n, _ptr(w_codes), _ptr(w_scales), activation, _ptr(dg),
+                                       ld_dg, _ptr(workspace), _stream(stream)), "gvq_i8_gated_gradient")
+
+
+def gvq_i8_gated_backward_workspace(rows, n_in, n):
+    return _size(lib().gvq_i8_gated_backward_workspace(rows, n_in, n), "gvq_i8_gated_backward_workspace")
+
+
+def gvq_i8_gated_backward(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, wt_codes, wt_scales, activation, dx, dx_dtype, ld_dx, dw,
+                          dw_dtype, ld_dw, accumulate, workspace, stream=None):
+    _check(lib().gvq_i8_gated_backward(_ptr(dh), ld_dh, _ptr(x), ld_x, dtype, rows, n_in, n, _ptr(w_codes), _ptr(w_scales), _ptr(wt_codes),
+                                       _ptr(wt_scales), activation, _ptr(dx), dx_dtype, ld_dx, _ptr(dw), dw_dtype, ld_dw, accumulate,
+                                       _ptr(workspace), _stream(stream)), "gvq_i8_gated_backward")
+
+
+def gvq_distill_workspace(rows, vocab, n_top):
+    return _size(lib().gvq_distill_workspace(rows, vocab, n_top), "gvq_distill_workspace")
+
+
+def gvq_distill(logits, dtype, rows, vocab, ld, top, top_dtype, index, n_top, ld_top, ld_index, weight, temperature, loss, grad, ld_grad,
+                workspace, stream=None):
+    _check(lib().gvq_distill(_ptr(logits), dtype, rows, vocab, ld, _ptr(top), top_dtype, _ptr(index), n_top, ld_top, ld_index, _ptr(weight),
+                             temperature, _ptr(loss), _ptr(grad), ld_grad, _ptr(workspace), _stream(stream)), "gvq_distill")
