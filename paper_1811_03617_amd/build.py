@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgvq.so")
 SOURCES = ["gvq_api.cpp", "gvq_codec.hip", "gvq_codec_long.hip", "gvq_codec_ws.hip", "gvq_flow.hip", "gvq_flow_c_f32.hip", "gvq_flow_c_bf16.hip", "gvq_flow_d.hip", "gvq_fit.hip", "gvq_moments.hip", "gvq_moments_int.hip", "gvq_eigen.hip", "gvq_sample.hip", "gvq_layout.hip", "gvq_monitor.hip",
            "gvq_train_api.cpp", "gvq_mx.hip", "gvq_mx_product.hip", "gvq_mx_few.hip", "gvq_muon.hip", "gvq_muon_small.hip",
-           "gvq_layers_api.cpp", "gvq_i8.hip", "gvq_i8_product.hip", "gvq_distill.hip"]
+           "gvq_layers_api.cpp", "gvq_i8.hip", "gvq_i8_product.hip", "gvq_i8_few.hip", "gvq_distill.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

@@ -1,0 +1,283 @@
+// Products of few rows with a matrix of 8-bit integers, where what there is to move is that matrix, once, and a tile's work-groups would be
+// too few to move it.
+//
+// A work-group has 16 rows of W (gated: 16 of each projection), its 16 waves take the sum in turns of 256 numbers, and each lane reads its operands
+// straight into registers: row lane % 16, 16 bytes of 64.  The waves' sums are whole numbers and are added exactly.  Up to four rows of x
+// are quantised by every work-group for itself, into LDS, while the first turns of W are on their way: that costs it one read of x from the
+// caches and saves a launch.  More rows come in codes, 16 or 32 to a work-group.
+#include "gvq_i8.h"
+#include "gvq_tile.h"
+
+#define I8_FEW_WAVES 16
+
+// The waves' sums of 16 rows of W and R times 16 of x, joined; a lane has four neighbouring results of one row of x.
+template <I8Mode MODE, typename OUT, int R>
+__device__ __forceinline__ void i8_few_out(const I8ProductArgs& a, int r0, int n0, int wave, int lane, const i4v (&acc)[R][MODE == I8_PLAIN ? 1 : 2],
+                                           const float* scales, i4v (*sums)[I8_FEW_WAVES][64])
+{
+    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2;
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int p = 0; p < PAIR; ++p) sums[t * PAIR + p][wave][lane] = acc[t][p];
+    __syncthreads();
+    if (wave >= R) return;
+    i4v v[2] = {sums[wave * PAIR][0][lane], sums[wave * PAIR + PAIR - 1][0][lane]};
+#pragma unroll 5   // (all of a pair's sums at one time would take 128 registers)
+    for (int i = 1; i < I8_FEW_WAVES; ++i) {
+        v[0] += sums[wave * PAIR][i][lane];
+        if constexpr (PAIR == 2) v[1] += sums[wave * PAIR + 1][i][lane];
+    }
+    const int r = r0 + 16 * wave + (lane & 15), c = n0 + 4 * (lane >> 4);
+    if (r < a.m && c < a.n) i8_finish<MODE>(a, (OUT*)a.out, r, c, i8_columns<MODE>(a, c), v[0], v[1], scales[r - r0]);
+}
+
+// Where a lane's row of W begins.
+__device__ __forceinline__ const signed char* i8_few_row(const I8ProductArgs& a, int n0, int lane, int which)
+{
+    const int r = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
+    return a.b + (int64_t)(which ? a.n + r : r) * a.ldk + 16 * (lane >> 4);
+}
+
+// ---- codes --------------------------------------------------------------------------------------------------------
+
+template <I8Mode MODE, typename OUT, int R>
+__global__ __launch_bounds__(64 * I8_FEW_WAVES) void i8_few_kernel(I8ProductArgs a)
+{
+    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2;
+    __shared__ __attribute__((aligned(16))) i4v sums[R * PAIR][I8_FEW_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int t = tile_of_block(blockIdx.x, gridDim.x), r0 = t % a.nm * (16 * R), n0 = t / a.nm * 16;
+    const signed char *w[PAIR], *x[R];
+#pragma unroll
+    for (int p = 0; p < PAIR; ++p) w[p] = i8_few_row(a, n0, lane, p);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int r = r0 + 16 * j + (lane & 15);
+        x[j] = a.a + (int64_t)(r < a.m ? r : a.m - 1) * a.ldk + 16 * (lane >> 4);
+    }
+    i4v acc[R][PAIR];
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int p = 0; p < PAIR; ++p) acc[j][p] = i4v{0, 0, 0, 0};
+    // this wave has the turns wave, wave + 16, ..; what is asked for behind the last one is the last one once more
+    const int turns_all = (int)(a.ldk / 256), turns = turns_all > wave ? (turns_all - wave + I8_FEW_WAVES - 1) / I8_FEW_WAVES : 0;
+    i4v q[2][PAIR][4], y[2][R][4];
+    auto ask = [&](int t, int set) {
+        const int64_t at = 256 * (int64_t)(t < turns ? wave + t * I8_FEW_WAVES : wave + (turns - 1) * I8_FEW_WAVES);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int p = 0; p < PAIR; ++p) q[set][p][i] = *(const i4v*)(w[p] + at + 64 * i);
+#pragma unroll
+            for (int j = 0; j < R; ++j) y[set][j][i] = *(const i4v*)(x[j] + at + 64 * i);
+        }
+    };
+    auto take = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int p = 0; p < PAIR; ++p) acc[j][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[set][p][i], y[set][j][i], acc[j][p], 0, 0, 0);
+    };
+    if (turns > 0) ask(0, 0);
+    for (int t = 0; t < turns; t += 2) {
+        ask(t + 1, 1);
+        take(0);
+        if (t + 1 >= turns) break;
+        ask(t + 2, 0);
+        take(1);
+    }
+    if ((a.ldk & 128) && wave == I8_FEW_WAVES - 1)   // half a turn is left
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int p = 0; p < PAIR; ++p)
+                    acc[j][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i4v*)(w[p] + a.ldk - 128 + 64 * i), *(const i4v*)(x[j] + a.ldk - 128 + 64 * i),
+                                                                    acc[j][p], 0, 0, 0);
+    i8_few_out<MODE, OUT, R>(a, r0, n0, wave, lane, acc, a.a_scales + r0, sums);
+}
+
+// ---- numbers --------------------------------------------------------------------------------------------------------
+
+// ROWS (1, 2 or 4, some of which may lie behind the last) of x; each has its share of the work-group's threads, that take eight numbers
+// at a time and keep HOLD times eight between the largest magnitude and the codes.
+template <typename X, I8Mode MODE, typename OUT, int ROWS>
+__global__ __launch_bounds__(64 * I8_FEW_WAVES) void i8_four_kernel(I8ProductArgs a, const X* x, int64_t ld_x, int k)
+{
+    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, HOLD = 4, T_ROW = 1024 / ROWS;
+    extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][ldk] codes, then the sums
+    __shared__ __attribute__((aligned(16))) i4v sums[PAIR][I8_FEW_WAVES][64];
+    __shared__ unsigned int part[I8_FEW_WAVES];
+    __shared__ float scales[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int n0 = blockIdx.x * 16;
+    const signed char* w[PAIR];
+#pragma unroll
+    for (int p = 0; p < PAIR; ++p) w[p] = i8_few_row(a, n0, lane, p);
+    const int turns_all = (int)(a.ldk / 256), turns = turns_all > wave ? (turns_all - wave + I8_FEW_WAVES - 1) / I8_FEW_WAVES : 0;
+    i4v q[2][PAIR][4];
+    auto ask = [&](int t, int set) {
+        const int64_t at = 256 * (int64_t)(t < turns ? wave + t * I8_FEW_WAVES : wave + (turns - 1) * I8_FEW_WAVES);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int p = 0; p < PAIR; ++p) q[set][p][i] = *(const i4v*)(w[p] + at + 64 * i);
+    };
+    const int row = threadIdx.x / T_ROW, t = threadIdx.x % T_ROW, chunks = (int)(a.ldk >> 3);
+    const X* from = x + (int64_t)(row < a.m ? row : a.m - 1) * ld_x;
+    float v[HOLD][8];
+    unsigned int top = 0;
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+        const int c = t + i * T_ROW;
+        if (c < chunks) mx_load8(from + 8 * c, true, k - 8 * c, v[i]);
+    }
+    if (turns > 0) {   // behind x's own numbers, which are needed first
+        ask(0, 0);
+        ask(1, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i)
+        if (t + i * T_ROW < chunks) {
+            const unsigned int u = mx_top8(v[i]);
+            top = u > top ? u : top;
+        }
+    for (int c = t + HOLD * T_ROW; c < chunks; c += T_ROW) {
+        float f[8];
+        mx_load8(from + 8 * c, true, k - 8 * c, f);
+        const unsigned int u = mx_top8(f);
+        top = u > top ? u : top;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned int o = (unsigned int)__shfl_xor((int)top, d);
+        top = o > top ? o : top;
+    }
+    if (lane == 0) part[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < I8_FEW_WAVES / ROWS; ++i) {
+        const unsigned int o = part[row * (I8_FEW_WAVES / ROWS) + i];
+        top = o > top ? o : top;
+    }
+    const I8Scale s = i8_scale(top);
+    const unsigned int keep = top >= 0x7f800000u ? 0u : ~0u;
+    if (t == 0) scales[row] = s.down;
+    char* codes = lds + row * a.ldk;
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+        const int c = t + i * T_ROW;
+        if (c < chunks)
+            *(u2*)(codes + 8 * c) = u2{i8_pack4(v[i][0], v[i][1], v[i][2], v[i][3], s.up) & keep, i8_pack4(v[i][4], v[i][5], v[i][6], v[i][7], s.up) & keep};
+    }
+    for (int c = t + HOLD * T_ROW; c < chunks; c += T_ROW) {
+        float f[8];
+        mx_load8(from + 8 * c, true, k - 8 * c, f);
+        *(u2*)(codes + 8 * c) = u2{i8_pack4(f[0], f[1], f[2], f[3], s.up) & keep, i8_pack4(f[4], f[5], f[6], f[7], s.up) & keep};
+    }
+    __syncthreads();
+    // lanes of rows that there are not multiply row 0, and nobody looks at what they get
+    const char* y = lds + ((lane & 15) < ROWS ? (lane & 15) : 0) * a.ldk + 16 * (lane >> 4);
+    i4v acc[1][PAIR];
+#pragma unroll
+    for (int p = 0; p < PAIR; ++p) acc[0][p] = i4v{0, 0, 0, 0};
+    auto take = [&](int t, int set) {
+        const int at = 256 * (wave + t * I8_FEW_WAVES);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i4v b = *(const i4v*)(y + at + 64 * i);
+#pragma unroll
+            for (int p = 0; p < PAIR; ++p) acc[0][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[set][p][i], b, acc[0][p], 0, 0, 0);
+        }
+    };
+    for (int t = 0; t < turns; t += 2) {
+        take(t, 0);
+        ask(t + 2, 0);
+        if (t + 1 >= turns) break;
+        take(t + 1, 1);
+        ask(t + 3, 1);
+    }
+    if ((a.ldk & 128) && wave == I8_FEW_WAVES - 1)   // half a turn is left
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const i4v b = *(const i4v*)(y + a.ldk - 128 + 64 * i);
+#pragma unroll
+            for (int p = 0; p < PAIR; ++p)
+                acc[0][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i4v*)(w[p] + a.ldk - 128 + 64 * i), b, acc[0][p], 0, 0, 0);
+        }
+    i8_few_out<MODE, OUT, 1>(a, 0, n0, wave, lane, acc, scales, sums);
+}
+
+template <I8Mode MODE, typename OUT>
+static int launch_codes(I8ProductArgs a, int tiles, hipStream_t st)
+{
+    a.nm = (a.m + 16 * tiles - 1) / (16 * tiles);
+    const int64_t groups = (int64_t)((a.n + 15) / 16) * a.nm;
+    if (groups > 0x7fffffff) return GVQ_EINVAL;
+    if (tiles == 1) hipLaunchKernelGGL((i8_few_kernel<MODE, OUT, 1>), dim3((unsigned)groups), dim3(64 * I8_FEW_WAVES), 0, st, a);
+    else hipLaunchKernelGGL((i8_few_kernel<MODE, OUT, 2>), dim3((unsigned)groups), dim3(64 * I8_FEW_WAVES), 0, st, a);
+    GVQ_HIP(hipGetLastError());
+    return GVQ_OK;
+}
+
+int gvq_launch_i8_few(const I8ProductArgs& a, int tiles, I8Mode mode, gvq_dtype_t dtype, hipStream_t st)
+{
+    if (dtype == GVQ_BF16)
+        return mode == I8_PLAIN ? launch_codes<I8_PLAIN, unsigned short>(a, tiles, st)
+                                : mode == I8_GATED ? launch_codes<I8_GATED, unsigned short>(a, tiles, st) : launch_codes<I8_INNER, unsigned short>(a, tiles, st);
+    return mode == I8_PLAIN ? launch_codes<I8_PLAIN, float>(a, tiles, st)
+                            : mode == I8_GATED ? launch_codes<I8_GATED, float>(a, tiles, st) : launch_codes<I8_INNER, float>(a, tiles, st);
+}
+
+#define I8_FOUR_LDS (64 * 1024)   // of codes
+
+template <typename X, I8Mode MODE, typename OUT, int ROWS>
+static int launch_numbers(const I8ProductArgs& a, const void* x, int64_t ld_x, int k, hipStream_t st)
+{
+    static gvq_once_per_device lds;
+    int dev;
+    GVQ_HIP(hipGetDevice(&dev));
+    const int rc = lds.call(dev, [] {
+        GVQ_HIP(hipFuncSetAttribute((const void*)i8_four_kernel<X, MODE, OUT, ROWS>, hipFuncAttributeMaxDynamicSharedMemorySize, I8_FOUR_LDS));
+        return (int)GVQ_OK;
+    });
+    if (rc != GVQ_OK) return rc;
+    hipLaunchKernelGGL((i8_four_kernel<X, MODE, OUT, ROWS>), dim3((unsigned)((a.n + 15) / 16)), dim3(64 * I8_FEW_WAVES), (unsigned)(ROWS * a.ldk), st, a,
+                       (const X*)x, ld_x, k);
+    GVQ_HIP(hipGetLastError());
+    return GVQ_OK;
+}
+template <typename X, I8Mode MODE, typename OUT>
+static int launch_rows(const I8ProductArgs& a, const void* x, int64_t ld_x, int k, hipStream_t st)
+{
+    return a.m == 1 ? launch_numbers<X, MODE, OUT, 1>(a, x, ld_x, k, st)
+                    : a.m == 2 ? launch_numbers<X, MODE, OUT, 2>(a, x, ld_x, k, st) : launch_numbers<X, MODE, OUT, 4>(a, x, ld_x, k, st);
+}
+template <typename X, typename OUT>
+static int launch_numbers_mode(const I8ProductArgs& a, const void* x, int64_t ld_x, int k, I8Mode mode, hipStream_t st)
+{
+    return mode == I8_PLAIN ? launch_rows<X, I8_PLAIN, OUT>(a, x, ld_x, k, st) : launch_rows<X, I8_GATED, OUT>(a, x, ld_x, k, st);
+}
+
+bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k, I8Mode mode)
+{
+    if (rows > 4 || mode == I8_INNER || (((uintptr_t)x | (uintptr_t)(ld_x * (x_dtype == GVQ_BF16 ? 2 : 4))) & 15) != 0) return false;
+    return (rows > 2 ? 4 : rows) * gvq_i8_row_bytes(k) <= I8_FOUR_LDS;
+}
+
+int gvq_launch_i8_few_numbers(I8ProductArgs a, const void* x, gvq_dtype_t x_dtype, int64_t ld_x, int64_t k, I8Mode mode, gvq_dtype_t dtype,
+                              hipStream_t st)
+{
+    const int64_t es = dtype == GVQ_BF16 ? 2 : 4;
+    a.words = (((uintptr_t)a.out | (uintptr_t)(a.ld * es)) & (uintptr_t)(4 * es - 1)) == 0;
+    if (x_dtype == GVQ_BF16)
+        return dtype == GVQ_BF16 ? launch_numbers_mode<unsigned short, unsigned short>(a, x, ld_x, (int)k, mode, st)
+                                 : launch_numbers_mode<unsigned short, float>(a, x, ld_x, (int)k, mode, st);
+    return dtype == GVQ_BF16 ? launch_numbers_mode<float, unsigned short>(a, x, ld_x, (int)k, mode, st)
+                             : launch_numbers_mode<float, float>(a, x, ld_x, (int)k, mode, st);
+}

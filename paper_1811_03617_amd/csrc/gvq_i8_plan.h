@@ -1,0 +1,49 @@
+// Which way an 8-bit product takes.  Plain C++: nothing here needs HIP.
+#pragma once
+#include <cstdint>
+
+// A way's time: rounds over 256 compute units, of up to `share` work-groups a unit; each round has a start and so much a step (128 numbers
+// of the sum), more for every work-group that shares the unit.  Fitted to 263 products (17 to 4096 rows, 256 to 25088 columns, sums of 384 to
+// 16384) that were each measured in all ways: what is picked is 1.6 % behind the fastest on average, 39 % at most (two of them; six in a
+// hundred more than 10 %).  Tiles of 128 x 128 by eight waves with four stages, and of 128 x 64, were never more than 0.7 % better on average and
+// are not built.
+struct I8Way {
+    int rows, cols;   // of the result a work-group takes
+    double call_us, start_us, step_us, more_us;
+    int share;
+};
+enum { I8_FEW_16, I8_FEW_32, I8_TILE_64, I8_TILE_64_DEEP, I8_TILE_128, I8_TILE_256, I8_WAYS };
+static const I8Way i8_ways[I8_WAYS] = {
+    {16, 16, 2.40, 0.96, 0.107, 0.109, 2},   // straight from memory, 16 rows of the first operand, and 32
+    {32, 16, 2.37, 1.03, 0.149, 0.170, 2},
+    {64, 64, 1.05, 2.74, 0.318, 0.165, 5},   // two stages, and four
+    {64, 64, 1.86, 2.17, 0.279, 0.118, 2},
+    {128, 128, 1.69, 4.31, 0.576, 0.408, 2},
+    {256, 256, 0.00, 9.21, 1.076, 0.0, 1},
+};
+
+// m x n results, each of `sums` sums (2: a gate's and another projection's) over `steps` steps.
+inline double i8_way_time(const I8Way& w, int64_t m, int64_t n, int sums, int64_t steps)
+{
+    // a tile has so many columns of sums; without tiles a work-group takes both sums of its columns
+    const bool few = w.cols == 16;
+    const int64_t across = few ? (n + 15) / 16 : (n * sums + w.cols - 1) / w.cols;
+    const int64_t groups = (m + w.rows - 1) / w.rows * across, per = (groups + 255) / 256;
+    const int64_t full = per / w.share, rest = per % w.share;
+    const double work = (few ? sums : 1) * (double)steps;
+    double t = w.call_us + (double)full * (w.start_us + (w.step_us + w.more_us * (w.share - 1)) * work);
+    if (rest > 0) t += w.start_us + (w.step_us + w.more_us * (rest - 1)) * work;
+    return t;
+}
+
+inline int i8_pick(int64_t m, int64_t n, int sums, int64_t steps)
+{
+    int best = I8_TILE_64;
+    double us = i8_way_time(i8_ways[best], m, n, sums, steps);
+    for (int k = 0; k < I8_WAYS; ++k) {
+        if (steps == 0 && i8_ways[k].cols == 16) continue;   // (a sum over nothing)
+        const double t = i8_way_time(i8_ways[k], m, n, sums, steps);
+        if (t < us) { us = t; best = k; }
+    }
+    return best;
+}

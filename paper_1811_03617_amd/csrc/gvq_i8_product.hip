@@ -3,6 +3,7 @@
 // operand's rows are a gate's and another projection's, a wave has both sums of the same places, and what leaves is act(g) u, or, given the
 // gradient of that, the gradients of g and u.
 #include "gvq_i8.h"
+#include "gvq_i8_plan.h"
 #include "gvq_tile.h"
 
 #define I8_STEP 128   // bytes of a row per step: a line
@@ -81,26 +82,187 @@ __device__ __forceinline__ void i8_tile(const I8ProductArgs& a, int tm, int tn, 
     }
 }
 
-__device__ __forceinline__ f4 i8_load4(const float* p, bool words, int left)
+
+// 256 x 256 by eight waves in two halves that take turns: while the four of one half multiply, one on each SIMD, the four of the other
+// read fragments and ask for rows, and a barrier ends every turn of the two.  A step's products of a wave (128 x 64, 128 numbers of the
+// sum) are four turns of 16 instructions, of half of its rows (A0, A1) and half of its columns each; F is the half of the columns that the
+// step begins with, B0 and B1 by turns, G the other.  What a turn multiplies was asked of LDS one turn earlier at the latest, so that no
+// turn waits for a read that it has just begun.  Each quarter of a stage (the rows of A0, A1, F or G of all waves, 16 KB) is in
+// registers two turns after its read began, and its place then takes the rows of two steps later.
+//   turn (step s)   reads        asks for     multiplies
+//   0               G (s)        A0 (s + 2)   A0 F
+//   1               A1 (s)       F (s + 2)    A0 G
+//   2               A0 (s + 1)   G (s + 2)    A1 G
+//   3               F (s + 1)    A1 (s + 2)   A1 F
+// Five quarters, ten copies of a wave, are younger than the one that the next turn reads.
+struct I8Pong {
+    static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, WAVES = 8, THREADS = 512, MI = 8, NI = 4;
+    static constexpr int STAGE = 512 * I8_STEP, LDS = 2 * STAGE;
+};
+
+// All but the youngest N copies are there, all but the youngest R reads in registers; then the other half's too.
+template <int N, int R>
+__device__ __forceinline__ void i8_turn_over()
 {
-    if (words && left >= 4) return *(const f4*)p;
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) v[i] = p[i];
-    return v;
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" ::"n"(N), "n"(R) : "memory");
 }
-__device__ __forceinline__ f4 i8_load4(const unsigned short* p, bool words, int left)
+
+template <I8Mode MODE>
+__device__ __forceinline__ void i8_tile_pong(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[8][4])
 {
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (words && left >= 4) {
-        const u2 o = *(const u2*)p;
-        return f4{__uint_as_float(o[0] << 16), __uint_as_float(o[0] & 0xffff0000u), __uint_as_float(o[1] << 16), __uint_as_float(o[1] & 0xffff0000u)};
-    }
+    typedef I8Pong T;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wm = wave / T::WN, wn = wave % T::WN, steps = (int)(a.ldk / I8_STEP);
+    const unsigned int lds0 = lds_offset(lds);
+    if (steps <= 0) return;
+    // quarters: 0 A0, 1 B0, 2 B1, 3 A1; a wave has two of the 16 copies of eight rows of each
+    const char* base[4][2];
+    unsigned int voff[4][2], to[4][2];
+    static_for<0, 8>([&](auto n) {
+        constexpr int q = decltype(n)::value / 2, i = decltype(n)::value % 2;
+        constexpr bool of_a = q == 0 || q == 3;
+        constexpr int half = q >= 2 ? 1 : 0;
+        const int c = 2 * wave + i, j0 = of_a ? (c >> 3) * 128 + half * 64 + (c & 7) * 8 : (c >> 2) * 64 + half * 32 + (c & 3) * 8;
+        const int j = j0 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+        int64_t first, r;
+        if (of_a) {
+            first = (int64_t)tm * T::BM + j0 < a.m ? (int64_t)tm * T::BM + j0 : a.m - 1;
+            r = (int64_t)tm * T::BM + j < a.m ? (int64_t)tm * T::BM + j : a.m - 1;
+        } else {
+            first = i8_row_of_b<MODE>(tn, T::BN, j0, a.n);
+            r = i8_row_of_b<MODE>(tn, T::BN, j, a.n);
+        }
+        base[q][i] = (const char*)(of_a ? a.a : a.b) + first * a.ldk;
+        voff[q][i] = (unsigned int)((r - first) * a.ldk) + 16 * piece;
+        to[q][i] = lds0 + (of_a ? 0 : T::BM * I8_STEP) + j0 * I8_STEP;
+    });
+    auto issue = [&](auto which, int s) {
+        constexpr int q = decltype(which)::value;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) v[i] = bf16_to_f32(p[i]);
-    return v;
+        for (int i = 0; i < 2; ++i) copy_rows_to_lds(base[q][i] + (int64_t)s * I8_STEP, voff[q][i], to[q][i] + (unsigned int)(s & 1) * T::STAGE);
+    };
+    const int row = lane & 15, piece[2] = {((lane >> 4) ^ (row & 7)) * 16, ((4 + (lane >> 4)) ^ (row & 7)) * 16};
+    i4v fa[2][4][2], fb[2][2][2];
+    auto read_a = [&](auto which, int s) {
+        constexpr int h = decltype(which)::value;
+        const char* st = lds + (s & 1) * T::STAGE + (wm * 128 + h * 64 + row) * I8_STEP;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int mi = 0; mi < 4; ++mi) fa[h][mi][k] = *(const i4v*)(st + piece[k] + mi * 16 * I8_STEP);
+    };
+    auto read_b = [&](auto which, int s) {
+        constexpr int h = decltype(which)::value;
+        const char* st = lds + (s & 1) * T::STAGE + (T::BM + wn * 64 + h * 32 + row) * I8_STEP;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int ni = 0; ni < 2; ++ni) fb[h][ni][k] = *(const i4v*)(st + piece[k] + ni * 16 * I8_STEP);
+    };
+    auto multiply = [&](auto ha, auto hb) {
+        constexpr int A = decltype(ha)::value, B = decltype(hb)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < 2; ++ni)
+                    acc[4 * A + mi][2 * B + ni] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[B][ni][k], fa[A][mi][k], acc[4 * A + mi][2 * B + ni], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+    };
+    typedef std::integral_constant<int, 0> C0;
+    typedef std::integral_constant<int, 1> C1;
+    typedef std::integral_constant<int, 3> C3;
+    auto step = [&](int s, auto first) {
+        constexpr int F = decltype(first)::value, G = 1 - F;
+        typedef std::integral_constant<int, F> BF;
+        typedef std::integral_constant<int, G> BG;
+        const bool more = s + 2 < steps;
+        auto turn_over = [&](auto reads) {
+            if (more) i8_turn_over<10, decltype(reads)::value>();
+            else i8_turn_over<0, decltype(reads)::value>();
+        };
+        typedef std::integral_constant<int, 4> R4;
+        typedef std::integral_constant<int, 8> R8;
+        read_b(BG{}, s);
+        if (more) issue(C0{}, s + 2);
+        turn_over(R4{});
+        multiply(C0{}, BF{});
+        read_a(C1{}, s);
+        if (more) issue(std::integral_constant<int, 1 + F>{}, s + 2);
+        turn_over(R8{});
+        multiply(C0{}, BG{});
+        read_a(C0{}, s + 1);   // (behind the last step: what is there, which nobody looks at)
+        if (more) issue(std::integral_constant<int, 1 + G>{}, s + 2);
+        turn_over(R8{});
+        multiply(C1{}, BG{});
+        read_b(BG{}, s + 1);
+        if (more) issue(C3{}, s + 2);
+        turn_over(R4{});
+        multiply(C1{}, BF{});
+    };
+    auto ask = [&](int s, auto first) {
+        constexpr int F = decltype(first)::value;
+        issue(C0{}, s);
+        issue(std::integral_constant<int, 1 + F>{}, s);
+        issue(std::integral_constant<int, 2 - F>{}, s);
+        issue(C3{}, s);
+    };
+    ask(0, C0{});
+    if (steps > 1) ask(1, C1{});
+    if (steps > 1) i8_turn_over<12, 0>();
+    else i8_turn_over<0, 0>();
+    read_a(C0{}, 0);
+    read_b(C0{}, 0);
+    if (steps > 1) i8_turn_over<10, 0>();
+    else i8_turn_over<0, 0>();
+    if (wave >= 4) asm volatile("s_barrier" ::: "memory");   // the second half is a turn behind
+    for (int s = 0; s < steps; s += 2) {
+        step(s, C0{});
+        if (s + 1 >= steps) break;
+        step(s + 1, C1{});
+    }
+    if (wave < 4) asm volatile("s_barrier" ::: "memory");
+}
+
+// A wave hands its results out through 4 KB of LDS, so that rows leave in 16-byte words side by side: straight from the accumulators
+// they would leave in pieces of 32 or 64 bytes.  ROWS of C columns at a time; a row's 16-byte pieces are exchanged by the row.
+template <typename OUT, int C>
+struct I8Hand {
+    static constexpr int ROW = C * (int)sizeof(OUT), PIECES = ROW / 16, ROWS = ROW >= 256 ? 16 : 32, PER = 16 / (int)sizeof(OUT);
+    static constexpr int MASK = PIECES < 8 ? PIECES - 1 : 7;
+    static_assert(ROWS * ROW <= 4096, "a wave's share");
+    static __device__ __forceinline__ int place(int r, int byte) { return r * ROW + ((byte >> 4 ^ (r & MASK)) << 4) + (byte & 15); }
+};
+template <typename OUT, int C>
+__device__ __forceinline__ void i8_put(char* w, int r, int c, f4 v)
+{
+    char* p = w + I8Hand<OUT, C>::place(r, c * (int)sizeof(OUT));
+    if constexpr (sizeof(OUT) == 4) *(f4*)p = v;
+    else *(u2*)p = u2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+template <typename OUT, int C>
+__device__ __forceinline__ void i8_hand_out(const char* w, OUT* out, int64_t ld, int rows, int cols, int lane)
+{
+    typedef I8Hand<OUT, C> H;
+#pragma unroll
+    for (int i = 0; i < H::ROWS * H::PIECES / 64; ++i) {
+        const int e = lane + 64 * i, r = e / H::PIECES, c = e % H::PIECES * H::PER, left = cols - c;
+        const u4 v = *(const u4*)(w + H::place(r, 16 * (e % H::PIECES)));
+        OUT* to = out + (int64_t)r * ld + c;
+        if (r < rows && left >= H::PER) *(u4*)to = v;
+        else if (r < rows)
+#pragma unroll
+            for (int k = 0; k < H::PER; ++k)
+                if (k < left) {
+                    if constexpr (sizeof(OUT) == 4) to[k] = __uint_as_float(v[k]);
+                    else to[k] = (OUT)(v[k >> 1] >> (16 * (k & 1)));
+                }
+    }
 }
 
 template <typename T, I8Mode MODE, typename OUT>
@@ -114,51 +276,59 @@ __global__ __launch_bounds__(T::THREADS) void i8_tile_kernel(I8ProductArgs a)
     for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = i4v{0, 0, 0, 0};
-    i8_tile<T, MODE>(a, tm, tn, lds, acc);
+    if constexpr (std::is_same<T, I8Pong>::value) i8_tile_pong<MODE>(a, tm, tn, lds, acc);
+    else i8_tile<T, MODE>(a, tm, tn, lds, acc);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int r0 = tm * T::BM + wave / T::WN * (T::BM / T::WM);
-    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, COLS = T::BN / T::WN / PAIR;
-    const int c0 = tn * (T::BN / PAIR) + wave % T::WN * COLS + 4 * (lane >> 4);
+    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, COLS = T::BN / T::WN / PAIR, NJ = T::NI / PAIR;
+    const int c0 = tn * (T::BN / PAIR) + wave % T::WN * COLS, cl = 4 * (lane >> 4);
     OUT* out = (OUT*)a.out;
+    I8Columns s[NJ];
 #pragma unroll
-    for (int ni = 0; ni < T::NI; ni += PAIR) {
-        const int c = c0 + 16 * (ni / PAIR), left = a.n - c;
-        f4 sg = {0.f, 0.f, 0.f, 0.f}, su = sg;
-        if (a.ldk > 0) {   // (a sum over nothing has no scales)
-            sg = i8_load4(a.b_scales + c, false, left);
-            if constexpr (MODE != I8_PLAIN) su = i8_load4(a.b_scales + a.n + c, false, left);
-        }
+    for (int j = 0; j < NJ; ++j) s[j] = i8_columns<MODE>(a, c0 + cl + 16 * j);
+    if (a.wide && !a.accumulate) {
+        typedef I8Hand<OUT, COLS> H;
+        constexpr int AT = H::ROWS / 16;
+        char* w = lds + wave * 4096;
+        __syncthreads();
+        static_for<0, T::MI / AT>([&](auto turn) {
+            constexpr int M = decltype(turn)::value * AT;
+            f4 more[AT][NJ];
+#pragma unroll
+            for (int mi = 0; mi < AT; ++mi) {
+                const int r = r0 + 16 * (M + mi) + (lane & 15), rr = r < a.m ? r : a.m - 1;
+                const float scale = a.ldk > 0 ? a.a_scales[rr] : 0.f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const I8Results v = i8_results<MODE, OUT>(a, rr, c0 + cl + 16 * j, s[j], acc[M + mi][j * PAIR], acc[M + mi][j * PAIR + PAIR - 1], scale);
+                    i8_put<OUT, COLS>(w, 16 * mi + (lane & 15), cl + 16 * j, v.g);
+                    more[mi][j] = v.u;
+                }
+            }
+            const int rows = a.m - (r0 + 16 * M), cols = a.n - c0;
+            OUT* to = out + (int64_t)(r0 + 16 * M) * a.ld + c0;
+            wave_lds_sync();
+            i8_hand_out<OUT, COLS>(w, to, a.ld, rows, cols, lane);
+            wave_lds_sync();
+            if constexpr (MODE == I8_INNER) {
+#pragma unroll
+                for (int mi = 0; mi < AT; ++mi)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) i8_put<OUT, COLS>(w, 16 * mi + (lane & 15), cl + 16 * j, more[mi][j]);
+                wave_lds_sync();
+                i8_hand_out<OUT, COLS>(w, to + a.n, a.ld, rows, cols, lane);
+                wave_lds_sync();
+            }
+        });
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int mi = 0; mi < T::MI; ++mi) {
             const int r = r0 + 16 * mi + (lane & 15);
-            if (r >= a.m) continue;
-            const float sa = a.ldk > 0 ? a.a_scales[r] : 0.f;
-            f4 g, u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                g[i] = (float)acc[mi][ni][i] * (sa * sg[i]);
-                if constexpr (MODE != I8_PLAIN) u[i] = (float)acc[mi][ni + 1][i] * (sa * su[i]);
-            }
-            if constexpr (MODE == I8_PLAIN) {
-                mx_store4(out + (int64_t)r * a.ld + c, a.words != 0, left, a.accumulate != 0, g);
-            } else if constexpr (MODE == I8_GATED) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) g[i] = i8_activation(g[i], a.activation) * u[i];
-                mx_store4(out + (int64_t)r * a.ld + c, a.words != 0, left, false, g);
-            } else {
-                const f4 dh = i8_load4((const OUT*)a.dh + (int64_t)r * a.ld_dh + c, a.dh_words != 0, left);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float value, slope;
-                    i8_activation_slope(g[i], a.activation, value, slope);
-                    g[i] = dh[i] * u[i] * slope;
-                    u[i] = dh[i] * value;
-                }
-                mx_store4(out + (int64_t)r * a.ld + c, a.words != 0, left, false, g);
-                mx_store4(out + (int64_t)r * a.ld + a.n + c, a.words != 0 && (a.n & 3) == 0, left, false, u);
-            }
+            if (r < a.m) i8_finish<MODE>(a, out, r, c0 + cl + 16 * j, s[j], acc[mi][j * PAIR], acc[mi][j * PAIR + PAIR - 1], a.ldk > 0 ? a.a_scales[r] : 0.f);
         }
-    }
 }
 
 template <typename T, I8Mode MODE, typename OUT>
@@ -183,9 +353,14 @@ static int launch_tile(I8ProductArgs a, hipStream_t st)
 }
 
 template <I8Mode MODE, typename OUT>
-static int launch_mode(const I8ProductArgs& a, hipStream_t st)
+static int launch_mode(const I8ProductArgs& a, int way, hipStream_t st)
 {
-    return launch_tile<I8Shape<128, 128, 2, 2, 2>, MODE, OUT>(a, st);
+    switch (way) {
+    case I8_TILE_64: return launch_tile<I8Shape<64, 64, 2, 2, 2>, MODE, OUT>(a, st);
+    case I8_TILE_64_DEEP: return launch_tile<I8Shape<64, 64, 2, 2, 4>, MODE, OUT>(a, st);
+    case I8_TILE_128: return launch_tile<I8Shape<128, 128, 2, 2, 2>, MODE, OUT>(a, st);
+    default: return launch_tile<I8Pong, MODE, OUT>(a, st);
+    }
 }
 
 int gvq_launch_i8_product(I8ProductArgs a, I8Mode mode, gvq_dtype_t dtype, hipStream_t st)
@@ -193,9 +368,12 @@ int gvq_launch_i8_product(I8ProductArgs a, I8Mode mode, gvq_dtype_t dtype, hipSt
     const int64_t es = dtype == GVQ_BF16 ? 2 : 4;
     a.words = (((uintptr_t)a.out | (uintptr_t)(a.ld * es)) & (uintptr_t)(4 * es - 1)) == 0;
     a.dh_words = (((uintptr_t)a.dh | (uintptr_t)(a.ld_dh * es)) & (uintptr_t)(4 * es - 1)) == 0;
+    a.wide = (((uintptr_t)a.out | (uintptr_t)(a.ld * es) | (mode == I8_INNER ? (uintptr_t)(a.n * es) : 0)) & 15) == 0;
+    const int way = i8_pick(a.m, a.n, mode == I8_PLAIN ? 1 : 2, a.ldk / I8_STEP);
+    if (way <= I8_FEW_32) return gvq_launch_i8_few(a, way == I8_FEW_16 ? 1 : 2, mode, dtype, st);
     if (dtype == GVQ_BF16)
-        return mode == I8_PLAIN ? launch_mode<I8_PLAIN, unsigned short>(a, st)
-                                : mode == I8_GATED ? launch_mode<I8_GATED, unsigned short>(a, st) : launch_mode<I8_INNER, unsigned short>(a, st);
-    return mode == I8_PLAIN ? launch_mode<I8_PLAIN, float>(a, st)
-                            : mode == I8_GATED ? launch_mode<I8_GATED, float>(a, st) : launch_mode<I8_INNER, float>(a, st);
+        return mode == I8_PLAIN ? launch_mode<I8_PLAIN, unsigned short>(a, way, st)
+                                : mode == I8_GATED ? launch_mode<I8_GATED, unsigned short>(a, way, st) : launch_mode<I8_INNER, unsigned short>(a, way, st);
+    return mode == I8_PLAIN ? launch_mode<I8_PLAIN, float>(a, way, st)
+                            : mode == I8_GATED ? launch_mode<I8_GATED, float>(a, way, st) : launch_mode<I8_INNER, float>(a, way, st);
 }

@@ -126,16 +126,21 @@ static int forward(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
     if (!aligned(y, size_of(y_dtype)) ||
         (n_in > 0 && (!aligned(x, size_of(dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16) || !aligned(workspace, 16))))
         return GVQ_EALIGN;
+    const I8Mode mode = both == 1 ? I8_PLAIN : I8_GATED;
     Codes q{nullptr, nullptr};
     if (n_in > 0) {
         Pieces p{(char*)workspace};
         q = take_matrix(p, rows, n_in);
-        const int rc = quantize(x, dtype, rows, n_in, ld_x, q, Codes{nullptr, nullptr}, nullptr, stream);
-        if (rc != GVQ_OK) return rc;
     }
     I8ProductArgs a = product(q.codes, q.scales, w_codes, w_scales, rows, n_out, n_in, y, ld_y, false);
     a.activation = activation;
-    return gvq_launch_i8_product(a, both == 1 ? I8_PLAIN : I8_GATED, y_dtype, (hipStream_t)stream);
+    if (n_in > 0) {
+        if (gvq_i8_few_numbers_takes(x, dtype, rows, ld_x, n_out, n_in, mode))
+            return gvq_launch_i8_few_numbers(a, x, dtype, ld_x, n_in, mode, y_dtype, (hipStream_t)stream);
+        const int rc = quantize(x, dtype, rows, n_in, ld_x, q, Codes{nullptr, nullptr}, nullptr, stream);
+        if (rc != GVQ_OK) return rc;
+    }
+    return gvq_launch_i8_product(a, mode, y_dtype, (hipStream_t)stream);
 }
 
 int gvq_i8_linear(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales,
