@@ -23,7 +23,10 @@ struct I8QuantArgs {
     unsigned int* peaks;             // [chunks][cols], for columns
     int64_t ldc, ldct;               // filled in by the launcher, as are:
     int64_t chunk_rows;
-    int words, across, chunks;
+    int words, chunks;
+    int row_blocks;                  // work-groups that the rows take,
+    int stripes, peak_blocks;        // that the columns' largest magnitudes take, side by side and in all,
+    int across, column_blocks;       // and the columns' codes
 };
 
 // What becomes of the sums of a product.
@@ -43,13 +46,17 @@ struct I8ProductArgs {
     int64_t ld_dh;
     int words, dh_words;  // rows are aligned to four elements
     int wide;             // all of the result's rows (inner: both halves) are aligned to 16 bytes
+    int bf16;             // the result's type
     int nm, nn, band;     // tiles, and how they are swept
 };
 
-int gvq_launch_i8_quantize(I8QuantArgs a, gvq_dtype_t dtype, hipStream_t st);
+// One or two matrices of one type, in the same launches.
+int gvq_launch_i8_quantize(const I8QuantArgs* matrices, int n, gvq_dtype_t dtype, hipStream_t st);
 int gvq_launch_i8_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, gvq_dtype_t dtype, int64_t ld,
                              hipStream_t st);
 int gvq_launch_i8_product(I8ProductArgs a, I8Mode mode, gvq_dtype_t dtype, hipStream_t st);
+// Two plain products, in one launch where that is the faster way.
+int gvq_launch_i8_products(I8ProductArgs a, gvq_dtype_t a_dtype, I8ProductArgs b, gvq_dtype_t b_dtype, hipStream_t st);
 
 typedef int i4v __attribute__((ext_vector_type(4)));
 

@@ -20,14 +20,14 @@ __device__ __forceinline__ unsigned int wave_max(unsigned int v)
 
 // ---- rows -------------------------------------------------------------------------------------------------------
 
-// A row to W waves, eight neighbouring numbers a thread at a time, HOLD times eight in registers; what is behind that is read again.
-template <typename T, int W>
-__global__ __launch_bounds__(W > 4 ? 64 * W : I8Q_THREADS) void i8_rows_kernel(I8QuantArgs a)
+// The `block`-th work-group's rows: four of them, a wave each, or one.  Eight neighbouring numbers a thread at a time, HOLD times eight
+// in registers; what is behind that is read again.
+template <typename T, int W, int HOLD>
+__device__ __forceinline__ void i8_rows(const I8QuantArgs& a, int block, unsigned int* part)
 {
-    constexpr int HOLD = 4, PER = W > 4 ? 1 : 4 / W, T_ROW = 64 * W;
-    __shared__ unsigned int part[W > 4 ? W : 4];
+    constexpr int PER = 4 / W, T_ROW = 64 * W;
     const int t = threadIdx.x % T_ROW;
-    const int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / T_ROW;
+    const int64_t r = (int64_t)block * PER + threadIdx.x / T_ROW;
     if (W == 1 && r >= a.rows) return;
     const T* x = (const T*)a.x + r * a.ld;
     const int chunks = (int)(a.ldc >> 3);
@@ -36,12 +36,14 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : I8Q_THREADS) void i8_rows_kernel(I
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
         const int c = t + i * T_ROW;
-        if (c < chunks) {
-            mx_load8(x + 8 * (int64_t)c, a.words != 0, a.cols - 8 * (int64_t)c, v[i]);
+        if (c < chunks) mx_load8(x + 8 * (int64_t)c, a.words != 0, a.cols - 8 * (int64_t)c, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i)
+        if (t + i * T_ROW < chunks) {
             const unsigned int u = mx_top8(v[i]);
             top = u > top ? u : top;
         }
-    }
     for (int c = t + HOLD * T_ROW; c < chunks; c += T_ROW) {
         float f[8];
         mx_load8(x + 8 * (int64_t)c, a.words != 0, a.cols - 8 * (int64_t)c, f);
@@ -50,12 +52,10 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : I8Q_THREADS) void i8_rows_kernel(I
     }
     top = wave_max(top);
     if constexpr (W > 1) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) part[wave] = top;
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
         __syncthreads();
-        const int first = wave / W * W;
 #pragma unroll
-        for (int i = 0; i < W; ++i) top = part[first + i] > top ? part[first + i] : top;
+        for (int i = 0; i < W; ++i) top = part[i] > top ? part[i] : top;
     }
     const I8Scale s = i8_scale(top);
     const unsigned int keep = top >= 0x7f800000u ? 0u : ~0u;
@@ -77,14 +77,30 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : I8Q_THREADS) void i8_rows_kernel(I
 
 // ---- columns ------------------------------------------------------------------------------------------------------
 
-// Largest magnitudes of a run of rows: a work-group takes 64 lanes' words of columns, its waves every fourth row.
+__device__ __forceinline__ void i8_raise(unsigned int& top, unsigned int u) { top = u > top ? u : top; }
 template <typename T>
-__global__ __launch_bounds__(I8Q_THREADS) void i8_peaks_kernel(I8QuantArgs a)
+__device__ __forceinline__ void i8_raise_word(unsigned int (&top)[16 / sizeof(T)], const u4& v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            i8_raise(top[i], v[i] & 0x7fffffffu);
+        } else {
+            i8_raise(top[2 * i], v[i] << 16 & 0x7fffffffu);
+            i8_raise(top[2 * i + 1], v[i] & 0x7fff0000u);
+        }
+    }
+}
+
+// Largest magnitudes of a run of rows: a work-group takes 64 lanes' words of columns, its waves every fourth row, eight at a time.
+// part: [4][64][PER + 1].
+template <typename T>
+__device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsigned int* part)
 {
     constexpr int PER = 16 / sizeof(T);
-    __shared__ unsigned int part[4][64][PER + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * PER, r0 = (int64_t)blockIdx.y * a.chunk_rows;
+    const int stripe = block % a.stripes, chunk = block / a.stripes;
+    const int64_t c = ((int64_t)stripe * 64 + lane) * PER, r0 = (int64_t)chunk * a.chunk_rows;
     const int64_t r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
     unsigned int top[PER];
 #pragma unroll
@@ -92,110 +108,111 @@ __global__ __launch_bounds__(I8Q_THREADS) void i8_peaks_kernel(I8QuantArgs a)
     if (c < a.cols) {
         const T* x = (const T*)a.x + c;
         if (a.words && c + PER <= a.cols) {
-#pragma unroll 4
-            for (int64_t r = r0 + wave; r < r1; r += 4) {
-                const u4 v = *(const u4*)(x + r * a.ld);
+            int64_t r = r0 + wave;
+            for (; r + 28 < r1; r += 32) {
+                u4 v[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (sizeof(T) == 4) {
-                        const unsigned int u = v[i] & 0x7fffffffu;
-                        top[i] = u > top[i] ? u : top[i];
-                    } else {
-                        const unsigned int lo = v[i] << 16 & 0x7fffffffu, hi = v[i] & 0x7fff0000u;
-                        top[2 * i] = lo > top[2 * i] ? lo : top[2 * i];
-                        top[2 * i + 1] = hi > top[2 * i + 1] ? hi : top[2 * i + 1];
-                    }
-                }
+                for (int i = 0; i < 8; ++i) v[i] = *(const u4*)(x + (r + 4 * i) * a.ld);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) i8_raise_word<T>(top, v[i]);
             }
+            for (; r < r1; r += 4) i8_raise_word<T>(top, *(const u4*)(x + r * a.ld));
         } else {
             for (int64_t r = r0 + wave; r < r1; r += 4)
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
                     if (c + i < a.cols) {
-                        unsigned int u;
-                        if constexpr (sizeof(T) == 4) u = __float_as_uint(x[r * a.ld + i]) & 0x7fffffffu;
-                        else u = ((unsigned int)x[r * a.ld + i] & 0x7fffu) << 16;
-                        top[i] = u > top[i] ? u : top[i];
+                        if constexpr (sizeof(T) == 4) i8_raise(top[i], __float_as_uint(x[r * a.ld + i]) & 0x7fffffffu);
+                        else i8_raise(top[i], ((unsigned int)x[r * a.ld + i] & 0x7fffu) << 16);
                     }
         }
     }
 #pragma unroll
-    for (int i = 0; i < PER; ++i) part[wave][lane][i] = top[i];
+    for (int i = 0; i < PER; ++i) part[(wave * 64 + lane) * (PER + 1) + i] = top[i];
     __syncthreads();
     for (int e = threadIdx.x; e < 64 * PER; e += I8Q_THREADS) {
-        const int64_t cc = (int64_t)blockIdx.x * 64 * PER + e;
+        const int64_t cc = (int64_t)stripe * 64 * PER + e;
         if (cc >= a.cols) break;
         unsigned int m = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const unsigned int u = part[w][e / PER][e % PER];
-            m = u > m ? u : m;
-        }
-        a.peaks[(int64_t)blockIdx.y * a.cols + cc] = m;
+        for (int w = 0; w < 4; ++w) i8_raise(m, part[(w * 64 + e / PER) * (PER + 1) + e % PER]);
+        a.peaks[(int64_t)chunk * a.cols + cc] = m;
     }
 }
 
 // 128 rows of 64 columns: a thread takes four rows of one word of columns, packs each column's four codes, and the tile leaves as
 // 128 bytes of each column.  In LDS a column is eight pieces of 16 bytes, exchanged by the column's group of eight.
 template <typename T>
-__global__ __launch_bounds__(I8Q_THREADS) void i8_columns_kernel(I8QuantArgs a)
+__device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
 {
-    constexpr int PER = 16 / sizeof(T), WORDS = 64 / PER, QUADS = I8Q_THREADS / WORDS;   // words of a row; quads of rows at a time
+    constexpr int PER = 16 / sizeof(T), WORDS = 64 / PER, QUADS = I8Q_THREADS / WORDS, TURNS = 32 / QUADS;   // words of a row; quads of rows at a time
     __shared__ __attribute__((aligned(16))) unsigned int turn[64 * 32];
-    __shared__ float ups[64];
-    __shared__ unsigned int keeps[64];
-    const int64_t tile = tile_of_block(blockIdx.x, gridDim.x);
-    const int64_t r0 = tile / a.across * 128, c0 = tile % a.across * 64;
-    if (threadIdx.x < 64) {
-        const int64_t c = c0 + threadIdx.x;
-        unsigned int top = 0;
-        if (c < a.cols)
-            for (int k = 0; k < a.chunks; ++k) {
-                const unsigned int u = a.peaks[(int64_t)k * a.cols + c];
-                top = u > top ? u : top;
-            }
-        const I8Scale s = i8_scale(top);
-        ups[threadIdx.x] = s.up;
-        keeps[threadIdx.x] = top >= 0x7f800000u ? 0u : ~0u;
-        if (r0 == 0 && c < a.cols) a.scales_t[c] = s.down;
-    }
-    __syncthreads();
+    __shared__ unsigned int tops[4][64];
+    const int64_t r0 = (int64_t)(block / a.across) * 128, c0 = (int64_t)(block % a.across) * 64;
     const int w = threadIdx.x % WORDS, quad0 = threadIdx.x / WORDS;
     const int64_t c = c0 + w * PER;
+    const T* x = (const T*)a.x + c;
+    const bool whole = a.words && c + PER <= a.cols;
+    // the numbers first, then what they are divided by
+    u4 word[TURNS][4];
+#pragma unroll
+    for (int p = 0; p < TURNS; ++p)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t r = r0 + 4 * (quad0 + p * QUADS) + k;
+            u4 v = {0u, 0u, 0u, 0u};
+            if (r < a.rows) {
+                if (whole) {
+                    v = *(const u4*)(x + r * a.ld);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if (c + i < a.cols) {
+                            if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(x[r * a.ld + i]);
+                            else v[i >> 1] |= (unsigned int)x[r * a.ld + i] << (16 * (i & 1));
+                        }
+                }
+            }
+            word[p][k] = v;
+        }
+    {
+        const int col = threadIdx.x & 63, first = threadIdx.x >> 6;
+        unsigned int top = 0;
+        if (c0 + col < a.cols) {
+#pragma unroll
+            for (int k = 0; k < I8_CHUNKS / 4; ++k)
+                if (first + 4 * k < a.chunks) i8_raise(top, a.peaks[(int64_t)(first + 4 * k) * a.cols + c0 + col]);
+        }
+        tops[first][col] = top;
+    }
+    __syncthreads();
     float up[PER];
     unsigned int keep[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) { up[i] = ups[w * PER + i]; keep[i] = keeps[w * PER + i]; }
+    for (int i = 0; i < PER; ++i) {
+        const int col = w * PER + i;
+        unsigned int top = tops[0][col];
+        i8_raise(top, tops[1][col]);
+        i8_raise(top, tops[2][col]);
+        i8_raise(top, tops[3][col]);
+        const I8Scale s = i8_scale(top);
+        up[i] = s.up;
+        keep[i] = top >= 0x7f800000u ? 0u : ~0u;
+        if (r0 == 0 && quad0 == 0 && c + i < a.cols) a.scales_t[c + i] = s.down;
+    }
 #pragma unroll
-    for (int p = 0; p < 32 / QUADS; ++p) {
+    for (int p = 0; p < TURNS; ++p) {
         const int quad = quad0 + p * QUADS;
-        float v[4][PER];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t r = r0 + 4 * quad + k;
-            const T* x = (const T*)a.x + r * a.ld + c;
-            if (r < a.rows && a.words && c + PER <= a.cols) {
-                const u4 u = *(const u4*)x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (sizeof(T) == 4) v[k][i] = __uint_as_float(u[i]);
-                    else { v[k][2 * i] = __uint_as_float(u[i] << 16); v[k][2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    v[k][i] = 0.f;
-                    if (r < a.rows && c + i < a.cols) {
-                        if constexpr (sizeof(T) == 4) v[k][i] = x[i];
-                        else v[k][i] = bf16_to_f32(x[i]);
-                    }
-                }
-            }
-        }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int col = w * PER + i;
-            turn[col * 32 + ((quad >> 2 ^ (col >> 3)) << 2) + (quad & 3)] = i8_pack4(v[0][i], v[1][i], v[2][i], v[3][i], up[i]) & keep[i];
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(word[p][k][i]);
+                else v[k] = __uint_as_float(i & 1 ? word[p][k][i >> 1] & 0xffff0000u : word[p][k][i >> 1] << 16);
+            }
+            turn[col * 32 + ((quad >> 2 ^ (col >> 3)) << 2) + (quad & 3)] = i8_pack4(v[0], v[1], v[2], v[3], up[i]) & keep[i];
         }
     }
     __syncthreads();
@@ -205,6 +222,43 @@ __global__ __launch_bounds__(I8Q_THREADS) void i8_columns_kernel(I8QuantArgs a)
         if (c0 + col < a.cols)
             *(u4*)(a.codes_t + (c0 + col) * a.ldct + r0 + 16 * piece) = *(const u4*)(turn + col * 32 + ((piece ^ (col >> 3)) << 2));
     }
+}
+
+// ---- one or two matrices --------------------------------------------------------------------------------------------
+
+struct I8Two {
+    I8QuantArgs a[2];
+};
+
+// First the rows of both and the columns' largest magnitudes: none needs another's result.  HOLD: what the longer rows keep.
+template <typename T, int HOLD>
+__global__ __launch_bounds__(I8Q_THREADS) void i8_rows_kernel(I8Two m)
+{
+    __shared__ unsigned int part[4 * 64 * (16 / sizeof(T) + 1)];
+    int block = blockIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const I8QuantArgs& a = m.a[i];
+        if (block < a.row_blocks) {
+            if (a.ldc <= 2048) i8_rows<T, 1, 4>(a, block, part);
+            else i8_rows<T, 4, HOLD>(a, block, part);
+            return;
+        }
+        block -= a.row_blocks;
+        if (block < a.peak_blocks) {
+            i8_peaks<T>(a, block, part);
+            return;
+        }
+        block -= a.peak_blocks;
+    }
+}
+// Then the columns' codes.
+template <typename T>
+__global__ __launch_bounds__(I8Q_THREADS) void i8_columns_kernel(I8Two m)
+{
+    const int block = tile_of_block(blockIdx.x, gridDim.x);
+    if (block < m.a[0].column_blocks) i8_columns_of<T>(m.a[0], block);
+    else i8_columns_of<T>(m.a[1], block - m.a[0].column_blocks);
 }
 
 // ---- back ---------------------------------------------------------------------------------------------------------
@@ -226,41 +280,49 @@ __global__ __launch_bounds__(I8Q_THREADS) void i8_values_kernel(const signed cha
 }
 
 template <typename T>
-static int launch_quantize(I8QuantArgs a, hipStream_t st)
+static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
 {
-    if (a.codes) {
-        // the fewest waves whose registers hold a row
-        if (a.ldc <= 2048)
-            hipLaunchKernelGGL((i8_rows_kernel<T, 1>), dim3((unsigned)((a.rows + 3) / 4)), dim3(I8Q_THREADS), 0, st, a);
-        else if (a.ldc <= 8192)
-            hipLaunchKernelGGL((i8_rows_kernel<T, 4>), dim3((unsigned)a.rows), dim3(I8Q_THREADS), 0, st, a);
-        else
-            hipLaunchKernelGGL((i8_rows_kernel<T, 16>), dim3((unsigned)a.rows), dim3(1024), 0, st, a);
-        GVQ_HIP(hipGetLastError());
+    constexpr int PER = 16 / sizeof(T);
+    I8Two m{};
+    int64_t first = 0, second = 0;
+    bool longer = false;
+    for (int i = 0; i < n; ++i) {
+        I8QuantArgs& a = m.a[i];
+        a = matrices[i];
+        a.ldc = gvq_i8_row_bytes(a.cols);
+        a.ldct = gvq_i8_row_bytes(a.rows);
+        a.words = (((uintptr_t)a.x | (uintptr_t)(a.ld * sizeof(T))) & 15) == 0;
+        if (a.codes) {
+            a.row_blocks = (int)(a.ldc <= 2048 ? (a.rows + 3) / 4 : a.rows);
+            longer |= a.ldc > 8192;
+        }
+        if (a.codes_t) {
+            a.chunk_rows = gvq_i8_chunk_rows(a.rows);
+            a.chunks = (int)((a.rows + a.chunk_rows - 1) / a.chunk_rows);
+            a.stripes = (int)((a.cols + 64 * PER - 1) / (64 * PER));
+            a.peak_blocks = a.stripes * a.chunks;
+            a.across = (int)((a.cols + 63) >> 6);
+            const int64_t tiles = a.across * (a.ldct >> 7);
+            if (tiles > 0x3fffffff) return GVQ_EINVAL;
+            a.column_blocks = (int)tiles;
+        }
+        first += a.row_blocks + a.peak_blocks;
+        second += a.column_blocks;
     }
-    if (a.codes_t) {
-        constexpr int PER = 16 / sizeof(T);
-        a.chunk_rows = gvq_i8_chunk_rows(a.rows);
-        a.chunks = (int)((a.rows + a.chunk_rows - 1) / a.chunk_rows);
-        a.across = (int)((a.cols + 63) >> 6);
-        const int64_t tiles = a.across * (a.ldct >> 7);
-        if (tiles > 0x7fffffff) return GVQ_EINVAL;
-        hipLaunchKernelGGL((i8_peaks_kernel<T>), dim3((unsigned)((a.cols + 64 * PER - 1) / (64 * PER)), (unsigned)a.chunks), dim3(I8Q_THREADS), 0,
-                           st, a);
-        GVQ_HIP(hipGetLastError());
-        hipLaunchKernelGGL((i8_columns_kernel<T>), dim3((unsigned)tiles), dim3(I8Q_THREADS), 0, st, a);
+    // rows of up to 16384 numbers stay in registers; the shorter ones' kernel has half of those, and more waves
+    if (longer) hipLaunchKernelGGL((i8_rows_kernel<T, 8>), dim3((unsigned)first), dim3(I8Q_THREADS), 0, st, m);
+    else hipLaunchKernelGGL((i8_rows_kernel<T, 4>), dim3((unsigned)first), dim3(I8Q_THREADS), 0, st, m);
+    GVQ_HIP(hipGetLastError());
+    if (second > 0) {
+        hipLaunchKernelGGL((i8_columns_kernel<T>), dim3((unsigned)second), dim3(I8Q_THREADS), 0, st, m);
         GVQ_HIP(hipGetLastError());
     }
     return GVQ_OK;
 }
 
-int gvq_launch_i8_quantize(I8QuantArgs a, gvq_dtype_t dtype, hipStream_t st)
+int gvq_launch_i8_quantize(const I8QuantArgs* matrices, int n, gvq_dtype_t dtype, hipStream_t st)
 {
-    const int64_t es = dtype == GVQ_BF16 ? 2 : 4;
-    a.ldc = gvq_i8_row_bytes(a.cols);
-    a.ldct = gvq_i8_row_bytes(a.rows);
-    a.words = (((uintptr_t)a.x | (uintptr_t)(a.ld * es)) & 15) == 0;
-    return dtype == GVQ_BF16 ? launch_quantize<unsigned short>(a, st) : launch_quantize<float>(a, st);
+    return dtype == GVQ_BF16 ? launch_quantize<unsigned short>(matrices, n, st) : launch_quantize<float>(matrices, n, st);
 }
 
 int gvq_launch_i8_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, gvq_dtype_t dtype, int64_t ld,

@@ -22,18 +22,23 @@ static const I8Way i8_ways[I8_WAYS] = {
     {256, 256, 0.00, 9.21, 1.076, 0.0, 1},
 };
 
-// m x n results, each of `sums` sums (2: a gate's and another projection's) over `steps` steps.
+// `groups` work-groups over `steps` steps each (on average).
+inline double i8_rounds(const I8Way& w, int64_t groups, double steps)
+{
+    const int64_t per = (groups + 255) / 256, full = per / w.share, rest = per % w.share;
+    double t = w.call_us + (double)full * (w.start_us + (w.step_us + w.more_us * (w.share - 1)) * steps);
+    if (rest > 0) t += w.start_us + (w.step_us + w.more_us * (rest - 1)) * steps;
+    return t;
+}
+// m x n results, each of `sums` sums (2: a gate's and another projection's): a tile has so many columns of sums, and without tiles a work-group takes
+// both sums of its columns.
+inline int64_t i8_groups(const I8Way& w, int64_t m, int64_t n, int sums)
+{
+    return (m + w.rows - 1) / w.rows * (w.cols == 16 ? (n + 15) / 16 : (n * sums + w.cols - 1) / w.cols);
+}
 inline double i8_way_time(const I8Way& w, int64_t m, int64_t n, int sums, int64_t steps)
 {
-    // a tile has so many columns of sums; without tiles a work-group takes both sums of its columns
-    const bool few = w.cols == 16;
-    const int64_t across = few ? (n + 15) / 16 : (n * sums + w.cols - 1) / w.cols;
-    const int64_t groups = (m + w.rows - 1) / w.rows * across, per = (groups + 255) / 256;
-    const int64_t full = per / w.share, rest = per % w.share;
-    const double work = (few ? sums : 1) * (double)steps;
-    double t = w.call_us + (double)full * (w.start_us + (w.step_us + w.more_us * (w.share - 1)) * work);
-    if (rest > 0) t += w.start_us + (w.step_us + w.more_us * (rest - 1)) * work;
-    return t;
+    return i8_rounds(w, i8_groups(w, m, n, sums), (double)steps * (w.cols == 16 ? sums : 1));
 }
 
 inline int i8_pick(int64_t m, int64_t n, int sums, int64_t steps)
@@ -43,6 +48,19 @@ inline int i8_pick(int64_t m, int64_t n, int sums, int64_t steps)
     for (int k = 0; k < I8_WAYS; ++k) {
         if (steps == 0 && i8_ways[k].cols == 16) continue;   // (a sum over nothing)
         const double t = i8_way_time(i8_ways[k], m, n, sums, steps);
+        if (t < us) { us = t; best = k; }
+    }
+    return best;
+}
+
+// Two plain products: the tiles that take both in one launch, or -1 if a launch each, in its own way, is faster.  A launch of its own is 2 us.
+inline int i8_pick_pair(int64_t m0, int64_t n0, int64_t steps0, int64_t m1, int64_t n1, int64_t steps1)
+{
+    int best = -1;
+    double us = i8_way_time(i8_ways[i8_pick(m0, n0, 1, steps0)], m0, n0, 1, steps0) + i8_way_time(i8_ways[i8_pick(m1, n1, 1, steps1)], m1, n1, 1, steps1) + 2.0;
+    for (int k = I8_TILE_64; k < I8_WAYS; ++k) {
+        const int64_t g0 = i8_groups(i8_ways[k], m0, n0, 1), g1 = i8_groups(i8_ways[k], m1, n1, 1);
+        const double t = i8_rounds(i8_ways[k], g0 + g1, ((double)g0 * steps0 + (double)g1 * steps1) / (double)(g0 + g1));
         if (t < us) { us = t; best = k; }
     }
     return best;

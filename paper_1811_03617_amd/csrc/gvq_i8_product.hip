@@ -265,19 +265,20 @@ __device__ __forceinline__ void i8_hand_out(const char* w, OUT* out, int64_t ld,
     }
 }
 
-template <typename T, I8Mode MODE, typename OUT>
-__global__ __launch_bounds__(T::THREADS) void i8_tile_kernel(I8ProductArgs a)
+template <typename T, I8Mode MODE>
+__device__ __forceinline__ void i8_sums(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[T::MI][T::NI])
 {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    int tm, tn;
-    tile_at(tile_of_block(blockIdx.x, a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
-    i4v acc[T::MI][T::NI];
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = i4v{0, 0, 0, 0};
     if constexpr (std::is_same<T, I8Pong>::value) i8_tile_pong<MODE>(a, tm, tn, lds, acc);
     else i8_tile<T, MODE>(a, tm, tn, lds, acc);
+}
+
+template <typename T, I8Mode MODE, typename OUT>
+__device__ __forceinline__ void i8_tile_out(const I8ProductArgs& a, int tm, int tn, char* lds, const i4v (&acc)[T::MI][T::NI])
+{
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int r0 = tm * T::BM + wave / T::WN * (T::BM / T::WM);
     constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, COLS = T::BN / T::WN / PAIR, NJ = T::NI / PAIR;
@@ -332,48 +333,139 @@ __global__ __launch_bounds__(T::THREADS) void i8_tile_kernel(I8ProductArgs a)
 }
 
 template <typename T, I8Mode MODE, typename OUT>
-static int launch_tile(I8ProductArgs a, hipStream_t st)
+__global__ __launch_bounds__(T::THREADS) void i8_tile_kernel(I8ProductArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int tm, tn;
+    tile_at(tile_of_block(blockIdx.x, a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
+    i4v acc[T::MI][T::NI];
+    i8_sums<T, MODE>(a, tm, tn, lds, acc);
+    i8_tile_out<T, MODE, OUT>(a, tm, tn, lds, acc);
+}
+
+// One plain product or two, whose tiles follow each other: the second's fill the round that the first's leave half empty.
+struct I8Pair {
+    I8ProductArgs a[2];
+};
+template <typename T>
+__global__ __launch_bounds__(T::THREADS) void i8_pair_kernel(I8Pair p)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int first = p.a[0].nm * p.a[0].nn, second = (int)blockIdx.x >= first;
+    const I8ProductArgs a = second ? p.a[1] : p.a[0];
+    int tm, tn;
+    tile_at(tile_of_block(blockIdx.x - (second ? first : 0), a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
+    i4v acc[T::MI][T::NI];
+    i8_sums<T, I8_PLAIN>(a, tm, tn, lds, acc);
+    if (a.bf16) i8_tile_out<T, I8_PLAIN, unsigned short>(a, tm, tn, lds, acc);
+    else i8_tile_out<T, I8_PLAIN, float>(a, tm, tn, lds, acc);
+}
+
+template <typename T, I8Mode MODE>
+static int set_tiles(I8ProductArgs& a)
 {
     constexpr int COLS = MODE == I8_PLAIN ? T::BN : T::BN / 2;
     a.nm = (a.m + T::BM - 1) / T::BM;
     a.nn = (a.n + COLS - 1) / COLS;
-    if ((int64_t)a.nm * a.nn > 0x7fffffff) return GVQ_EINVAL;
     a.band = 4;
-    static gvq_once_per_device lds;
+    return (int64_t)a.nm * a.nn > 0x3fffffff ? GVQ_EINVAL : GVQ_OK;
+}
+template <typename T, typename K, typename ARGS>
+static int launch_kernel(K kernel, gvq_once_per_device& lds, const ARGS& args, int64_t tiles, hipStream_t st)
+{
     int dev;
     GVQ_HIP(hipGetDevice(&dev));
-    const int rc = lds.call(dev, [] {
-        GVQ_HIP(hipFuncSetAttribute((const void*)i8_tile_kernel<T, MODE, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+    const int rc = lds.call(dev, [&] {
+        GVQ_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
         return (int)GVQ_OK;
     });
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((i8_tile_kernel<T, MODE, OUT>), dim3(a.nm * a.nn), dim3(T::THREADS), T::LDS, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(T::THREADS), T::LDS, st, args);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
 
+template <typename T, I8Mode MODE, typename OUT>
+static int launch_tile(I8ProductArgs a, hipStream_t st)
+{
+    static gvq_once_per_device lds;
+    const int rc = set_tiles<T, MODE>(a);
+    return rc != GVQ_OK ? rc : launch_kernel<T>(i8_tile_kernel<T, MODE, OUT>, lds, a, (int64_t)a.nm * a.nn, st);
+}
+template <typename T>
+static int launch_pair(I8Pair p, hipStream_t st)
+{
+    static gvq_once_per_device lds;
+    int64_t tiles = 0;
+    for (I8ProductArgs& a : p.a) {
+        if (a.m == 0) continue;
+        const int rc = set_tiles<T, I8_PLAIN>(a);
+        if (rc != GVQ_OK) return rc;
+        tiles += (int64_t)a.nm * a.nn;
+    }
+    return launch_kernel<T>(i8_pair_kernel<T>, lds, p, tiles, st);
+}
+
+typedef I8Shape<64, 64, 2, 2, 2> I8Tile64;
+typedef I8Shape<64, 64, 2, 2, 4> I8Tile64Deep;
+typedef I8Shape<128, 128, 2, 2, 2> I8Tile128;
+
+static int launch_plain(const I8Pair& p, int way, hipStream_t st)
+{
+    switch (way) {
+    case I8_TILE_64: return launch_pair<I8Tile64>(p, st);
+    case I8_TILE_64_DEEP: return launch_pair<I8Tile64Deep>(p, st);
+    case I8_TILE_128: return launch_pair<I8Tile128>(p, st);
+    default: return launch_pair<I8Pong>(p, st);
+    }
+}
 template <I8Mode MODE, typename OUT>
 static int launch_mode(const I8ProductArgs& a, int way, hipStream_t st)
 {
     switch (way) {
-    case I8_TILE_64: return launch_tile<I8Shape<64, 64, 2, 2, 2>, MODE, OUT>(a, st);
-    case I8_TILE_64_DEEP: return launch_tile<I8Shape<64, 64, 2, 2, 4>, MODE, OUT>(a, st);
-    case I8_TILE_128: return launch_tile<I8Shape<128, 128, 2, 2, 2>, MODE, OUT>(a, st);
+    case I8_TILE_64: return launch_tile<I8Tile64, MODE, OUT>(a, st);
+    case I8_TILE_64_DEEP: return launch_tile<I8Tile64Deep, MODE, OUT>(a, st);
+    case I8_TILE_128: return launch_tile<I8Tile128, MODE, OUT>(a, st);
     default: return launch_tile<I8Pong, MODE, OUT>(a, st);
     }
 }
 
-int gvq_launch_i8_product(I8ProductArgs a, I8Mode mode, gvq_dtype_t dtype, hipStream_t st)
+static void set_words(I8ProductArgs& a, I8Mode mode, gvq_dtype_t dtype)
 {
     const int64_t es = dtype == GVQ_BF16 ? 2 : 4;
+    a.bf16 = dtype == GVQ_BF16;
     a.words = (((uintptr_t)a.out | (uintptr_t)(a.ld * es)) & (uintptr_t)(4 * es - 1)) == 0;
     a.dh_words = (((uintptr_t)a.dh | (uintptr_t)(a.ld_dh * es)) & (uintptr_t)(4 * es - 1)) == 0;
     a.wide = (((uintptr_t)a.out | (uintptr_t)(a.ld * es) | (mode == I8_INNER ? (uintptr_t)(a.n * es) : 0)) & 15) == 0;
+}
+
+int gvq_launch_i8_product(I8ProductArgs a, I8Mode mode, gvq_dtype_t dtype, hipStream_t st)
+{
+    set_words(a, mode, dtype);
     const int way = i8_pick(a.m, a.n, mode == I8_PLAIN ? 1 : 2, a.ldk / I8_STEP);
     if (way <= I8_FEW_32) return gvq_launch_i8_few(a, way == I8_FEW_16 ? 1 : 2, mode, dtype, st);
+    if (mode == I8_PLAIN) {
+        I8Pair p{};
+        p.a[0] = a;
+        return launch_plain(p, way, st);
+    }
     if (dtype == GVQ_BF16)
-        return mode == I8_PLAIN ? launch_mode<I8_PLAIN, unsigned short>(a, way, st)
-                                : mode == I8_GATED ? launch_mode<I8_GATED, unsigned short>(a, way, st) : launch_mode<I8_INNER, unsigned short>(a, way, st);
-    return mode == I8_PLAIN ? launch_mode<I8_PLAIN, float>(a, way, st)
-                            : mode == I8_GATED ? launch_mode<I8_GATED, float>(a, way, st) : launch_mode<I8_INNER, float>(a, way, st);
+        return mode == I8_GATED ? launch_mode<I8_GATED, unsigned short>(a, way, st) : launch_mode<I8_INNER, unsigned short>(a, way, st);
+    return mode == I8_GATED ? launch_mode<I8_GATED, float>(a, way, st) : launch_mode<I8_INNER, float>(a, way, st);
+}
+
+int gvq_launch_i8_products(I8ProductArgs a, gvq_dtype_t a_dtype, I8ProductArgs b, gvq_dtype_t b_dtype, hipStream_t st)
+{
+    const int way = i8_pick_pair(a.m, a.n, a.ldk / I8_STEP, b.m, b.n, b.ldk / I8_STEP);
+    if (way < 0) {
+        const int rc = gvq_launch_i8_product(a, I8_PLAIN, a_dtype, st);
+        return rc != GVQ_OK ? rc : gvq_launch_i8_product(b, I8_PLAIN, b_dtype, st);
+    }
+    set_words(a, I8_PLAIN, a_dtype);
+    set_words(b, I8_PLAIN, b_dtype);
+    // the longer tiles first
+    I8Pair p{};
+    p.a[0] = a.ldk >= b.ldk ? a : b;
+    p.a[1] = a.ldk >= b.ldk ? b : a;
+    return launch_plain(p, way, st);
 }

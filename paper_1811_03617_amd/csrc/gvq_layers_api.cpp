@@ -38,14 +38,19 @@ Codes take_matrix(Pieces& p, int64_t rows, int64_t cols)
     return Codes{c, (float*)p.take(4 * rows)};
 }
 
-int quantize(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld, Codes q, Codes qt, void* peaks, void* stream)
+I8QuantArgs matrix(const void* x, int64_t rows, int64_t cols, int64_t ld, Codes q, Codes qt, void* peaks)
 {
     I8QuantArgs a{};
     a.x = x; a.rows = rows; a.cols = cols; a.ld = ld;
     a.codes = q.codes; a.scales = q.scales;
     a.codes_t = qt.codes; a.scales_t = qt.scales;
     a.peaks = (unsigned int*)peaks;
-    return gvq_launch_i8_quantize(a, dtype, (hipStream_t)stream);
+    return a;
+}
+int quantize(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld, Codes q, Codes qt, void* peaks, void* stream)
+{
+    const I8QuantArgs a = matrix(x, rows, cols, ld, q, qt, peaks);
+    return gvq_launch_i8_quantize(&a, 1, dtype, (hipStream_t)stream);
 }
 
 // A sum over nothing has no scales.
@@ -180,16 +185,16 @@ int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t
         void* y_peaks = p.take(peaks_of(rows, n_out));
         xt = take_matrix(p, n_in, rows);
         void* x_peaks = p.take(peaks_of(rows, n_in));
-        rc = quantize(dy, dtype, rows, n_out, ld_dy, dx ? q : none, dw ? qt : none, y_peaks, stream);
-        if (rc == GVQ_OK && dw) rc = quantize(x, dtype, rows, n_in, ld_x, none, xt, x_peaks, stream);
+        const I8QuantArgs both[2] = {matrix(dy, rows, n_out, ld_dy, dx ? q : none, dw ? qt : none, y_peaks), matrix(x, rows, n_in, ld_x, none, xt, x_peaks)};
+        rc = gvq_launch_i8_quantize(both, dw ? 2 : 1, dtype, (hipStream_t)stream);
+        if (rc != GVQ_OK) return rc;
     }
-    if (rc == GVQ_OK && dx && rows > 0)
-        rc = gvq_launch_i8_product(product(q.codes, q.scales, wt_codes, wt_scales, rows, n_in, n_out, dx, ld_dx, false), I8_PLAIN, dx_dtype,
-                                   (hipStream_t)stream);
-    if (rc == GVQ_OK && dw && n_out > 0)
-        rc = gvq_launch_i8_product(product(qt.codes, qt.scales, xt.codes, xt.scales, n_out, n_in, rows, dw, ld_dw, accumulate != 0), I8_PLAIN,
-                                   dw_dtype, (hipStream_t)stream);
-    return rc;
+    const I8ProductArgs to_x = product(q.codes, q.scales, wt_codes, wt_scales, rows, n_in, n_out, dx, ld_dx, false),
+                        to_w = product(qt.codes, qt.scales, xt.codes, xt.scales, n_out, n_in, rows, dw, ld_dw, accumulate != 0);
+    const bool want_x = dx && rows > 0, want_w = dw && n_out > 0;
+    if (want_x && want_w) return gvq_launch_i8_products(to_x, dx_dtype, to_w, dw_dtype, (hipStream_t)stream);
+    if (want_x) return gvq_launch_i8_product(to_x, I8_PLAIN, dx_dtype, (hipStream_t)stream);
+    return want_w ? gvq_launch_i8_product(to_w, I8_PLAIN, dw_dtype, (hipStream_t)stream) : GVQ_OK;
 }
 
 int gvq_i8_gated(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales, int64_t n,
