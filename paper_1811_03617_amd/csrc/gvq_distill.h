@@ -19,4 +19,6 @@ struct DistillArgs {
     int64_t ld_grad;
 };
 
+// Pieces that a row is cut into: few rows of many logits.  workspace: two floats for each.
+int gvq_distill_parts(int64_t rows, int64_t vocab);
 int gvq_launch_distill(const DistillArgs& a, gvq_dtype_t dtype, void* workspace, hipStream_t st);

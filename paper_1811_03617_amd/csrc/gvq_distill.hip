@@ -2,35 +2,41 @@
 //
 //   p = softmax(a / t) over the row's entries, q = softmax(z / t):  l = w t^2 sum_j p_j (log p_j - log q_j),  dz = w t (q - p).
 //
-// One pass keeps each thread's largest logit and its sum of powers; the sums are joined, the row is read again and its gradient leaves.
 // Powers are of 2, of (z - largest) c with c = log2(e) / t: the difference first, since z c alone may leave fp32 (masks of the type's lowest
-// value) and loses bits that the difference keeps.  Bound: memory.
+// value) and loses bits that the difference keeps.  With e_j = 2^((a_j - top_a) c), A = sum e_j, S = sum_v 2^((z_v - top_z) c):
+//   l = w t^2 ln 2 (sum_j e_j ((a_j - top_a) c - (z_j - top_z) c) / A + log2 S - log2 A),
+// so that two rounds of joining are enough: the largest, then A, S and that sum.
+//
+// A row to a wave, to four or to sixteen; each thread keeps its first words of the row in registers and reads only the rest a second
+// time, for the gradient.  Bound: memory.
 #include "gvq_distill.h"
 
-// Eight neighbouring logits of a row.
-__device__ __forceinline__ void distill_load8(const float* p, float (&v)[8])
-{
-    const f4 a = *(const f4*)p, b = *((const f4*)p + 1);
+// Eight neighbouring logits of a row, as they lie in memory.
+template <typename T>
+struct DistillWord {
+    u4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p)
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-}
-__device__ __forceinline__ void distill_load8(const unsigned short* p, float (&v)[8])
-{
-    const u4 a = *(const u4*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(a[i] << 16);
-        v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *((const u4*)p + i);
     }
-}
+    __device__ __forceinline__ void numbers(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(v[i >> 2][i & 3]);
+            else f[i] = __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
+        }
+    }
+};
 __device__ __forceinline__ void distill_store8(float* p, const float (&v)[8])
 {
-    *(f4*)p = f4{v[0], v[1], v[2], v[3]};
-    *((f4*)p + 1) = f4{v[4], v[5], v[6], v[7]};
+    stream_store((f4*)p, f4{v[0], v[1], v[2], v[3]});
+    stream_store((f4*)p + 1, f4{v[4], v[5], v[6], v[7]});
 }
 __device__ __forceinline__ void distill_store8(unsigned short* p, const float (&v)[8])
 {
-    *(u4*)p = u4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    stream_store((u4*)p, u4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
 }
 __device__ __forceinline__ float distill_load(const float* p) { return *p; }
 __device__ __forceinline__ float distill_load(const unsigned short* p) { return bf16_to_f32(*p); }
@@ -66,147 +72,351 @@ __device__ __forceinline__ int distill_head(const T* p, int n)
     return h < n ? h : n;
 }
 
-template <int THREADS, typename F>
-__device__ __forceinline__ float block_all(float v, float* part, F join)
+// What all lanes of a wave hold, joined, for every lane: along rows of 16 lanes, then the rows.  `none` joins without effect.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float distill_lane(float none, float v)
 {
+    return __uint_as_float((unsigned int)__builtin_amdgcn_update_dpp((int)__float_as_uint(none), (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float wave_all(float v, float none, F join)
+{
+    v = join(v, distill_lane<0x111, 0xf>(none, v));   // row_shr 1, 2, 4, 8
+    v = join(v, distill_lane<0x112, 0xf>(none, v));
+    v = join(v, distill_lane<0x114, 0xf>(none, v));
+    v = join(v, distill_lane<0x118, 0xf>(none, v));
+    v = join(v, distill_lane<0x142, 0xa>(none, v));   // row_bcast 15, 31
+    v = join(v, distill_lane<0x143, 0xc>(none, v));
+    return __uint_as_float((unsigned int)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+// Three values over a row's team of threads.  part: [3][TEAM / 64], of this call alone.
+template <int TEAM, typename F>
+__device__ __forceinline__ void team_all(float (&v)[3], float none, float* part, F join)
+{
+    constexpr int WAVES = TEAM / 64;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = join(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = part[0];
+    for (int k = 0; k < 3; ++k) v[k] = wave_all(v[k], none, join);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int i = 1; i < THREADS / 64; ++i) v = join(v, part[i]);
-    return v;
+            for (int k = 0; k < 3; ++k) part[k * WAVES + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            v[k] = part[k * WAVES];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v[k] = join(v[k], part[k * WAVES + i]);
+        }
+    }
+}
+struct JoinMax {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct JoinSum {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+template <int TEAM>
+__device__ __forceinline__ void team_sync()
+{
+    if constexpr (TEAM > 64) __syncthreads();
+    else wave_lds_sync();
 }
 
-// The row's entries: probabilities into p, the student's logits there into z, places into at (-1: absent).  Returns the sum of p log p.
-// All of the work-group; false when there are none.
-template <int THREADS, typename T>
-__device__ __forceinline__ bool distill_entries(const DistillArgs& a, int64_t row, const T* z, float* p, float* zj, int* at, float* part, float& plogp)
+// A row's entries in LDS: the teacher's logits and then e, the student's logits there, their places (-1: absent).
+struct DistillEntries {
+    float *e, *z;
+    int* at;
+};
+template <int TEAM, typename T>
+__device__ __forceinline__ void distill_entries(const DistillArgs& a, int64_t row, int t, const T* z, const DistillEntries& n, float& any, float& top)
 {
-    float top = -INFINITY, any = 0.f;
-    for (int j = threadIdx.x; j < a.n_top; j += THREADS) {
-        const int64_t i = a.index[row * a.ld_index + j];
+    any = 0.f;
+    top = -INFINITY;
+    for (int j = t; j < a.n_top; j += TEAM) {
+        const int64_t i = a.index[row * a.ld_index + j], at = row * a.ld_top + j;
         const bool there = i >= 0 && i < a.vocab;
-        at[j] = there ? (int)i : -1;
-        float v = -INFINITY;
+        float v = -INFINITY, s = 0.f;
         if (there) {
-            const int64_t e = row * a.ld_top + j;
-            v = a.top_bf16 ? bf16_to_f32(((const unsigned short*)a.top)[e]) : ((const float*)a.top)[e];
-            zj[j] = distill_load(z + i);
+            v = a.top_bf16 ? bf16_to_f32(((const unsigned short*)a.top)[at]) : ((const float*)a.top)[at];
+            s = distill_load(z + i);
             any = 1.f;
         }
-        p[j] = v;
+        n.at[j] = there ? (int)i : -1;
+        n.e[j] = v;
+        n.z[j] = s;
         top = fmaxf(top, v);
     }
-    any = block_all<THREADS>(any, part, [](float x, float y) { return fmaxf(x, y); });
-    if (any == 0.f) return false;
-    top = block_all<THREADS>(top, part, [](float x, float y) { return fmaxf(x, y); });
-    float sum = 0.f;
-    for (int j = threadIdx.x; j < a.n_top; j += THREADS)
-        if (at[j] >= 0) sum += distill_power(p[j], top, a.log2_t);
-    sum = block_all<THREADS>(sum, part, [](float x, float y) { return x + y; });
-    const float l2 = __builtin_amdgcn_logf(sum);
-    float s = 0.f;
-    for (int j = threadIdx.x; j < a.n_top; j += THREADS)
-        if (at[j] >= 0) {
-            const float l = (p[j] - top) * a.log2_t - l2, q = __builtin_amdgcn_exp2f(l);
-            p[j] = q;
-            if (q != 0.f) s += q * l;   // (0 log 0 is 0)
+}
+// A and the sum of the loss.
+template <int TEAM>
+__device__ __forceinline__ void distill_sums(const DistillArgs& a, int t, const DistillEntries& n, float top, float from, float& A, float& D)
+{
+    const float c = a.log2_t;
+    A = 0.f;
+    D = 0.f;
+    for (int j = t; j < a.n_top; j += TEAM)
+        if (n.at[j] >= 0) {
+            const float d = (n.e[j] - top) * c, e = __builtin_amdgcn_exp2f(d);
+            n.e[j] = e;
+            A += e;
+            if (e != 0.f) D += e * (d - (n.z[j] - from) * c);   // (0 log 0 is 0)
         }
-    plogp = block_all<THREADS>(s, part, [](float x, float y) { return x + y; });
-    return true;
+}
+// The gradient at the entries' places in [lo, hi), once the rest has been written; the first of several entries of one place has the
+// sum of all.
+template <int TEAM, typename T>
+__device__ __forceinline__ void distill_places(const DistillArgs& a, int t, const DistillEntries& n, T* g, int lo, int hi, float from, float scale, float per)
+{
+    for (int j = t; j < a.n_top; j += TEAM) {
+        const int at = n.at[j];
+        if (at < lo || at >= hi) continue;
+        float sum = 0.f;
+        bool first = true;
+        for (int k = 0; k < a.n_top; ++k)
+            if (n.at[k] == at) {
+                if (k < j) first = false;
+                sum += n.e[k];
+            }
+        if (first) distill_store(g + at, distill_power(n.z[j], from, a.log2_t) * scale - sum * per);
+    }
 }
 
-// One work-group a row.
-template <typename T, int THREADS, bool GRAD>
-__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
+// The gradient of eight neighbours.
+template <typename T>
+__device__ __forceinline__ void distill_out(const DistillWord<T>& word, T* g, bool same, float from, float c, float scale)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float part[THREADS / 64];
-    float *p = (float*)lds, *zj = p + a.n_top;
-    int* at = (int*)(zj + a.n_top);
-    const int64_t row = blockIdx.x;
+    float v[8];
+    word.numbers(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = distill_power(v[k], from, c) * scale;
+    if (same) distill_store8(g, v);
+    else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) distill_store(g + k, v[k]);
+}
+
+// TEAM threads a row (64: four rows a work-group), HOLD times eight logits of each in registers.
+template <typename T, int TEAM, int HOLD, bool GRAD>
+__global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void distill_row_kernel(DistillArgs a)
+{
+    constexpr int ROWS = TEAM > 64 ? 1 : 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][3][n_top]
+    __shared__ float part[2][3 * TEAM / 64];
+    const int t = threadIdx.x % TEAM, which = threadIdx.x / TEAM;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + which;
+    if (ROWS > 1 && row >= a.rows) return;
     const T* z = (const T*)a.logits + row * a.ld;
     T* g = GRAD ? (T*)a.grad + row * a.ld_grad : nullptr;
-    const float w = a.weight ? a.weight[row] : 1.f;
-    float plogp;
-    if (w == 0.f || !distill_entries<THREADS>(a, row, z, p, zj, at, part, plogp)) {
-        if (threadIdx.x == 0) a.loss[row] = 0.f;
+    const float w = a.weight ? a.weight[row] : 1.f, c = a.log2_t;
+    DistillEntries n;
+    n.e = (float*)lds + which * 3 * a.n_top;
+    n.z = n.e + a.n_top;
+    n.at = (int*)(n.z + a.n_top);
+    float round[3] = {0.f, -INFINITY, -INFINITY};   // any entries, the largest of them, the largest logit
+    const int head = distill_head(z, a.vocab), words = (a.vocab - head) / 8, rest = a.vocab - 8 * words;
+    DistillWord<T> held[HOLD];
+    DistillSum sum = {-INFINITY, 0.f};
+    if (w != 0.f) {
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i)
+            if (t + i * TEAM < words) held[i].load(z + head + 8 * (t + i * TEAM));
+        distill_entries<TEAM>(a, row, t, z, n, round[0], round[1]);
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i)
+            if (t + i * TEAM < words) {
+                float v[8];
+                held[i].numbers(v);
+                distill_add(sum, v, c);
+            }
+        for (int i = t + HOLD * TEAM; i < words; i += TEAM) {
+            DistillWord<T> word;
+            float v[8];
+            word.load(z + head + 8 * i);
+            word.numbers(v);
+            distill_add(sum, v, c);
+        }
+        for (int i = t; i < rest; i += TEAM) {
+            const float v[1] = {distill_load(z + (i < head ? i : 8 * words + i))};
+            distill_add(sum, v, c);
+        }
+        round[2] = sum.top;
+    }
+    team_all<TEAM>(round, -INFINITY, part[0], JoinMax());
+    if (!(round[0] > 0.f)) {   // weight 0 or no entries
+        if (t == 0) a.loss[row] = 0.f;
         if (GRAD)
-            for (int i = threadIdx.x; i < a.vocab; i += THREADS) distill_store(g + i, 0.f);
+            for (int i = t; i < a.vocab; i += TEAM) distill_store(g + i, 0.f);
         return;
     }
-    const float c = a.log2_t;
-    const int head = distill_head(z, a.vocab), words = (a.vocab - head) / 8, tail = head + 8 * words;
-    DistillSum sum = {-INFINITY, 0.f};
-    for (int i = threadIdx.x; i < words; i += THREADS) {
-        float v[8];
-        distill_load8(z + head + 8 * i, v);
-        distill_add(sum, v, c);
-    }
-    for (int i = threadIdx.x; i < head + a.vocab - tail; i += THREADS) {
-        const float v[1] = {distill_load(z + (i < head ? i : tail + i - head))};
-        distill_add(sum, v, c);
-    }
-    const float top = block_all<THREADS>(sum.top, part, [](float x, float y) { return fmaxf(x, y); });
-    const float from = distill_from(top);
-    const float s = block_all<THREADS>(sum.sum * distill_power(sum.top, from, c), part, [](float x, float y) { return x + y; });
-    const float l2 = __builtin_amdgcn_logf(s);
-    float l = 0.f;
-    for (int j = threadIdx.x; j < a.n_top; j += THREADS)
-        if (at[j] >= 0 && p[j] != 0.f) l += p[j] * ((zj[j] - from) * c - l2);
-    l = block_all<THREADS>(l, part, [](float x, float y) { return x + y; });
-    if (threadIdx.x == 0) a.loss[row] = w * a.t * a.t * 0.69314718f * (plogp - l);
+    const float from = distill_from(round[2]);
+    float sums[3];   // A, D, S
+    distill_sums<TEAM>(a, t, n, round[1], from, sums[0], sums[1]);
+    sums[2] = sum.sum * distill_power(sum.top, from, c);
+    team_all<TEAM>(sums, 0.f, part[1], JoinSum());
+    if (t == 0)
+        a.loss[row] = w * a.t * a.t * 0.69314718f * (sums[1] / sums[0] + __builtin_amdgcn_logf(sums[2]) - __builtin_amdgcn_logf(sums[0]));
     if constexpr (GRAD) {
-        const float scale = w * a.t / s;
+        const float scale = w * a.t / sums[2];
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
-        for (int i = threadIdx.x; i < words; i += THREADS) {
-            float v[8];
-            distill_load8(z + head + 8 * i, v);
+        for (int i = t + HOLD * TEAM; i < words; i += TEAM) {
+            DistillWord<T> word;
+            word.load(z + head + 8 * i);
+            distill_out(word, g + head + 8 * i, same, from, c, scale);
+        }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = distill_power(v[k], from, c) * scale;
-            if (same) distill_store8(g + head + 8 * i, v);
-            else
-#pragma unroll
-                for (int k = 0; k < 8; ++k) distill_store(g + head + 8 * i + k, v[k]);
+        for (int i = 0; i < HOLD; ++i)
+            if (t + i * TEAM < words) distill_out(held[i], g + head + 8 * (t + i * TEAM), same, from, c, scale);
+        for (int i = t; i < rest; i += TEAM) {
+            const int at = i < head ? i : 8 * words + i;
+            distill_store(g + at, distill_power(distill_load(z + at), from, c) * scale);
         }
-        for (int i = threadIdx.x; i < head + a.vocab - tail; i += THREADS) {
-            const int e = i < head ? i : tail + i - head;
-            distill_store(g + e, distill_power(distill_load(z + e), from, c) * scale);
-        }
-        // the entries' places once more, now that the rest of the row has been written; the first of several entries of one place has
-        // the sum of all
-        __syncthreads();
-        for (int j = threadIdx.x; j < a.n_top; j += THREADS) {
-            if (at[j] < 0) continue;
-            float sum_p = 0.f;
-            bool first = true;
-            for (int k = 0; k < a.n_top; ++k)
-                if (at[k] == at[j]) {
-                    if (k < j) first = false;
-                    sum_p += p[k];
-                }
-            if (first) distill_store(g + at[j], distill_power(zj[j], from, c) * scale - sum_p * (w * a.t));
-        }
+        team_sync<TEAM>();
+        distill_places<TEAM>(a, t, n, g, 0, a.vocab, from, scale, w * a.t / sums[0]);
     }
 }
 
-template <typename T, int THREADS>
+// ---- few rows of many logits -----------------------------------------------------------------------------------------
+
+// A row in `parts` pieces of whole words; its largest logits and sums go into sums [rows][parts][2], and a second launch joins them.
+struct DistillPiece {
+    int lo, hi;
+};
+__device__ __forceinline__ DistillPiece distill_piece(int vocab, int parts, int part)
+{
+    const int per = ((vocab + parts - 1) / parts + 7) / 8 * 8;
+    const int lo = per * part < vocab ? per * part : vocab;
+    return {lo, vocab - lo < per ? vocab : lo + per};
+}
+// Each number of the piece that is this thread's, by words where they can be.
+template <int TEAM, typename T, typename F8, typename F1>
+__device__ __forceinline__ void distill_each(const T* z, DistillPiece p, F8 word, F1 one)
+{
+    const int n = p.hi - p.lo, head = distill_head(z + p.lo, n), words = (n - head) / 8, rest = n - 8 * words;
+    for (int i = threadIdx.x; i < words; i += TEAM) word(p.lo + head + 8 * i);
+    for (int i = threadIdx.x; i < rest; i += TEAM) one(p.lo + (i < head ? i : 8 * words + i));
+}
+
+template <typename T, int TEAM>
+__global__ __launch_bounds__(TEAM) void distill_part_kernel(DistillArgs a, int parts, float* sums)
+{
+    __shared__ float shared[2][3 * TEAM / 64];
+    const int64_t row = blockIdx.x / parts;
+    const int part = blockIdx.x % parts;
+    if (a.weight && a.weight[row] == 0.f) return;   // (nobody reads its sums)
+    const T* z = (const T*)a.logits + row * a.ld;
+    const float c = a.log2_t;
+    DistillSum sum = {-INFINITY, 0.f};
+    distill_each<TEAM>(z, distill_piece(a.vocab, parts, part), [&](int i) {
+        DistillWord<T> word;
+        float v[8];
+        word.load(z + i);
+        word.numbers(v);
+        distill_add(sum, v, c);
+    }, [&](int i) {
+        const float v[1] = {distill_load(z + i)};
+        distill_add(sum, v, c);
+    });
+    float top[3] = {sum.top, -INFINITY, -INFINITY};
+    team_all<TEAM>(top, -INFINITY, shared[0], JoinMax());
+    float s[3] = {sum.sum * distill_power(sum.top, distill_from(top[0]), c), 0.f, 0.f};
+    team_all<TEAM>(s, 0.f, shared[1], JoinSum());
+    if (threadIdx.x == 0) {
+        sums[2 * (row * parts + part)] = top[0];
+        sums[2 * (row * parts + part) + 1] = s[0];
+    }
+}
+
+template <typename T, int TEAM, bool GRAD>
+__global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int parts, const float* sums)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float shared[2][3 * TEAM / 64];
+    const int pieces = GRAD ? parts : 1, t = threadIdx.x;
+    const int64_t row = blockIdx.x / pieces;
+    const DistillPiece piece = distill_piece(a.vocab, parts, blockIdx.x % pieces);
+    const T* z = (const T*)a.logits + row * a.ld;
+    T* g = GRAD ? (T*)a.grad + row * a.ld_grad : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f, c = a.log2_t;
+    DistillEntries n;
+    n.e = (float*)lds;
+    n.z = n.e + a.n_top;
+    n.at = (int*)(n.z + a.n_top);
+    float round[3] = {0.f, -INFINITY, -INFINITY};
+    DistillSum mine = {-INFINITY, 0.f};
+    if (w != 0.f) {
+        distill_entries<TEAM>(a, row, t, z, n, round[0], round[1]);
+        if (t < parts) mine = {sums[2 * (row * parts + t)], sums[2 * (row * parts + t) + 1]};
+        round[2] = mine.top;
+    }
+    team_all<TEAM>(round, -INFINITY, shared[0], JoinMax());
+    if (!(round[0] > 0.f)) {
+        if (t == 0 && piece.lo == 0) a.loss[row] = 0.f;
+        if (GRAD)
+            for (int i = piece.lo + t; i < piece.hi; i += TEAM) distill_store(g + i, 0.f);
+        return;
+    }
+    const float from = distill_from(round[2]);
+    float s[3];
+    distill_sums<TEAM>(a, t, n, round[1], from, s[0], s[1]);
+    s[2] = mine.sum * distill_power(mine.top, from, c);
+    team_all<TEAM>(s, 0.f, shared[1], JoinSum());
+    if (t == 0 && piece.lo == 0)
+        a.loss[row] = w * a.t * a.t * 0.69314718f * (s[1] / s[0] + __builtin_amdgcn_logf(s[2]) - __builtin_amdgcn_logf(s[0]));
+    if constexpr (GRAD) {
+        const float scale = w * a.t / s[2];
+        const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
+        distill_each<TEAM>(z, piece, [&](int i) {
+            DistillWord<T> word;
+            word.load(z + i);
+            distill_out(word, g + i, same, from, c, scale);
+        }, [&](int i) { distill_store(g + i, distill_power(distill_load(z + i), from, c) * scale); });
+        __syncthreads();
+        distill_places<TEAM>(a, t, n, g, piece.lo, piece.hi, from, scale, w * a.t / s[0]);
+    }
+}
+
+template <typename T, int TEAM, int HOLD>
 static int launch_rows(const DistillArgs& a, hipStream_t st)
 {
-    const unsigned lds = (unsigned)(12 * a.n_top);
-    if (a.grad) hipLaunchKernelGGL((distill_row_kernel<T, THREADS, true>), dim3((unsigned)a.rows), dim3(THREADS), lds, st, a);
-    else hipLaunchKernelGGL((distill_row_kernel<T, THREADS, false>), dim3((unsigned)a.rows), dim3(THREADS), lds, st, a);
+    constexpr int ROWS = TEAM > 64 ? 1 : 4;
+    const unsigned lds = (unsigned)(ROWS * 12 * a.n_top);
+    const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS)), threads(TEAM > 64 ? TEAM : 256);
+    if (a.grad) hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, true>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, false>), grid, threads, lds, st, a);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
 
+#define DISTILL_TEAM 256   // of a piece
+
+// In place the second launch's work-groups read the student's logits at entries that another piece's have replaced: then rows stay whole.
+int gvq_distill_parts(int64_t rows, int64_t vocab)
+{
+    if (rows >= 128 || vocab < 65536) return 1;
+    const int64_t want = (512 + rows - 1) / rows, most = vocab / 8192 < DISTILL_TEAM ? vocab / 8192 : DISTILL_TEAM;   // (a thread each joins them)
+    return (int)(want < most ? want : most);
+}
+
+template <typename T>
+static int launch_distill(const DistillArgs& a, float* sums, hipStream_t st)
+{
+    const int parts = a.grad == a.logits ? 1 : gvq_distill_parts(a.rows, a.vocab);
+    if (parts > 1) {
+        const unsigned lds = (unsigned)(12 * a.n_top);
+        const dim3 grid((unsigned)(a.rows * parts)), threads(DISTILL_TEAM);
+        hipLaunchKernelGGL((distill_part_kernel<T, DISTILL_TEAM>), grid, threads, 0, st, a, parts, sums);
+        GVQ_HIP(hipGetLastError());
+        if (a.grad) hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, true>), grid, threads, lds, st, a, parts, sums);
+        else hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, false>), dim3((unsigned)a.rows), threads, lds, st, a, parts, sums);
+        GVQ_HIP(hipGetLastError());
+        return GVQ_OK;
+    }
+    if (a.vocab <= 2048 && a.n_top <= 256) return launch_rows<T, 64, 4>(a, st);
+    if (a.vocab <= 8192) return launch_rows<T, 256, 4>(a, st);
+    return launch_rows<T, 1024, sizeof(T) == 2 ? 6 : 3>(a, st);
+}
+
 int gvq_launch_distill(const DistillArgs& a, gvq_dtype_t dtype, void* workspace, hipStream_t st)
 {
-    (void)workspace;
-    const bool wide = a.vocab > 8192;
-    if (dtype == GVQ_BF16) return wide ? launch_rows<unsigned short, 1024>(a, st) : launch_rows<unsigned short, 256>(a, st);
-    return wide ? launch_rows<float, 1024>(a, st) : launch_rows<float, 256>(a, st);
+    return dtype == GVQ_BF16 ? launch_distill<unsigned short>(a, (float*)workspace, st) : launch_distill<float>(a, (float*)workspace, st);
 }

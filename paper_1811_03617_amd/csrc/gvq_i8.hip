@@ -140,16 +140,17 @@ __device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsign
     }
 }
 
-// 128 rows of 64 columns: a thread takes four rows of one word of columns, packs each column's four codes, and the tile leaves as
+// 128 rows of 256 bytes: a thread takes four rows of one word of columns, packs each column's four codes, and the tile leaves as
 // 128 bytes of each column.  In LDS a column is eight pieces of 16 bytes, exchanged by the column's group of eight.
 template <typename T>
 __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
 {
-    constexpr int PER = 16 / sizeof(T), WORDS = 64 / PER, QUADS = I8Q_THREADS / WORDS, TURNS = 32 / QUADS;   // words of a row; quads of rows at a time
-    __shared__ __attribute__((aligned(16))) unsigned int turn[64 * 32];
-    __shared__ unsigned int tops[4][64];
-    const int64_t r0 = (int64_t)(block / a.across) * 128, c0 = (int64_t)(block % a.across) * 64;
-    const int w = threadIdx.x % WORDS, quad0 = threadIdx.x / WORDS;
+    constexpr int PER = 16 / sizeof(T), COLS = 16 * PER, QUADS = I8Q_THREADS / 16, TURNS = 32 / QUADS;   // quads of rows at a time
+    constexpr int PARTS = I8Q_THREADS / COLS;   // threads that look for one column's largest magnitude
+    __shared__ __attribute__((aligned(16))) unsigned int turn[COLS * 32];
+    __shared__ unsigned int tops[PARTS][COLS];
+    const int64_t r0 = (int64_t)(block / a.across) * 128, c0 = (int64_t)(block % a.across) * COLS;
+    const int w = threadIdx.x & 15, quad0 = threadIdx.x >> 4;
     const int64_t c = c0 + w * PER;
     const T* x = (const T*)a.x + c;
     const bool whole = a.words && c + PER <= a.cols;
@@ -176,12 +177,12 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
             word[p][k] = v;
         }
     {
-        const int col = threadIdx.x & 63, first = threadIdx.x >> 6;
+        const int col = threadIdx.x % COLS, first = threadIdx.x / COLS;
         unsigned int top = 0;
         if (c0 + col < a.cols) {
 #pragma unroll
-            for (int k = 0; k < I8_CHUNKS / 4; ++k)
-                if (first + 4 * k < a.chunks) i8_raise(top, a.peaks[(int64_t)(first + 4 * k) * a.cols + c0 + col]);
+            for (int k = 0; k < I8_CHUNKS / PARTS; ++k)
+                if (first + PARTS * k < a.chunks) i8_raise(top, a.peaks[(int64_t)(first + PARTS * k) * a.cols + c0 + col]);
         }
         tops[first][col] = top;
     }
@@ -192,9 +193,8 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
     for (int i = 0; i < PER; ++i) {
         const int col = w * PER + i;
         unsigned int top = tops[0][col];
-        i8_raise(top, tops[1][col]);
-        i8_raise(top, tops[2][col]);
-        i8_raise(top, tops[3][col]);
+#pragma unroll
+        for (int k = 1; k < PARTS; ++k) i8_raise(top, tops[k][col]);
         const I8Scale s = i8_scale(top);
         up[i] = s.up;
         keep[i] = top >= 0x7f800000u ? 0u : ~0u;
@@ -212,15 +212,15 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
                 if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(word[p][k][i]);
                 else v[k] = __uint_as_float(i & 1 ? word[p][k][i >> 1] & 0xffff0000u : word[p][k][i >> 1] << 16);
             }
-            turn[col * 32 + ((quad >> 2 ^ (col >> 3)) << 2) + (quad & 3)] = i8_pack4(v[0], v[1], v[2], v[3], up[i]) & keep[i];
+            turn[col * 32 + ((quad >> 2 ^ (col >> 3 & 7)) << 2) + (quad & 3)] = i8_pack4(v[0], v[1], v[2], v[3], up[i]) & keep[i];
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < COLS / 32; ++p) {
         const int e = threadIdx.x + p * I8Q_THREADS, col = e >> 3, piece = e & 7;
         if (c0 + col < a.cols)
-            *(u4*)(a.codes_t + (c0 + col) * a.ldct + r0 + 16 * piece) = *(const u4*)(turn + col * 32 + ((piece ^ (col >> 3)) << 2));
+            *(u4*)(a.codes_t + (c0 + col) * a.ldct + r0 + 16 * piece) = *(const u4*)(turn + col * 32 + ((piece ^ (col >> 3 & 7)) << 2));
     }
 }
 
@@ -301,7 +301,7 @@ static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
             a.chunks = (int)((a.rows + a.chunk_rows - 1) / a.chunk_rows);
             a.stripes = (int)((a.cols + 64 * PER - 1) / (64 * PER));
             a.peak_blocks = a.stripes * a.chunks;
-            a.across = (int)((a.cols + 63) >> 6);
+            a.across = (int)((a.cols + 16 * PER - 1) / (16 * PER));
             const int64_t tiles = a.across * (a.ldct >> 7);
             if (tiles > 0x3fffffff) return GVQ_EINVAL;
             a.column_blocks = (int)tiles;

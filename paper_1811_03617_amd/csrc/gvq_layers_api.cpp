@@ -256,7 +256,8 @@ int gvq_i8_gated_backward(const void* dh, int64_t ld_dh, const void* x, int64_t 
 int64_t gvq_distill_workspace(int64_t rows, int64_t vocab, int64_t n_top)
 {
     if (!in_range(rows) || !in_range(vocab) || n_top < 0 || n_top > GVQ_MAX_TOP) return GVQ_EINVAL;
-    return 0;
+    const int parts = gvq_distill_parts(rows, vocab);
+    return parts > 1 ? up256(8 * rows * parts) : 0;
 }
 
 int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* top, gvq_dtype_t top_dtype,
@@ -267,9 +268,9 @@ int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t voc
     if (ld < vocab || ld_top < n_top || ld_index < n_top || (grad && ld_grad < vocab)) return GVQ_EINVAL;
     if (!(temperature >= 1e-3 && temperature <= 1e3)) return GVQ_EINVAL;
     if (rows == 0) return GVQ_OK;
-    if (!loss || (vocab > 0 && !logits) || (n_top > 0 && (!top || !index))) return GVQ_EINVAL;
+    if (!loss || (vocab > 0 && !logits) || (n_top > 0 && (!top || !index)) || (gvq_distill_parts(rows, vocab) > 1 && !workspace)) return GVQ_EINVAL;
     if (!aligned(logits, size_of(dtype)) || !aligned(top, size_of(top_dtype)) || !aligned(index, 8) || !aligned(weight, 4) || !aligned(loss, 4) ||
-        !aligned(grad, size_of(dtype)))
+        !aligned(grad, size_of(dtype)) || !aligned(workspace, 16))
         return GVQ_EALIGN;
     DistillArgs a{};
     a.logits = logits; a.rows = rows; a.ld = ld; a.vocab = (int)vocab;

@@ -9,7 +9,7 @@ stream.  No call records a gradient: `loss` refuses logits that need one, `loss_
 import torch
 
 from . import gvq
-from .mx import _check, _matrix, _no_graph, _now, _workspace, _device
+from .mx import _check, _matrix, _device, _no_graph, _now, _size
 
 
 def _run(logits, top, index, temperature, weight, grad, want):
@@ -31,10 +31,11 @@ def _run(logits, top, index, temperature, weight, grad, want):
         if (rows_g, cols_g) != (rows, vocab) or code_g != code:
             raise ValueError("out: the shape and dtype of logits are needed")
     losses = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    ws = _workspace(logits.device, "gvq_distill_workspace", rows, vocab, n)
+    size = _size("gvq_distill_workspace", rows, vocab, n)
+    ws = torch.empty(size, dtype=torch.uint8, device=logits.device) if size else None   # (most calls need none)
     _check(gvq.lib().gvq_distill(logits.data_ptr(), code, rows, vocab, ld, top.data_ptr(), code_top, index.data_ptr(), n, ld_top,
                                  s0 if rows > 1 else n, None if weight is None else weight.data_ptr(), temperature, losses.data_ptr(),
-                                 grad.data_ptr() if want else None, ld_grad, ws.data_ptr(), _now()), "gvq_distill")
+                                 grad.data_ptr() if want else None, ld_grad, None if ws is None else ws.data_ptr(), _now()), "gvq_distill")
     return losses, grad
 
 
