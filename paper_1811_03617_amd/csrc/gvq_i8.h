@@ -26,7 +26,7 @@ struct I8QuantArgs {
     int words, chunks;
     int row_blocks;                  // work-groups that the rows take,
     int stripes, peak_blocks;        // that the columns' largest magnitudes take, side by side and in all,
-    int across, column_blocks;       // and the columns' codes
+    int across, column_blocks, band; // and the columns' codes, swept so many tiles down at a time
 };
 
 // What becomes of the sums of a product.

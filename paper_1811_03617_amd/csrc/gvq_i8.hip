@@ -149,7 +149,9 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
     constexpr int PARTS = I8Q_THREADS / COLS;   // threads that look for one column's largest magnitude
     __shared__ __attribute__((aligned(16))) unsigned int turn[COLS * 32];
     __shared__ unsigned int tops[PARTS][COLS];
-    const int64_t r0 = (int64_t)(block / a.across) * 128, c0 = (int64_t)(block % a.across) * COLS;
+    int down, over;
+    tile_at(block, (int)(a.ldct >> 7), a.across, a.band, down, over);
+    const int64_t r0 = (int64_t)down * 128, c0 = (int64_t)over * COLS;
     const int w = threadIdx.x & 15, quad0 = threadIdx.x >> 4;
     const int64_t c = c0 + w * PER;
     const T* x = (const T*)a.x + c;
@@ -305,6 +307,7 @@ static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
             const int64_t tiles = a.across * (a.ldct >> 7);
             if (tiles > 0x3fffffff) return GVQ_EINVAL;
             a.column_blocks = (int)tiles;
+            a.band = 16;
         }
         first += a.row_blocks + a.peak_blocks;
         second += a.column_blocks;

@@ -102,55 +102,109 @@ __global__ __launch_bounds__(64 * I8_FEW_WAVES) void i8_few_kernel(I8ProductArgs
     i8_few_out<MODE, OUT, R>(a, r0, n0, wave, lane, acc, a.a_scales + r0, sums);
 }
 
+// Every wave's LDS writes are done; what it asked of memory may still be on its way.
+__device__ __forceinline__ void i8_join_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // ---- numbers --------------------------------------------------------------------------------------------------------
 
+// Eight neighbouring numbers as they lie in memory, of which `left` are in the matrix (the others are 0).
+template <typename T>
+struct I8Word {
+    u4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p, int left)
+    {
+        if (left >= 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *((const u4*)p + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = u4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) {
+                    if constexpr (sizeof(T) == 4) v[i >> 2][i & 3] = __float_as_uint(p[i]);
+                    else v[0][i >> 1] |= (unsigned int)p[i] << (16 * (i & 1));
+                }
+        }
+    }
+    __device__ __forceinline__ void numbers(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(v[i >> 2][i & 3]);
+            else f[i] = __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
+        }
+    }
+    __device__ __forceinline__ unsigned int top() const
+    {
+        float f[8];
+        numbers(f);
+        return mx_top8(f);
+    }
+    __device__ __forceinline__ u2 codes(float up, unsigned int keep) const
+    {
+        float f[8];
+        numbers(f);
+        return u2{i8_pack4(f[0], f[1], f[2], f[3], up) & keep, i8_pack4(f[4], f[5], f[6], f[7], up) & keep};
+    }
+};
+
 // ROWS (1, 2 or 4, some of which may lie behind the last) of x; each has its share of the work-group's threads, that take eight numbers
-// at a time and keep HOLD times eight between the largest magnitude and the codes.
+// at a time and keep their first HOLD words between the largest magnitude and the codes.  A work-group packs x once and goes through
+// every gridDim-th group of 16 rows of W: a wave's turns of all its groups are one stream, asked for two turns ahead, and while one wave joins
+// the sums of a group the others are at the next.
 template <typename X, I8Mode MODE, typename OUT, int ROWS>
 __global__ __launch_bounds__(64 * I8_FEW_WAVES) void i8_four_kernel(I8ProductArgs a, const X* x, int64_t ld_x, int k)
 {
-    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, HOLD = 4, T_ROW = 1024 / ROWS;
-    extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][ldk] codes, then the sums
-    __shared__ __attribute__((aligned(16))) i4v sums[PAIR][I8_FEW_WAVES][64];
+    constexpr int PAIR = MODE == I8_PLAIN ? 1 : 2, HOLD = 8 / sizeof(X), T_ROW = 1024 / ROWS;
+    extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][ldk] codes
+    __shared__ __attribute__((aligned(16))) i4v sums[2][PAIR][I8_FEW_WAVES][64];
     __shared__ unsigned int part[I8_FEW_WAVES];
     __shared__ float scales[16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int n0 = blockIdx.x * 16;
-    const signed char* w[PAIR];
-#pragma unroll
-    for (int p = 0; p < PAIR; ++p) w[p] = i8_few_row(a, n0, lane, p);
-    const int turns_all = (int)(a.ldk / 256), turns = turns_all > wave ? (turns_all - wave + I8_FEW_WAVES - 1) / I8_FEW_WAVES : 0;
-    i4v q[2][PAIR][4];
-    auto ask = [&](int t, int set) {
-        const int64_t at = 256 * (int64_t)(t < turns ? wave + t * I8_FEW_WAVES : wave + (turns - 1) * I8_FEW_WAVES);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int p = 0; p < PAIR; ++p) q[set][p][i] = *(const i4v*)(w[p] + at + 64 * i);
-    };
     const int row = threadIdx.x / T_ROW, t = threadIdx.x % T_ROW, chunks = (int)(a.ldk >> 3);
     const X* from = x + (int64_t)(row < a.m ? row : a.m - 1) * ld_x;
-    float v[HOLD][8];
+    I8Word<X> held[HOLD];
     unsigned int top = 0;
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
         const int c = t + i * T_ROW;
-        if (c < chunks) mx_load8(from + 8 * c, true, k - 8 * c, v[i]);
-    }
-    if (turns > 0) {   // behind x's own numbers, which are needed first
-        ask(0, 0);
-        ask(1, 1);
+        if (c < chunks) held[i].load(from + 8 * c, k - 8 * c);
     }
 #pragma unroll
     for (int i = 0; i < HOLD; ++i)
         if (t + i * T_ROW < chunks) {
-            const unsigned int u = mx_top8(v[i]);
+            const unsigned int u = held[i].top();
             top = u > top ? u : top;
         }
+    // W's first turns are on their way while x is packed
+    const int turns_all = (int)(a.ldk / 256), turns = turns_all > wave ? (turns_all - wave + I8_FEW_WAVES - 1) / I8_FEW_WAVES : 0;
+    const int groups = ((a.n + 15) / 16 - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    i4v q[2][PAIR][4];
+    int ask_turn = 0, ask_group = 0;   // what is asked for next; behind the last turn nothing is
+    auto ask = [&](int set) {
+        if (ask_group >= groups) return;
+        const int n0 = ((int)blockIdx.x + ask_group * (int)gridDim.x) * 16;
+        const int64_t at = 256 * (int64_t)(wave + ask_turn * I8_FEW_WAVES);
+#pragma unroll
+        for (int p = 0; p < PAIR; ++p) {
+            const signed char* w = i8_few_row(a, n0, lane, p) + at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[set][p][i] = *(const i4v*)(w + 64 * i);
+        }
+        if (++ask_turn == turns) { ask_turn = 0; ++ask_group; }
+    };
+    if (turns > 0) {
+        ask(0);
+        ask(1);
+    }
     for (int c = t + HOLD * T_ROW; c < chunks; c += T_ROW) {
-        float f[8];
-        mx_load8(from + 8 * c, true, k - 8 * c, f);
-        const unsigned int u = mx_top8(f);
+        I8Word<X> more;
+        more.load(from + 8 * c, k - 8 * c);
+        const unsigned int u = more.top();
         top = u > top ? u : top;
     }
 #pragma unroll
@@ -172,45 +226,73 @@ __global__ __launch_bounds__(64 * I8_FEW_WAVES) void i8_four_kernel(I8ProductArg
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
         const int c = t + i * T_ROW;
-        if (c < chunks)
-            *(u2*)(codes + 8 * c) = u2{i8_pack4(v[i][0], v[i][1], v[i][2], v[i][3], s.up) & keep, i8_pack4(v[i][4], v[i][5], v[i][6], v[i][7], s.up) & keep};
+        if (c < chunks) *(u2*)(codes + 8 * c) = held[i].codes(s.up, keep);
     }
     for (int c = t + HOLD * T_ROW; c < chunks; c += T_ROW) {
-        float f[8];
-        mx_load8(from + 8 * c, true, k - 8 * c, f);
-        *(u2*)(codes + 8 * c) = u2{i8_pack4(f[0], f[1], f[2], f[3], s.up) & keep, i8_pack4(f[4], f[5], f[6], f[7], s.up) & keep};
+        I8Word<X> more;
+        more.load(from + 8 * c, k - 8 * c);
+        *(u2*)(codes + 8 * c) = more.codes(s.up, keep);
     }
     __syncthreads();
     // lanes of rows that there are not multiply row 0, and nobody looks at what they get
     const char* y = lds + ((lane & 15) < ROWS ? (lane & 15) : 0) * a.ldk + 16 * (lane >> 4);
-    i4v acc[1][PAIR];
+    i4v acc[PAIR];
+    int turn = 0, group = 0;   // what is multiplied next
+    auto clear = [&]() {
 #pragma unroll
-    for (int p = 0; p < PAIR; ++p) acc[0][p] = i4v{0, 0, 0, 0};
-    auto take = [&](int t, int set) {
-        const int at = 256 * (wave + t * I8_FEW_WAVES);
+        for (int p = 0; p < PAIR; ++p) acc[p] = i4v{0, 0, 0, 0};
+    };
+    // A group's sums meet: all waves' in one of two places, which a wave in turn adds up.  That wave is here again, past the next group's
+    // barrier, before anybody writes the same place.
+    auto join = [&]() {
+        const int n0 = ((int)blockIdx.x + group * (int)gridDim.x) * 16;
+        if ((a.ldk & 128) && wave == I8_FEW_WAVES - 1)   // half a turn is left
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const i4v b = *(const i4v*)(y + a.ldk - 128 + 64 * i);
+#pragma unroll
+                for (int p = 0; p < PAIR; ++p)
+                    acc[p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i4v*)(i8_few_row(a, n0, lane, p) + a.ldk - 128 + 64 * i), b, acc[p], 0, 0, 0);
+            }
+        i4v(*place)[I8_FEW_WAVES][64] = sums[group & 1];
+#pragma unroll
+        for (int p = 0; p < PAIR; ++p) place[p][wave][lane] = acc[p];
+        i8_join_barrier();
+        if (wave == (group & (I8_FEW_WAVES - 1))) {
+            i4v v[2] = {place[0][0][lane], place[PAIR - 1][0][lane]};
+#pragma unroll 5   // (all of a pair's sums at one time would take 128 registers)
+            for (int i = 1; i < I8_FEW_WAVES; ++i) {
+                v[0] += place[0][i][lane];
+                if constexpr (PAIR == 2) v[1] += place[1][i][lane];
+            }
+            const int r = lane & 15, c = n0 + 4 * (lane >> 4);
+            if (r < a.m && c < a.n) i8_finish<MODE>(a, (OUT*)a.out, r, c, i8_columns<MODE>(a, c), v[0], v[1], scales[r]);
+        }
+        clear();
+        ++group;
+        turn = 0;
+    };
+    auto take = [&](int set) {
+        const int at = 256 * (wave + turn * I8_FEW_WAVES);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const i4v b = *(const i4v*)(y + at + 64 * i);
 #pragma unroll
-            for (int p = 0; p < PAIR; ++p) acc[0][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[set][p][i], b, acc[0][p], 0, 0, 0);
+            for (int p = 0; p < PAIR; ++p) acc[p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[set][p][i], b, acc[p], 0, 0, 0);
         }
+        ask(set);
+        if (++turn == turns) join();
     };
-    for (int t = 0; t < turns; t += 2) {
-        take(t, 0);
-        ask(t + 2, 0);
-        if (t + 1 >= turns) break;
-        take(t + 1, 1);
-        ask(t + 3, 1);
+    clear();
+    if (turns == 0) {
+        while (group < groups) join();
+        return;
     }
-    if ((a.ldk & 128) && wave == I8_FEW_WAVES - 1)   // half a turn is left
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const i4v b = *(const i4v*)(y + a.ldk - 128 + 64 * i);
-#pragma unroll
-            for (int p = 0; p < PAIR; ++p)
-                acc[0][p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i4v*)(w[p] + a.ldk - 128 + 64 * i), b, acc[0][p], 0, 0, 0);
-        }
-    i8_few_out<MODE, OUT, 1>(a, 0, n0, wave, lane, acc, scales, sums);
+    while (group < groups) {
+        take(0);
+        if (group >= groups) break;
+        take(1);
+    }
 }
 
 template <I8Mode MODE, typename OUT>
@@ -247,7 +329,8 @@ static int launch_numbers(const I8ProductArgs& a, const void* x, int64_t ld_x, i
         return (int)GVQ_OK;
     });
     if (rc != GVQ_OK) return rc;
-    hipLaunchKernelGGL((i8_four_kernel<X, MODE, OUT, ROWS>), dim3((unsigned)((a.n + 15) / 16)), dim3(64 * I8_FEW_WAVES), (unsigned)(ROWS * a.ldk), st, a,
+    const int groups = (a.n + 15) / 16;
+    hipLaunchKernelGGL((i8_four_kernel<X, MODE, OUT, ROWS>), dim3((unsigned)(groups < 256 ? groups : 256)), dim3(64 * I8_FEW_WAVES), (unsigned)(ROWS * a.ldk), st, a,
                        (const X*)x, ld_x, k);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
