@@ -15,24 +15,25 @@ from .mx import _check, _matrix, _device, _no_graph, _now, _size
 def _run(logits, top, index, temperature, weight, grad, want):
     code, ld, rows, vocab = _matrix(logits, "logits")
     code_top, ld_top, rows_top, n = _matrix(top, "top")
-    if rows_top != rows or tuple(index.shape) != (rows, n) or index.dtype != torch.int64 or not index.is_cuda or index.get_device() != _device():
+    if rows_top != rows or tuple(index.shape) != (rows, n) or index.dtype is not torch.int64 or index.get_device() != _device():
         raise ValueError("top and index: a row for each of logits' rows, of one length, and int64 of the index, are needed")
     s0, s1 = index.stride()
     if (n > 1 and s1 != 1) or (rows > 1 and s0 < n):
         raise ValueError("index: neighbouring elements of a row have to be next to each other, and rows must not overlap")
-    if weight is not None and (weight.dtype != torch.float32 or tuple(weight.shape) != (rows,) or not weight.is_contiguous() or not weight.is_cuda
+    if weight is not None and (weight.dtype is not torch.float32 or tuple(weight.shape) != (rows,) or not weight.is_contiguous()
                                or weight.get_device() != _device()):
         raise ValueError(f"weight: float32 of shape ({rows},), contiguous, on the current GPU is needed")
     ld_grad = vocab
     if want:
         if grad is None:
-            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        code_g, ld_grad, rows_g, cols_g = _matrix(grad, "out")
-        if (rows_g, cols_g) != (rows, vocab) or code_g != code:
-            raise ValueError("out: the shape and dtype of logits are needed")
-    losses = torch.empty(rows, dtype=torch.float32, device=logits.device)
+            grad = logits.new_empty((rows, vocab))
+        else:
+            code_g, ld_grad, rows_g, cols_g = _matrix(grad, "out")
+            if (rows_g, cols_g) != (rows, vocab) or code_g != code:
+                raise ValueError("out: the shape and dtype of logits are needed")
+    losses = logits.new_empty(rows, dtype=torch.float32)
     size = _size("gvq_distill_workspace", rows, vocab, n)
-    ws = torch.empty(size, dtype=torch.uint8, device=logits.device) if size else None   # (most calls need none)
+    ws = logits.new_empty(size, dtype=torch.uint8) if size else None   # (most calls need none)
     _check(gvq.lib().gvq_distill(logits.data_ptr(), code, rows, vocab, ld, top.data_ptr(), code_top, index.data_ptr(), n, ld_top,
                                  s0 if rows > 1 else n, None if weight is None else weight.data_ptr(), temperature, losses.data_ptr(),
                                  grad.data_ptr() if want else None, ld_grad, None if ws is None else ws.data_ptr(), _now()), "gvq_distill")

@@ -16,7 +16,7 @@ from typing import NamedTuple
 import torch
 
 from . import gvq
-from .mx import _check, _device, _dtype, _matrix, _no_graph, _now, _workspace
+from .mx import _check, _device, _dtype, _matrix, _no_graph, _now, _size
 
 _ACTIVATIONS = {"silu": gvq.SILU, "gelu": gvq.GELU}
 
@@ -34,15 +34,20 @@ def _stored(q, name, rows, cols):
     codes, scales, r, c = q
     if r != rows or c != cols:
         raise ValueError(f"{name}: {rows} x {cols} is needed, not {r} x {c}")
-    for t, dtype, n in ((codes, torch.int8, 128 * ((cols + 127) // 128)), (scales, torch.float32, 1)):
-        if t.dtype != dtype or t.numel() != rows * n or not t.is_contiguous() or not t.is_cuda or t.get_device() != _device():
-            raise ValueError(f"{name}: codes and scales are not those of a {rows} x {cols} matrix on the current GPU")
+    here = _device()   # (a tensor on the host says -1)
+    if (codes.dtype is not torch.int8 or scales.dtype is not torch.float32 or codes.numel() != rows * (cols + 127 & -128) or scales.numel() != rows
+            or not codes.is_contiguous() or not scales.is_contiguous() or codes.get_device() != here or scales.get_device() != here):
+        raise ValueError(f"{name}: codes and scales are not those of a {rows} x {cols} matrix on the current GPU")
     return codes.data_ptr(), scales.data_ptr()
 
 
-def _empty(rows, cols, device):
-    return I8Matrix(torch.empty((rows, 128 * ((cols + 127) // 128)), dtype=torch.int8, device=device),
-                    torch.empty(rows, dtype=torch.float32, device=device), rows, cols)
+def _empty(rows, cols, x):
+    return I8Matrix(x.new_empty((rows, cols + 127 & -128), dtype=torch.int8), x.new_empty(rows, dtype=torch.float32), rows, cols)
+
+
+def _space(x, name, *sizes):
+    """A call's workspace.  (new_empty is a fifth faster than torch.empty with a dtype and a device, and small calls are as long as that.)"""
+    return x.new_empty(_size(name, *sizes), dtype=torch.uint8)
 
 
 def _activation(name):
@@ -54,9 +59,9 @@ def _activation(name):
 
 def _quantize(x, along_rows, along_cols):
     code, ld, rows, cols = _matrix(x, "x")
-    q = _empty(rows, cols, x.device) if along_rows else None
-    t = _empty(cols, rows, x.device) if along_cols else None
-    ws = _workspace(x.device, "gvq_i8_quantize_workspace", rows, cols) if along_cols else None
+    q = _empty(rows, cols, x) if along_rows else None
+    t = _empty(cols, rows, x) if along_cols else None
+    ws = _space(x, "gvq_i8_quantize_workspace", rows, cols) if along_cols else None
     _check(gvq.lib().gvq_i8_quantize(x.data_ptr(), code, rows, cols, ld, q and q[0].data_ptr(), q and q[1].data_ptr(), t and t[0].data_ptr(),
                                      t and t[1].data_ptr(), None if ws is None else ws.data_ptr(), _now()), "gvq_i8_quantize")
     return q, t
@@ -109,19 +114,19 @@ def linear(x, w, dtype=None):
     code, ld, rows, n_in = _matrix(x, "x")
     n_out = w.rows
     codes, scales = _stored(w, "w", n_out, n_in)
-    y = torch.empty((rows, n_out), dtype=dtype or x.dtype, device=x.device)
-    ws = _workspace(x.device, "gvq_i8_linear_workspace", rows, n_in)
+    y = x.new_empty((rows, n_out), dtype=dtype)
+    ws = _space(x, "gvq_i8_linear_workspace", rows, n_in)
     _check(gvq.lib().gvq_i8_linear(x.data_ptr(), code, rows, n_in, ld, codes, scales, n_out, y.data_ptr(), _dtype(y.dtype, "dtype"), n_out,
                                    ws.data_ptr(), _now()), "gvq_i8_linear")
     return y
 
 
-def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, device):
+def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, x):
     """(tensor, dtype code, row stride) of dw, given or made."""
     if dw is None:
         if accumulate:
             raise ValueError("dw: is needed to add to")
-        dw = torch.empty((rows, cols), dtype=dw_dtype, device=device)
+        dw = x.new_empty((rows, cols), dtype=dw_dtype)
     code, ld, r, c = _matrix(dw, "dw")
     if (r, c) != (rows, cols):
         raise ValueError(f"dw: shape ({rows}, {cols}) is needed")
@@ -136,9 +141,9 @@ def linear_backward(dy, x, wt, dw=None, accumulate=False, dw_dtype=torch.float32
     if rows_x != rows or code_x != code:
         raise ValueError("x: as many rows as dy, and its dtype, are needed")
     codes, scales = _stored(wt, "wt", n_in, n_out) if need_dx else (None, None)
-    dx = torch.empty((rows, n_in), dtype=x.dtype, device=x.device) if need_dx else None
-    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, n_out, n_in, x.device)
-    ws = _workspace(x.device, "gvq_i8_linear_backward_workspace", rows, n_in, n_out)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
+    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, n_out, n_in, x)
+    ws = _space(x, "gvq_i8_linear_backward_workspace", rows, n_in, n_out)
     _check(gvq.lib().gvq_i8_linear_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, code, rows, n_in, n_out, codes, scales,
                                             None if dx is None else dx.data_ptr(), code, n_in, dw.data_ptr(), code_w, ld_dw,
                                             int(accumulate), ws.data_ptr(), _now()), "gvq_i8_linear_backward")
@@ -159,8 +164,8 @@ def gated(x, w, activation="silu", dtype=None):
     code, ld, rows, n_in = _matrix(x, "x")
     n = _halves(w)
     codes, scales = _stored(w, "w", 2 * n, n_in)
-    h = torch.empty((rows, n), dtype=dtype or x.dtype, device=x.device)
-    ws = _workspace(x.device, "gvq_i8_linear_workspace", rows, n_in)
+    h = x.new_empty((rows, n), dtype=dtype)
+    ws = _space(x, "gvq_i8_linear_workspace", rows, n_in)
     _check(gvq.lib().gvq_i8_gated(x.data_ptr(), code, rows, n_in, ld, codes, scales, n, act, h.data_ptr(), _dtype(h.dtype, "dtype"), n,
                                   ws.data_ptr(), _now()), "gvq_i8_gated")
     return h
@@ -179,8 +184,8 @@ def gated_gradient(dh, x, w, activation="silu"):
     """The gradient of [g | u] from that of `gated`'s result, in x's dtype: the dy of the layer that w is."""
     act = _activation(activation)
     code, ld_dh, ld_x, rows, n_in, n, codes, scales = _gated_inputs(dh, x, w)
-    dg = torch.empty((rows, 2 * n), dtype=x.dtype, device=x.device)
-    ws = _workspace(x.device, "gvq_i8_linear_workspace", rows, n_in)
+    dg = x.new_empty((rows, 2 * n))
+    ws = _space(x, "gvq_i8_linear_workspace", rows, n_in)
     _check(gvq.lib().gvq_i8_gated_gradient(dh.data_ptr(), ld_dh, x.data_ptr(), ld_x, code, rows, n_in, n, codes, scales, act, dg.data_ptr(),
                                            2 * n, ws.data_ptr(), _now()), "gvq_i8_gated_gradient")
     return dg
@@ -191,9 +196,9 @@ def gated_backward(dh, x, w, wt, activation="silu", dw=None, accumulate=False, d
     act = _activation(activation)
     code, ld_dh, ld_x, rows, n_in, n, codes, scales = _gated_inputs(dh, x, w)
     t_codes, t_scales = _stored(wt, "wt", n_in, 2 * n) if need_dx else (None, None)
-    dx = torch.empty((rows, n_in), dtype=x.dtype, device=x.device) if need_dx else None
-    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, 2 * n, n_in, x.device)
-    ws = _workspace(x.device, "gvq_i8_gated_backward_workspace", rows, n_in, n)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
+    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, 2 * n, n_in, x)
+    ws = _space(x, "gvq_i8_gated_backward_workspace", rows, n_in, n)
     _check(gvq.lib().gvq_i8_gated_backward(dh.data_ptr(), ld_dh, x.data_ptr(), ld_x, code, rows, n_in, n, codes, scales, t_codes, t_scales, act,
                                            None if dx is None else dx.data_ptr(), code, n_in, dw.data_ptr(), code_w, ld_dw, int(accumulate),
                                            ws.data_ptr(), _now()), "gvq_i8_gated_backward")
