@@ -160,8 +160,8 @@ __device__ __forceinline__ I8Columns i8_columns(const I8ProductArgs& a, int c)
 struct I8Results {
     f4 g, u;
 };
-template <I8Mode MODE, typename OUT>
-__device__ __forceinline__ I8Results i8_results(const I8ProductArgs& a, int r, int c, const I8Columns& s, i4v sums_g, i4v sums_u, float scale)
+template <I8Mode MODE>
+__device__ __forceinline__ I8Results i8_results(const I8Columns& s, i4v sums_g, i4v sums_u, float scale, int activation, f4 dh)
 {
     f4 g, u = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -171,13 +171,12 @@ __device__ __forceinline__ I8Results i8_results(const I8ProductArgs& a, int r, i
     }
     if constexpr (MODE == I8_GATED) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = i8_activation(g[i], a.activation) * u[i];
+        for (int i = 0; i < 4; ++i) g[i] = i8_activation(g[i], activation) * u[i];
     } else if constexpr (MODE == I8_INNER) {
-        const f4 dh = i8_load4((const OUT*)a.dh + (int64_t)r * a.ld_dh + c, a.dh_words != 0, a.n - c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float value, slope;
-            i8_activation_slope(g[i], a.activation, value, slope);
+            i8_activation_slope(g[i], activation, value, slope);
             g[i] = dh[i] * u[i] * slope;
             u[i] = dh[i] * value;
         }
@@ -187,7 +186,9 @@ __device__ __forceinline__ I8Results i8_results(const I8ProductArgs& a, int r, i
 template <I8Mode MODE, typename OUT>
 __device__ __forceinline__ void i8_finish(const I8ProductArgs& a, OUT* out, int r, int c, const I8Columns& s, i4v sums_g, i4v sums_u, float scale)
 {
-    const I8Results v = i8_results<MODE, OUT>(a, r, c, s, sums_g, sums_u, scale);
+    f4 dh = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (MODE == I8_INNER) dh = i8_load4((const OUT*)a.dh + (int64_t)r * a.ld_dh + c, a.dh_words != 0, a.n - c);
+    const I8Results v = i8_results<MODE>(s, sums_g, sums_u, scale, a.activation, dh);
     OUT* p = out + (int64_t)r * a.ld + c;
     mx_store4(p, a.words != 0, a.n - c, MODE == I8_PLAIN && a.accumulate != 0, v.g);
     if constexpr (MODE == I8_INNER) mx_store4(p + a.n, a.words != 0 && (a.n & 3) == 0, a.n - c, false, v.u);

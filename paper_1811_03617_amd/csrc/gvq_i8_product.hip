@@ -245,10 +245,20 @@ __device__ __forceinline__ void i8_put(char* w, int r, int c, f4 v)
     if constexpr (sizeof(OUT) == 4) *(f4*)p = v;
     else *(u2*)p = u2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
+// `wide`: rows are aligned to 16 bytes; otherwise a lane stores one number, next to its neighbours' (4095 x 4097 x 4096 104 us; four to a lane,
+// straight from the accumulators, 129).
 template <typename OUT, int C>
-__device__ __forceinline__ void i8_hand_out(const char* w, OUT* out, int64_t ld, int rows, int cols, int lane)
+__device__ __forceinline__ void i8_hand_out(const char* w, OUT* out, int64_t ld, int rows, int cols, bool wide, int lane)
 {
     typedef I8Hand<OUT, C> H;
+    if (!wide) {
+#pragma unroll 4
+        for (int i = 0; i < H::ROWS * C / 64; ++i) {
+            const int e = lane + 64 * i, r = e / C, c = e % C;
+            if (r < rows && c < cols) out[(int64_t)r * ld + c] = *(const OUT*)(w + H::place(r, c * (int)sizeof(OUT)));
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < H::ROWS * H::PIECES / 64; ++i) {
         const int e = lane + 64 * i, r = e / H::PIECES, c = e % H::PIECES * H::PER, left = cols - c;
@@ -287,7 +297,7 @@ __device__ __forceinline__ void i8_tile_out(const I8ProductArgs& a, int tm, int 
     I8Columns s[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) s[j] = i8_columns<MODE>(a, c0 + cl + 16 * j);
-    if (a.wide && !a.accumulate) {
+    if (!a.accumulate) {
         typedef I8Hand<OUT, COLS> H;
         constexpr int AT = H::ROWS / 16;
         char* w = lds + wave * 4096;
@@ -295,21 +305,44 @@ __device__ __forceinline__ void i8_tile_out(const I8ProductArgs& a, int tm, int 
         static_for<0, T::MI / AT>([&](auto turn) {
             constexpr int M = decltype(turn)::value * AT;
             f4 more[AT][NJ];
+            const int rows = a.m - (r0 + 16 * M), cols = a.n - c0;
+            if (MODE == I8_INNER && !a.dh_words) {   // dh comes the same way
+                const OUT* dh = (const OUT*)a.dh + (int64_t)(r0 + 16 * M) * a.ld_dh + c0;
+#pragma unroll 4
+                for (int i = 0; i < H::ROWS * COLS / 64; ++i) {
+                    const int e = lane + 64 * i, r = e / COLS, c = e % COLS;
+                    if (r < rows && c < cols) *(OUT*)(w + H::place(r, c * (int)sizeof(OUT))) = dh[(int64_t)r * a.ld_dh + c];
+                }
+                wave_lds_sync();
+#pragma unroll
+                for (int mi = 0; mi < AT; ++mi)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+                        more[mi][j] = i8_load4((const OUT*)(w + H::place(16 * mi + (lane & 15), (cl + 16 * j) * (int)sizeof(OUT))), true, 4);
+                wave_lds_sync();
+            } else if (MODE == I8_INNER) {
+#pragma unroll
+                for (int mi = 0; mi < AT; ++mi)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const int r = r0 + 16 * (M + mi) + (lane & 15), c = c0 + cl + 16 * j;
+                        more[mi][j] = i8_load4((const OUT*)a.dh + (int64_t)(r < a.m ? r : a.m - 1) * a.ld_dh + c, true, a.n - c);
+                    }
+            }
 #pragma unroll
             for (int mi = 0; mi < AT; ++mi) {
                 const int r = r0 + 16 * (M + mi) + (lane & 15), rr = r < a.m ? r : a.m - 1;
                 const float scale = a.ldk > 0 ? a.a_scales[rr] : 0.f;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
-                    const I8Results v = i8_results<MODE, OUT>(a, rr, c0 + cl + 16 * j, s[j], acc[M + mi][j * PAIR], acc[M + mi][j * PAIR + PAIR - 1], scale);
+                    const I8Results v = i8_results<MODE>(s[j], acc[M + mi][j * PAIR], acc[M + mi][j * PAIR + PAIR - 1], scale, a.activation, more[mi][j]);
                     i8_put<OUT, COLS>(w, 16 * mi + (lane & 15), cl + 16 * j, v.g);
                     more[mi][j] = v.u;
                 }
             }
-            const int rows = a.m - (r0 + 16 * M), cols = a.n - c0;
             OUT* to = out + (int64_t)(r0 + 16 * M) * a.ld + c0;
             wave_lds_sync();
-            i8_hand_out<OUT, COLS>(w, to, a.ld, rows, cols, lane);
+            i8_hand_out<OUT, COLS>(w, to, a.ld, rows, cols, a.wide != 0, lane);
             wave_lds_sync();
             if constexpr (MODE == I8_INNER) {
 #pragma unroll
@@ -317,7 +350,7 @@ __device__ __forceinline__ void i8_tile_out(const I8ProductArgs& a, int tm, int 
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) i8_put<OUT, COLS>(w, 16 * mi + (lane & 15), cl + 16 * j, more[mi][j]);
                 wave_lds_sync();
-                i8_hand_out<OUT, COLS>(w, to + a.n, a.ld, rows, cols, lane);
+                i8_hand_out<OUT, COLS>(w, to + a.n, a.ld, rows, cols, a.wide != 0, lane);
                 wave_lds_sync();
             }
         });
