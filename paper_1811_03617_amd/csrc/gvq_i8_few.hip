@@ -349,7 +349,8 @@ static int launch_numbers_mode(const I8ProductArgs& a, const void* x, int64_t ld
 
 bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k, I8Mode mode)
 {
-    if (rows > 4 || mode == I8_INNER || (((uintptr_t)x | (uintptr_t)(ld_x * (x_dtype == GVQ_BF16 ? 2 : 4))) & 15) != 0) return false;
+    const int64_t row = rows > 1 ? ld_x * (x_dtype == GVQ_BF16 ? 2 : 4) : 0;   // a single row is aligned where it begins
+    if (rows > 4 || mode == I8_INNER || (((uintptr_t)x | (uintptr_t)row) & 15) != 0) return false;
     return (rows > 2 ? 4 : rows) * gvq_i8_row_bytes(k) <= I8_FOUR_LDS;
 }
 

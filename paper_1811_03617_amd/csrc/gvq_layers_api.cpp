@@ -160,25 +160,40 @@ int64_t gvq_i8_linear_backward_workspace(int64_t rows, int64_t n_in, int64_t n_o
     return matrix_of(rows, n_out) + matrix_of(n_out, rows) + peaks_of(rows, n_out) + matrix_of(n_in, rows) + peaks_of(rows, n_in);
 }
 
-int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
-                           int64_t n_out, const void* wt_codes, const float* wt_scales, void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw,
-                           gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate, void* workspace, void* stream)
+// Whether there is nothing to do, or the arguments are refused: what a backward pass looks at before it begins.  dy: of the layer's outputs, or
+// null where it is about to be made.
+static int look_at_backward(const void* dy, bool dy_is_given, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
+                            int64_t n_out, const void* wt_codes, const float* wt_scales, const void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx,
+                            const void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, const void* workspace, bool* nothing)
 {
+    *nothing = false;
     if (!is_dtype(dtype) || (dx && !is_dtype(dx_dtype)) || (dw && !is_dtype(dw_dtype)) || !is_sum(rows) || !in_range(n_in) || !is_sum(n_out))
         return GVQ_EINVAL;
     if (ld_dy < n_out || (dx && ld_dx < n_in) || (dw && (ld_x < n_in || ld_dw < n_in))) return GVQ_EINVAL;
-    if (n_in == 0 || (rows == 0 && n_out == 0)) return GVQ_OK;
+    *nothing = n_in == 0 || (rows == 0 && n_out == 0);
+    if (*nothing) return GVQ_OK;
     if (!dx && !dw) return GVQ_EINVAL;
     const bool some = rows > 0 && n_out > 0;
-    if (some && (!dy || !workspace || (dx && (!wt_codes || !wt_scales)) || (dw && !x))) return GVQ_EINVAL;
+    if (some && ((dy_is_given && !dy) || !workspace || (dx && (!wt_codes || !wt_scales)) || (dw && !x))) return GVQ_EINVAL;
     if ((some && (!aligned(dy, size_of(dtype)) || !aligned(workspace, 16))) ||
         (dx && (!aligned(dx, size_of(dx_dtype)) || !aligned(wt_codes, 16) || !aligned(wt_scales, 16))) ||
         (dw && (!aligned(dw, size_of(dw_dtype)) || !aligned(x, size_of(dtype)))))
         return GVQ_EALIGN;
+    return GVQ_OK;
+}
+
+int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
+                           int64_t n_out, const void* wt_codes, const float* wt_scales, void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw,
+                           gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate, void* workspace, void* stream)
+{
+    bool nothing;
+    int rc = look_at_backward(dy, true, ld_dy, x, ld_x, dtype, rows, n_in, n_out, wt_codes, wt_scales, dx, dx_dtype, ld_dx, dw, dw_dtype, ld_dw,
+                              workspace, &nothing);
+    if (rc != GVQ_OK || nothing) return rc;
+    const bool some = rows > 0 && n_out > 0;
     Pieces p{(char*)workspace};
     const Codes none{nullptr, nullptr};
     Codes q = none, qt = none, xt = none;
-    int rc = GVQ_OK;
     if (some) {
         q = take_matrix(p, rows, n_out);
         qt = take_matrix(p, n_out, rows);
@@ -204,23 +219,32 @@ int gvq_i8_gated(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, i
     return forward(x, dtype, rows, n_in, ld_x, w_codes, w_scales, n, 2, activation, h, h_dtype, ld_h, workspace, stream);
 }
 
-int gvq_i8_gated_gradient(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t n,
-                          const void* w_codes, const float* w_scales, gvq_activation_t activation, void* dg, int64_t ld_dg, void* workspace,
-                          void* stream)
+static int look_at_gradient(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t n,
+                            const void* w_codes, const float* w_scales, gvq_activation_t activation, const void* dg, bool dg_is_given,
+                            int64_t ld_dg, const void* workspace)
 {
     if (!is_activation(activation) || !is_dtype(dtype) || !in_range(rows) || !is_sum(n_in) || !in_range(n) || !in_range(2 * n) || ld_x < n_in ||
         ld_dh < n || ld_dg < 2 * n)
         return GVQ_EINVAL;
     if (rows == 0 || n == 0) return GVQ_OK;
-    if (!dh || !dg || (n_in > 0 && (!x || !w_codes || !w_scales || !workspace))) return GVQ_EINVAL;
+    if (!dh || (dg_is_given && !dg) || (n_in > 0 && (!x || !w_codes || !w_scales || !workspace))) return GVQ_EINVAL;
     if (!aligned(dh, size_of(dtype)) || !aligned(dg, size_of(dtype)) ||
         (n_in > 0 && (!aligned(x, size_of(dtype)) || !aligned(w_codes, 16) || !aligned(w_scales, 16) || !aligned(workspace, 16))))
         return GVQ_EALIGN;
+    return GVQ_OK;
+}
+
+int gvq_i8_gated_gradient(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t n,
+                          const void* w_codes, const float* w_scales, gvq_activation_t activation, void* dg, int64_t ld_dg, void* workspace,
+                          void* stream)
+{
+    int rc = look_at_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, dg, true, ld_dg, workspace);
+    if (rc != GVQ_OK || rows == 0 || n == 0) return rc;
     Codes q{nullptr, nullptr};
     if (n_in > 0) {
         Pieces p{(char*)workspace};
         q = take_matrix(p, rows, n_in);
-        const int rc = quantize(x, dtype, rows, n_in, ld_x, q, Codes{nullptr, nullptr}, nullptr, stream);
+        rc = quantize(x, dtype, rows, n_in, ld_x, q, Codes{nullptr, nullptr}, nullptr, stream);
         if (rc != GVQ_OK) return rc;
     }
     I8ProductArgs a = product(q.codes, q.scales, w_codes, w_scales, rows, n, n_in, dg, ld_dg, false);
@@ -242,12 +266,16 @@ int gvq_i8_gated_backward(const void* dh, int64_t ld_dh, const void* x, int64_t 
                           void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate,
                           void* workspace, void* stream)
 {
-    if (n < 0 || n > GVQ_I8_MAX_SUM / 2 || !is_sum(n_in)) return GVQ_EINVAL;
-    if (dx == nullptr && dw == nullptr) return GVQ_EINVAL;
-    if (rows > 0 && n > 0 && (!workspace || !aligned(workspace, 16))) return workspace ? GVQ_EALIGN : GVQ_EINVAL;
+    if (n < 0 || n > GVQ_I8_MAX_SUM / 2) return GVQ_EINVAL;
+    bool nothing;
+    int rc = look_at_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, nullptr, false, 2 * n, workspace);
+    if (rc == GVQ_OK)
+        rc = look_at_backward(nullptr, false, 2 * n, x, ld_x, dtype, rows, n_in, 2 * n, wt_codes, wt_scales, dx, dx_dtype, ld_dx, dw, dw_dtype, ld_dw,
+                              workspace, &nothing);
+    if (rc != GVQ_OK || nothing) return rc;
     Pieces p{(char*)workspace};
-    char* dg = rows > 0 && n > 0 ? p.take(8 * rows * n) : (char*)workspace;
-    int rc = gvq_i8_gated_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, dg, 2 * n, p.at, stream);
+    void* dg = rows > 0 && n > 0 ? p.take(8 * rows * n) : nullptr;
+    rc = gvq_i8_gated_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, dg, 2 * n, p.at, stream);
     if (rc != GVQ_OK) return rc;
     return gvq_i8_linear_backward(dg, 2 * n, x, ld_x, dtype, rows, n_in, 2 * n, wt_codes, wt_scales, dx, dx_dtype, ld_dx, dw, dw_dtype, ld_dw,
                                   accumulate, p.at, stream);
