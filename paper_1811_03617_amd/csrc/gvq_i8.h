@@ -24,6 +24,7 @@ struct I8QuantArgs {
     int64_t ldc, ldct;               // filled in by the launcher, as are:
     int64_t chunk_rows;
     int words, chunks;
+    int past;                        // past the caches
     int row_blocks;                  // work-groups that the rows take,
     int stripes, peak_blocks;        // that the columns' largest magnitudes take, side by side and in all,
     int across, column_blocks, band; // and the columns' codes, swept so many tiles down at a time

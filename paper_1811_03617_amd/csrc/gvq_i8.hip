@@ -77,6 +77,13 @@ __device__ __forceinline__ void i8_rows(const I8QuantArgs& a, int block, unsigne
 
 // ---- columns ------------------------------------------------------------------------------------------------------
 
+// 16 bytes, past the caches or through them.
+template <bool PAST>
+__device__ __forceinline__ u4 i8_word(const void* p)
+{
+    if constexpr (PAST) return stream_load((const u4*)p);
+    else return *(const u4*)p;
+}
 __device__ __forceinline__ void i8_raise(unsigned int& top, unsigned int u) { top = u > top ? u : top; }
 template <typename T>
 __device__ __forceinline__ void i8_raise_word(unsigned int (&top)[16 / sizeof(T)], const u4& v)
@@ -109,13 +116,17 @@ __device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsign
         const T* x = (const T*)a.x + c;
         if (a.words && c + PER <= a.cols) {
             int64_t r = r0 + wave;
-            for (; r + 28 < r1; r += 32) {
-                u4 v[8];
+            auto eight = [&](auto past) {
+                for (; r + 28 < r1; r += 32) {
+                    u4 v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = *(const u4*)(x + (r + 4 * i) * a.ld);
+                    for (int i = 0; i < 8; ++i) v[i] = i8_word<decltype(past)::value>(x + (r + 4 * i) * a.ld);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) i8_raise_word<T>(top, v[i]);
-            }
+                    for (int i = 0; i < 8; ++i) i8_raise_word<T>(top, v[i]);
+                }
+            };
+            if (a.past) eight(std::true_type{});
+            else eight(std::false_type{});
             for (; r < r1; r += 4) i8_raise_word<T>(top, *(const u4*)(x + r * a.ld));
         } else {
             for (int64_t r = r0 + wave; r < r1; r += 4)
@@ -140,15 +151,15 @@ __device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsign
     }
 }
 
+template <typename T>
+constexpr int I8_COLUMNS = 256 / sizeof(T);   // of a tile
 // 128 rows of 256 bytes: a thread takes four rows of one word of columns, packs each column's four codes, and the tile leaves as
 // 128 bytes of each column.  In LDS a column is eight pieces of 16 bytes, exchanged by the column's group of eight.
-template <typename T>
-__device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
+template <typename T, bool PAST>
+__device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block, unsigned int* turn, unsigned int* tops)
 {
-    constexpr int PER = 16 / sizeof(T), COLS = 16 * PER, QUADS = I8Q_THREADS / 16, TURNS = 32 / QUADS;   // quads of rows at a time
+    constexpr int PER = 16 / sizeof(T), COLS = I8_COLUMNS<T>, QUADS = I8Q_THREADS / 16, TURNS = 32 / QUADS;   // quads of rows at a time
     constexpr int PARTS = I8Q_THREADS / COLS;   // threads that look for one column's largest magnitude
-    __shared__ __attribute__((aligned(16))) unsigned int turn[COLS * 32];
-    __shared__ unsigned int tops[PARTS][COLS];
     int down, over;
     tile_at(block, (int)(a.ldct >> 7), a.across, a.band, down, over);
     const int64_t r0 = (int64_t)down * 128, c0 = (int64_t)over * COLS;
@@ -166,7 +177,7 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
             u4 v = {0u, 0u, 0u, 0u};
             if (r < a.rows) {
                 if (whole) {
-                    v = *(const u4*)(x + r * a.ld);
+                    v = i8_word<PAST>(x + r * a.ld);
                 } else {
 #pragma unroll
                     for (int i = 0; i < PER; ++i)
@@ -186,7 +197,7 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
             for (int k = 0; k < I8_CHUNKS / PARTS; ++k)
                 if (first + PARTS * k < a.chunks) i8_raise(top, a.peaks[(int64_t)(first + PARTS * k) * a.cols + c0 + col]);
         }
-        tops[first][col] = top;
+        tops[first * COLS + col] = top;
     }
     __syncthreads();
     float up[PER];
@@ -194,9 +205,9 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int col = w * PER + i;
-        unsigned int top = tops[0][col];
+        unsigned int top = tops[col];
 #pragma unroll
-        for (int k = 1; k < PARTS; ++k) i8_raise(top, tops[k][col]);
+        for (int k = 1; k < PARTS; ++k) i8_raise(top, tops[k * COLS + col]);
         const I8Scale s = i8_scale(top);
         up[i] = s.up;
         keep[i] = top >= 0x7f800000u ? 0u : ~0u;
@@ -221,10 +232,19 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block)
 #pragma unroll
     for (int p = 0; p < COLS / 32; ++p) {
         const int e = threadIdx.x + p * I8Q_THREADS, col = e >> 3, piece = e & 7;
-        if (c0 + col < a.cols)
-            *(u4*)(a.codes_t + (c0 + col) * a.ldct + r0 + 16 * piece) = *(const u4*)(turn + col * 32 + ((piece ^ (col >> 3 & 7)) << 2));
+        u4* to = (u4*)(a.codes_t + (c0 + col) * a.ldct + r0 + 16 * piece);
+        const u4 v = *(const u4*)(turn + col * 32 + ((piece ^ (col >> 3 & 7)) << 2));
+        if (c0 + col < a.cols) {
+            if constexpr (PAST) stream_store(to, v);
+            else *to = v;
+        }
     }
 }
+
+// Columns read their matrix twice.  What is larger than this goes past the caches both times (4096 x 25088 bf16 numbers that no cache
+// holds: largest magnitudes 35 us and codes 72, through the caches 77 and 73), what is smaller is found there the second time (of 500 x 1000 and
+// 500 x 4096 fp32 numbers a layer's gradients take 28 us past them, 26 through them).
+#define I8_PAST (64 << 20)
 
 // ---- one or two matrices --------------------------------------------------------------------------------------------
 
@@ -255,12 +275,14 @@ __global__ __launch_bounds__(I8Q_THREADS) void i8_rows_kernel(I8Two m)
     }
 }
 // Then the columns' codes.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(I8Q_THREADS) void i8_columns_kernel(I8Two m)
 {
+    __shared__ __attribute__((aligned(16))) unsigned int turn[I8_COLUMNS<T> * 32];
+    __shared__ unsigned int tops[I8Q_THREADS];
     const int block = tile_of_block(blockIdx.x, gridDim.x);
-    if (block < m.a[0].column_blocks) i8_columns_of<T>(m.a[0], block);
-    else i8_columns_of<T>(m.a[1], block - m.a[0].column_blocks);
+    if (block < m.a[0].column_blocks) i8_columns_of<T, PAST>(m.a[0], block, turn, tops);
+    else i8_columns_of<T, PAST>(m.a[1], block - m.a[0].column_blocks, turn, tops);
 }
 
 // ---- back ---------------------------------------------------------------------------------------------------------
@@ -287,7 +309,7 @@ static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
     constexpr int PER = 16 / sizeof(T);
     I8Two m{};
     int64_t first = 0, second = 0;
-    bool longer = false;
+    bool longer = false, past = false;
     for (int i = 0; i < n; ++i) {
         I8QuantArgs& a = m.a[i];
         a = matrices[i];
@@ -303,7 +325,8 @@ static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
             a.chunks = (int)((a.rows + a.chunk_rows - 1) / a.chunk_rows);
             a.stripes = (int)((a.cols + 64 * PER - 1) / (64 * PER));
             a.peak_blocks = a.stripes * a.chunks;
-            a.across = (int)((a.cols + 16 * PER - 1) / (16 * PER));
+            a.across = (int)((a.cols + I8_COLUMNS<T> - 1) / I8_COLUMNS<T>);
+            past |= a.rows * a.cols * (int64_t)sizeof(T) > I8_PAST;
             const int64_t tiles = a.across * (a.ldct >> 7);
             if (tiles > 0x3fffffff) return GVQ_EINVAL;
             a.column_blocks = (int)tiles;
@@ -312,12 +335,14 @@ static int launch_quantize(const I8QuantArgs* matrices, int n, hipStream_t st)
         first += a.row_blocks + a.peak_blocks;
         second += a.column_blocks;
     }
+    for (I8QuantArgs& a : m.a) a.past = past;
     // rows of up to 16384 numbers stay in registers; the shorter ones' kernel has half of those, and more waves
     if (longer) hipLaunchKernelGGL((i8_rows_kernel<T, 8>), dim3((unsigned)first), dim3(I8Q_THREADS), 0, st, m);
     else hipLaunchKernelGGL((i8_rows_kernel<T, 4>), dim3((unsigned)first), dim3(I8Q_THREADS), 0, st, m);
     GVQ_HIP(hipGetLastError());
     if (second > 0) {
-        hipLaunchKernelGGL((i8_columns_kernel<T>), dim3((unsigned)second), dim3(I8Q_THREADS), 0, st, m);
+        if (past) hipLaunchKernelGGL((i8_columns_kernel<T, true>), dim3((unsigned)second), dim3(I8Q_THREADS), 0, st, m);
+        else hipLaunchKernelGGL((i8_columns_kernel<T, false>), dim3((unsigned)second), dim3(I8Q_THREADS), 0, st, m);
         GVQ_HIP(hipGetLastError());
     }
     return GVQ_OK;

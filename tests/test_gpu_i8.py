@@ -180,6 +180,18 @@ def test_gradients_against_differences(i8):
     assert (np.abs(_np(dx) - cv @ wv) <= room + 1e-5).all()
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(4097, 8200, BF16), (2100, 8193, F32), (131, 140000, F32)])
+def test_columns_of_what_no_cache_holds(i8, rows, cols, dtype):
+    """Over 64 MB, where both passes go past the caches: rows of whole words and not."""
+    x = (torch.randn(rows, cols, device=DEV) * torch.exp(torch.randn(cols, device=DEV))).to(dtype)
+    m = x.float().abs().amax(0)
+    most = torch.full_like(m, 127.0)
+    q = i8.quantize_columns(x)
+    assert torch.equal(q.scales, m / most)
+    assert torch.equal(q.codes[:, :rows].double(), torch.round(x.t().double() * (most / m).double()[:, None]))
+    assert not q.codes[:, rows:].any()
+
+
 def test_sizes_of_zero(i8):
     w = i8.quantize(torch.randn(6, 10, device=DEV))
     assert i8.linear(torch.empty(0, 10, device=DEV), w).shape == (0, 6)
