@@ -77,6 +77,9 @@ __device__ __forceinline__ void i8_rows(const I8QuantArgs& a, int block, unsigne
 
 // ---- columns ------------------------------------------------------------------------------------------------------
 
+// A number's bits as fp32 has them.
+__device__ __forceinline__ unsigned int i8_bits(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ unsigned int i8_bits(unsigned short v) { return (unsigned int)v << 16; }
 // 16 bytes, past the caches or through them.
 template <bool PAST>
 __device__ __forceinline__ u4 i8_word(const void* p)
@@ -105,17 +108,17 @@ template <typename T>
 __device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsigned int* part)
 {
     constexpr int PER = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int stripe = block % a.stripes, chunk = block / a.stripes;
     const int64_t c = ((int64_t)stripe * 64 + lane) * PER, r0 = (int64_t)chunk * a.chunk_rows;
     const int64_t r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
     unsigned int top[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) top[i] = 0;
-    if (c < a.cols) {
+    if (a.words) {
         const T* x = (const T*)a.x + c;
-        if (a.words && c + PER <= a.cols) {
-            int64_t r = r0 + wave;
+        int64_t r = r0 + wave;
+        if (c + PER <= a.cols) {
             auto eight = [&](auto past) {
                 for (; r + 28 < r1; r += 32) {
                     u4 v[8];
@@ -128,18 +131,29 @@ __device__ __forceinline__ void i8_peaks(const I8QuantArgs& a, int block, unsign
             if (a.past) eight(std::true_type{});
             else eight(std::false_type{});
             for (; r < r1; r += 4) i8_raise_word<T>(top, *(const u4*)(x + r * a.ld));
-        } else {
-            for (int64_t r = r0 + wave; r < r1; r += 4)
+        } else if (c < a.cols) {
+            for (; r < r1; r += 4)
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
-                    if (c + i < a.cols) {
-                        if constexpr (sizeof(T) == 4) i8_raise(top[i], __float_as_uint(x[r * a.ld + i]) & 0x7fffffffu);
-                        else i8_raise(top[i], ((unsigned int)x[r * a.ld + i] & 0x7fffu) << 16);
-                    }
+                    if (c + i < a.cols) i8_raise(top[i], i8_bits(x[r * a.ld + i]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) part[(wave * 64 + lane) * (PER + 1) + i] = top[i];
+    } else {
+        // rows that start anywhere: a lane has one number of each 64, next to its neighbours'
+        const int first = stripe * 64 * PER + lane, last = (int)a.cols - 1;
+#pragma unroll 2
+        for (int64_t r = r0 + wave; r < r1; r += 4) {
+            const T* x = (const T*)a.x + r * a.ld;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) i8_raise(top[i], i8_bits(x[first + 64 * i < last ? first + 64 * i : last]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = 64 * i + lane;
+            part[(wave * 64 + e / PER) * (PER + 1) + e % PER] = top[i];
         }
     }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) part[(wave * 64 + lane) * (PER + 1) + i] = top[i];
     __syncthreads();
     for (int e = threadIdx.x; e < 64 * PER; e += I8Q_THREADS) {
         const int64_t cc = (int64_t)stripe * 64 * PER + e;
@@ -175,16 +189,16 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block, u
         for (int k = 0; k < 4; ++k) {
             const int64_t r = r0 + 4 * (quad0 + p * QUADS) + k;
             u4 v = {0u, 0u, 0u, 0u};
-            if (r < a.rows) {
-                if (whole) {
-                    v = i8_word<PAST>(x + r * a.ld);
-                } else {
+            if (whole) {
+                if (r < a.rows) v = i8_word<PAST>(x + r * a.ld);
+            } else {
+                // (from addresses that are always there, so that none of these loads waits for another)
+                const T* p = (const T*)a.x + (r < a.rows ? r : a.rows - 1) * a.ld;
 #pragma unroll
-                    for (int i = 0; i < PER; ++i)
-                        if (c + i < a.cols) {
-                            if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(x[r * a.ld + i]);
-                            else v[i >> 1] |= (unsigned int)x[r * a.ld + i] << (16 * (i & 1));
-                        }
+                for (int i = 0; i < PER; ++i) {
+                    const unsigned int u = i8_bits(p[c + i < a.cols ? c + i : a.cols - 1]), in = r < a.rows && c + i < a.cols ? u : 0u;
+                    if constexpr (sizeof(T) == 4) v[i] = in;
+                    else v[i >> 1] |= i & 1 ? in : in >> 16;
                 }
             }
             word[p][k] = v;

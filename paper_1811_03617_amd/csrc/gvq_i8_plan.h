@@ -4,22 +4,23 @@
 
 // A way's time: rounds over 256 compute units, of up to `share` work-groups a unit; each round has a start and so much a step (128 numbers
 // of the sum), more for every work-group that shares the unit.  Fitted to 263 products (17 to 4096 rows, 256 to 25088 columns, sums of 384 to
-// 16384) that were each measured in all ways: what is picked is 1.6 % behind the fastest on average, 39 % at most (two of them; six in a
-// hundred more than 10 %).  Tiles of 128 x 128 by eight waves with four stages, and of 128 x 64, were never more than 0.7 % better on average and
-// are not built.
+// 16384) that were each measured in all ways: what is picked is 1.2 % behind the fastest on average, four in a hundred more than 10 %, one 44 %.
+// Without the tiles whose sums two or four teams share the fastest of the others is 9 % behind on average; 64 x 64 with more stages, 128 x 128 with two
+// teams and 128 x 64 with three would add 0.4 % and are not built.
 struct I8Way {
     int rows, cols;   // of the result a work-group takes
     double call_us, start_us, step_us, more_us;
     int share;
 };
-enum { I8_FEW_16, I8_FEW_32, I8_TILE_64, I8_TILE_64_DEEP, I8_TILE_128, I8_TILE_256, I8_WAYS };
+enum { I8_FEW_16, I8_FEW_32, I8_TILE_64, I8_TILE_64_TWO, I8_TILE_64_FOUR, I8_TILE_128, I8_TILE_256, I8_WAYS };
 static const I8Way i8_ways[I8_WAYS] = {
-    {16, 16, 2.40, 0.96, 0.107, 0.109, 2},   // straight from memory, 16 rows of the first operand, and 32
-    {32, 16, 2.37, 1.03, 0.149, 0.170, 2},
-    {64, 64, 1.05, 2.74, 0.318, 0.165, 5},   // two stages, and four
-    {64, 64, 1.86, 2.17, 0.279, 0.118, 2},
-    {128, 128, 1.69, 4.31, 0.576, 0.408, 2},
-    {256, 256, 0.00, 9.21, 1.076, 0.0, 1},
+    {16, 16, 2.45, 0.96, 0.107, 0.110, 2},   // straight from memory, 16 rows of the first operand, and 32
+    {32, 16, 2.42, 1.02, 0.149, 0.169, 2},
+    {64, 64, 1.16, 2.77, 0.346, 0.152, 5},   // one team, two, four
+    {64, 64, 1.83, 2.68, 0.246, 0.133, 2},
+    {64, 64, 1.30, 3.84, 0.207, 0.0, 1},
+    {128, 128, 1.73, 4.47, 0.580, 0.369, 2},
+    {256, 256, 0.00, 9.49, 1.105, 0.0, 1},
 };
 
 // `groups` work-groups over `steps` steps each (on average).

@@ -10,13 +10,16 @@
 
 // BM rows of A by BN of B, WM x WN waves.  A step's rows lie in LDS one behind the other, row r's piece c of 16 bytes in place
 // c ^ (r & 7): the 16 lanes whose reads are served together then cover all banks.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// PARTS: teams of WM x WN waves that take the steps in turn, each with stages of its own; their sums, whole numbers, are added at the end.  One team
+// alone on a compute unit waits for its barriers and reads most of the time.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int PARTS_ = 1>
 struct I8Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
-    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, MI = BM / WM / 16, NI = BN / WN / 16;
-    static constexpr int STAGE = (BM + BN) * I8_STEP, LDS = STAGE * STAGES;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, PARTS = PARTS_;
+    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES * PARTS, MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int STAGE = (BM + BN) * I8_STEP, LDS = STAGE * STAGES * PARTS;
     static constexpr int GROUPS = (BM + BN) / 8, COPIES = GROUPS / WAVES;   // 1 KB copies of a step: eight rows each
     static_assert(GROUPS % WAVES == 0 && BM % 16 == 0 && LDS <= 160 * 1024 && COPIES * STAGES < 64, "whole copies, LDS and vmcnt");
+    static_assert((PARTS - 1) * WAVES * MI * NI * 1024 <= LDS && WAVES * 4096 <= LDS, "the teams' sums, then the results");
 };
 
 // Row of B that the tile's row j is.  Gated: groups of 16 of the gate's and of the other's in turn.
@@ -31,12 +34,15 @@ __device__ __forceinline__ int64_t i8_row_of_b(int tn, int BN, int j, int n)
     return (int64_t)(r < n ? r : n - 1) + ((j >> 4) & 1 ? n : 0);
 }
 
+// The first team's waves return true, with the sums.
 template <typename T, I8Mode MODE>
-__device__ __forceinline__ void i8_tile(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[T::MI][T::NI])
+__device__ __forceinline__ bool i8_tile(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[T::MI][T::NI])
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int lane = threadIdx.x & 63, every = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), team = T::PARTS > 1 ? every / T::WAVES : 0,
+              wave = T::PARTS > 1 ? every % T::WAVES : every;
     const int wm = wave / T::WN, wn = wave % T::WN, steps = (int)(a.ldk / I8_STEP);
-    const unsigned int lds0 = lds_offset(lds);
+    char* mine = lds + team * T::STAGES * T::STAGE;
+    const unsigned int lds0 = lds_offset(mine);
     const char* base[T::COPIES];
     unsigned int voff[T::COPIES];
 #pragma unroll
@@ -53,19 +59,21 @@ __device__ __forceinline__ void i8_tile(const I8ProductArgs& a, int tm, int tn, 
             voff[i] = (unsigned int)((r - first) * a.ldk) + 16 * piece;
         }
     }
-    auto issue = [&](int s) {
-        const unsigned int to = lds0 + (unsigned int)(s % T::STAGES) * T::STAGE + (unsigned int)(wave * T::COPIES) * 1024;
+    // the team's turns: its t-th step is step t PARTS + team
+    auto issue = [&](int t) {
+        const unsigned int to = lds0 + (unsigned int)(t % T::STAGES) * T::STAGE + (unsigned int)(wave * T::COPIES) * 1024;
 #pragma unroll
-        for (int i = 0; i < T::COPIES; ++i) copy_rows_to_lds(base[i] + (int64_t)s * I8_STEP, voff[i], to + i * 1024);
+        for (int i = 0; i < T::COPIES; ++i) copy_rows_to_lds(base[i] + (int64_t)(t * T::PARTS + team) * I8_STEP, voff[i], to + i * 1024);
     };
-    const int row = lane & 15;
-    for (int s = 0; s < T::STAGES - 1 && s < steps; ++s) issue(s);
-    for (int s = 0; s < steps; ++s) {
-        // this wave's copies of step s have arrived, and then everybody's; everybody is done with the place that is asked for next
-        if (s + T::STAGES - 1 <= steps) tile_barrier<T::COPIES * (T::STAGES - 2)>();
+    const int row = lane & 15, turns = (steps + T::PARTS - 1) / T::PARTS, own = steps > team ? (steps - team + T::PARTS - 1) / T::PARTS : 0;
+    for (int t = 0; t < T::STAGES - 1 && t < own; ++t) issue(t);
+    for (int t = 0; t < turns; ++t) {
+        // this wave's copies of its step have arrived, and then everybody's; everybody is done with the place that is asked for next
+        if (t + T::STAGES - 1 <= own) tile_barrier<T::COPIES * (T::STAGES - 2)>();
         else tile_barrier<0>();
-        if (s + T::STAGES - 1 < steps) issue(s + T::STAGES - 1);
-        const char* st = lds + (s % T::STAGES) * T::STAGE;
+        if (t + T::STAGES - 1 < own) issue(t + T::STAGES - 1);
+        if (T::PARTS > 1 && t >= own) continue;
+        const char* st = mine + (t % T::STAGES) * T::STAGE;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int piece = ((4 * k + (lane >> 4)) ^ (row & 7)) * 16;
@@ -80,8 +88,25 @@ __device__ __forceinline__ void i8_tile(const I8ProductArgs& a, int tm, int tn, 
             }
         }
     }
+    if constexpr (T::PARTS > 1) {
+        i4v* sums = (i4v*)lds + lane;
+        __syncthreads();
+        if (team > 0)
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) sums[(((team - 1) * T::WAVES + wave) * T::MI * T::NI + mi * T::NI + ni) * 64] = acc[mi][ni];
+        __syncthreads();
+        if (team == 0)
+#pragma unroll
+            for (int p = 0; p < T::PARTS - 1; ++p)
+#pragma unroll
+                for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] += sums[((p * T::WAVES + wave) * T::MI * T::NI + mi * T::NI + ni) * 64];
+    }
+    return team == 0;
 }
-
 
 // 256 x 256 by eight waves in two halves that take turns: while the four of one half multiply, one on each SIMD, the four of the other
 // read fragments and ask for rows, and a barrier ends every turn of the two.  A step's products of a wave (128 x 64, 128 numbers of the
@@ -276,14 +301,17 @@ __device__ __forceinline__ void i8_hand_out(const char* w, OUT* out, int64_t ld,
 }
 
 template <typename T, I8Mode MODE>
-__device__ __forceinline__ void i8_sums(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[T::MI][T::NI])
+__device__ __forceinline__ bool i8_sums(const I8ProductArgs& a, int tm, int tn, char* lds, i4v (&acc)[T::MI][T::NI])
 {
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = i4v{0, 0, 0, 0};
+    bool first = true;
     if constexpr (std::is_same<T, I8Pong>::value) i8_tile_pong<MODE>(a, tm, tn, lds, acc);
-    else i8_tile<T, MODE>(a, tm, tn, lds, acc);
+    else first = i8_tile<T, MODE>(a, tm, tn, lds, acc);
+    __syncthreads();
+    return first;
 }
 
 template <typename T, I8Mode MODE, typename OUT>
@@ -301,7 +329,6 @@ __device__ __forceinline__ void i8_tile_out(const I8ProductArgs& a, int tm, int 
         typedef I8Hand<OUT, COLS> H;
         constexpr int AT = H::ROWS / 16;
         char* w = lds + wave * 4096;
-        __syncthreads();
         static_for<0, T::MI / AT>([&](auto turn) {
             constexpr int M = decltype(turn)::value * AT;
             f4 more[AT][NJ];
@@ -372,8 +399,7 @@ __global__ __launch_bounds__(T::THREADS) void i8_tile_kernel(I8ProductArgs a)
     int tm, tn;
     tile_at(tile_of_block(blockIdx.x, a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
     i4v acc[T::MI][T::NI];
-    i8_sums<T, MODE>(a, tm, tn, lds, acc);
-    i8_tile_out<T, MODE, OUT>(a, tm, tn, lds, acc);
+    if (i8_sums<T, MODE>(a, tm, tn, lds, acc)) i8_tile_out<T, MODE, OUT>(a, tm, tn, lds, acc);
 }
 
 // One plain product or two, whose tiles follow each other: the second's fill the round that the first's leave half empty.
@@ -389,7 +415,7 @@ __global__ __launch_bounds__(T::THREADS) void i8_pair_kernel(I8Pair p)
     int tm, tn;
     tile_at(tile_of_block(blockIdx.x - (second ? first : 0), a.nm * a.nn), a.nm, a.nn, a.band, tm, tn);
     i4v acc[T::MI][T::NI];
-    i8_sums<T, I8_PLAIN>(a, tm, tn, lds, acc);
+    if (!i8_sums<T, I8_PLAIN>(a, tm, tn, lds, acc)) return;
     if (a.bf16) i8_tile_out<T, I8_PLAIN, unsigned short>(a, tm, tn, lds, acc);
     else i8_tile_out<T, I8_PLAIN, float>(a, tm, tn, lds, acc);
 }
@@ -440,14 +466,16 @@ static int launch_pair(I8Pair p, hipStream_t st)
 }
 
 typedef I8Shape<64, 64, 2, 2, 2> I8Tile64;
-typedef I8Shape<64, 64, 2, 2, 4> I8Tile64Deep;
+typedef I8Shape<64, 64, 2, 2, 2, 2> I8Tile64Two;
+typedef I8Shape<64, 64, 2, 2, 2, 4> I8Tile64Four;
 typedef I8Shape<128, 128, 2, 2, 2> I8Tile128;
 
 static int launch_plain(const I8Pair& p, int way, hipStream_t st)
 {
     switch (way) {
     case I8_TILE_64: return launch_pair<I8Tile64>(p, st);
-    case I8_TILE_64_DEEP: return launch_pair<I8Tile64Deep>(p, st);
+    case I8_TILE_64_TWO: return launch_pair<I8Tile64Two>(p, st);
+    case I8_TILE_64_FOUR: return launch_pair<I8Tile64Four>(p, st);
     case I8_TILE_128: return launch_pair<I8Tile128>(p, st);
     default: return launch_pair<I8Pong>(p, st);
     }
@@ -457,7 +485,8 @@ static int launch_mode(const I8ProductArgs& a, int way, hipStream_t st)
 {
     switch (way) {
     case I8_TILE_64: return launch_tile<I8Tile64, MODE, OUT>(a, st);
-    case I8_TILE_64_DEEP: return launch_tile<I8Tile64Deep, MODE, OUT>(a, st);
+    case I8_TILE_64_TWO: return launch_tile<I8Tile64Two, MODE, OUT>(a, st);
+    case I8_TILE_64_FOUR: return launch_tile<I8Tile64Four, MODE, OUT>(a, st);
     case I8_TILE_128: return launch_tile<I8Tile128, MODE, OUT>(a, st);
     default: return launch_tile<I8Pong, MODE, OUT>(a, st);
     }

@@ -1,5 +1,5 @@
 """8-bit products through each of the ways they can take: straight from memory (16 or 32 rows a work-group, few of these in numbers) and tiles of
-four shapes; one product and two in one launch; plain, gated, and the gated block's inner gradient.
+three shapes, the smallest with sums of one team, two and four; one product and two in one launch; plain, gated, and the gated block's inner gradient.
 
 Whole numbers of up to 127 with 127 in every row: each scale is 1 and a sum is exact, so that a plain result is that sum rounded once.
 """
@@ -15,25 +15,28 @@ PLAIN = [
     (17, 300, 900), (9, 70, 12500), (40, 1000, 700),        # 16 rows a work-group
     (17, 4096, 4097), (77, 1000, 4096),                     # 32
     (500, 1001, 300), (100, 4099, 384), (129, 2500, 250),   # tiles: 64 x 64
-    (65, 4096, 16300), (300, 2500, 4096),                   # more stages
+    (50, 6801, 700), (80, 3409, 1500), (80, 3409, 129),     # their sums by two teams
+    (65, 4096, 16300), (300, 2500, 4096),                   # and by four
     (1000, 8190, 2000),                                     # 128 x 128
     (3000, 4097, 520), (2049, 8190, 1300),                  # 256 x 256
 ]
 GATED = [
     (17, 300, 900), (9, 70, 12500),
-    (17, 4096, 4097), (77, 1000, 4096),
+    (17, 3409, 300), (30, 3409, 700),
     (500, 1001, 300), (129, 2500, 250),
-    (300, 2500, 4096),
-    (100, 8895, 4500), (471, 2299, 4500),
+    (17, 6801, 700), (300, 2500, 4096),
+    (17, 4096, 4097), (77, 1000, 4096),
+    (444, 6801, 700), (293, 3409, 6300),
     (600, 8001, 1000), (2049, 4100, 130),
 ]
 # rows, columns in and out of a layer
 PAIRS = [
     (33, 130, 70), (300, 261, 140), (257, 100, 513),        # both gradients in one launch: 64 x 64
-    (1000, 1000, 1000),
+    (1000, 1000, 1000),                                     # two teams
+    (1521, 123, 3100), (1521, 70, 6300),                    # four
     (500, 4096, 1000),
     (2000, 3001, 2500),
-    (857, 1930, 7415),                                      # a launch each
+    (2286, 3409, 3100),                                     # a launch each
 ]
 
 
