@@ -191,7 +191,7 @@ __device__ __forceinline__ void i8_columns_of(const I8QuantArgs& a, int block, u
             u4 v = {0u, 0u, 0u, 0u};
             if (whole) {
                 if (r < a.rows) v = i8_word<PAST>(x + r * a.ld);
-            } else {
+            } else if (c < a.cols) {
                 // (from addresses that are always there, so that none of these loads waits for another)
                 const T* p = (const T*)a.x + (r < a.rows ? r : a.rows - 1) * a.ld;
 #pragma unroll
