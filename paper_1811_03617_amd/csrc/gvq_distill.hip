@@ -8,7 +8,8 @@
 // so that two rounds of joining are enough: the largest, then A, S and that sum.
 //
 // A row to a wave, to four or to sixteen; each thread keeps its first words of the row in registers and reads only the rest a second
-// time, for the gradient.  Bound: memory.
+// time, for the gradient.  Bound: memory, each logit in and out once: 4096 x 131072 bf16 445 us (4.8 TB/s, a plain copy's 5.1), the losses alone 179 (6.0);
+// 16384 x 4096 bf16 51; below that a launch and two joins, 2048 x 1000 fp32 7.6.
 #include "gvq_distill.h"
 
 // Eight neighbouring logits of a row, as they lie in memory.
@@ -389,17 +390,21 @@ static int launch_rows(const DistillArgs& a, hipStream_t st)
 
 #define DISTILL_TEAM 256   // of a piece
 
-// In place the second launch's work-groups read the student's logits at entries that another piece's have replaced: then rows stay whole.
+// Few rows of many logits leave most of the chip idle while each waits for its own loads; in pieces of at least 2048 they fill it, for a second
+// launch (whole and in pieces, us with the gradient: 1 x 32768 bf16 8.7 and 7.9, 16 x 50021 fp32 12.1 and 9.8, 1 x 131072 bf16 18.7 and 7.8,
+// 64 x 131072 20.1 and 13.1, 96 x 65536 13.4 and 13.0; but 1 x 20000 7.5 and 8.5, 64 x 32768 9.4 and 9.5, 96 x 50021 11.8 and 12.7, 112 x 131072
+// 20.5 and 21.4).  Pieces of at least 8192 instead: 1.5 us more for one row, nothing from 64 on.
 int gvq_distill_parts(int64_t rows, int64_t vocab)
 {
-    if (rows >= 128 || vocab < 65536) return 1;
-    const int64_t want = (512 + rows - 1) / rows, most = vocab / 8192 < DISTILL_TEAM ? vocab / 8192 : DISTILL_TEAM;   // (a thread each joins them)
+    if (rows > 96 || vocab < 32768 || vocab < 640 * rows) return 1;
+    const int64_t want = (512 + rows - 1) / rows, most = vocab / 2048 < DISTILL_TEAM ? vocab / 2048 : DISTILL_TEAM;   // (a thread each joins them)
     return (int)(want < most ? want : most);
 }
 
 template <typename T>
 static int launch_distill(const DistillArgs& a, float* sums, hipStream_t st)
 {
+    // in place the second launch's work-groups would read the student's logits at entries that another piece's have replaced: rows stay whole
     const int parts = a.grad == a.logits ? 1 : gvq_distill_parts(a.rows, a.vocab);
     if (parts > 1) {
         const unsigned lds = (unsigned)(12 * a.n_top);
@@ -411,8 +416,12 @@ static int launch_distill(const DistillArgs& a, float* sums, hipStream_t st)
         GVQ_HIP(hipGetLastError());
         return GVQ_OK;
     }
-    if (a.vocab <= 2048 && a.n_top <= 256) return launch_rows<T, 64, 4>(a, st);
-    if (a.vocab <= 8192) return launch_rows<T, 256, 4>(a, st);
+    // by a row's bytes.  A wave, four and sixteen of them (us with the gradient): 16384 x 1000 bf16 23, 37; 8192 x 2048 bf16 19, 23; 8192 x 2048 fp32
+    // 36, 30; 4096 x 8192 bf16 35, 28, 48; 8192 x 4096 fp32 77, 54, 81; 4096 x 16384 bf16 -, 50, 60; 4096 x 32000 bf16 -, 112, 107; 64 x 32000 -, 13,
+    // 9.2.  Many entries would take a wave's row too much LDS.
+    const int64_t bytes = (int64_t)a.vocab * (int64_t)sizeof(T);
+    if (bytes <= 4096 && a.n_top <= 256) return launch_rows<T, 64, sizeof(T) == 2 ? 4 : 2>(a, st);
+    if (bytes <= (a.rows >= 1024 ? 32768 : 16384)) return launch_rows<T, 256, 4>(a, st);
     return launch_rows<T, 1024, sizeof(T) == 2 ? 6 : 3>(a, st);
 }
 

@@ -198,6 +198,6 @@ __device__ __forceinline__ void i8_finish(const I8ProductArgs& a, OUT* out, int 
 // Products of few rows without LDS tiles (gvq_i8_few.hip): of `tiles` times 16 rows of codes a work-group, or of at most four rows of numbers,
 // quantised on the way.
 int gvq_launch_i8_few(const I8ProductArgs& a, int tiles, I8Mode mode, gvq_dtype_t dtype, hipStream_t st);
-bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k, I8Mode mode);
+bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t k, I8Mode mode);
 int gvq_launch_i8_few_numbers(I8ProductArgs a, const void* x, gvq_dtype_t x_dtype, int64_t ld_x, int64_t k, I8Mode mode, gvq_dtype_t dtype,
                               hipStream_t st);

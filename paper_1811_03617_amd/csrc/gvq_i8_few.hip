@@ -5,6 +5,8 @@
 // straight into registers: row lane % 16, 16 bytes of 64.  The waves' sums are whole numbers and are added exactly.  Up to four rows of x
 // are quantised by every work-group for itself, into LDS, while the first turns of W are on their way: that costs it one read of x from the
 // caches and saves a launch.  More rows come in codes, 16 or 32 to a work-group.
+// Bound: memory, W once; what a compute unit can have on its way (about 29 bytes a ns) and the latency at both ends for small ones.  One bf16 row through
+// 4096 x 25088 20.2 us (5.1 TB/s of W), through 25088 x 4096 23, through 4096 x 4096 6.2; gated 2 x 8192 x 4096 19; codes of 16 rows through 4096 x 4096 7.1.
 #include "gvq_i8.h"
 #include "gvq_tile.h"
 
@@ -316,7 +318,7 @@ int gvq_launch_i8_few(const I8ProductArgs& a, int tiles, I8Mode mode, gvq_dtype_
                             : mode == I8_GATED ? launch_codes<I8_GATED, float>(a, tiles, st) : launch_codes<I8_INNER, float>(a, tiles, st);
 }
 
-#define I8_FOUR_LDS (64 * 1024)   // of codes
+#define I8_FOUR_LDS (64 * 1024)   // of codes, beside 64 KB of sums
 
 template <typename X, I8Mode MODE, typename OUT, int ROWS>
 static int launch_numbers(const I8ProductArgs& a, const void* x, int64_t ld_x, int k, hipStream_t st)
@@ -347,7 +349,10 @@ static int launch_numbers_mode(const I8ProductArgs& a, const void* x, int64_t ld
     return mode == I8_PLAIN ? launch_rows<X, I8_PLAIN, OUT>(a, x, ld_x, k, st) : launch_rows<X, I8_GATED, OUT>(a, x, ld_x, k, st);
 }
 
-bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t n, int64_t k, I8Mode mode)
+// Against a launch that quantises and another that multiplies (us, one and four bf16 rows): 1000 x 1000 4.1 and 6.2, 4.4 and 6.4; 4096 x 4096 6.2 and 9.4,
+// 6.9 and 10.2; 4096 x 25088 20 and 29, 30 and 31; gated 8192 x 4096 19 and 24, 20 and 25; at worst 25088 x 4096 23 and 22, 24 and 22, where each unit goes
+// through many groups.  At most 64 KB of codes: LDS has to hold them beside as much of sums.
+bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t k, I8Mode mode)
 {
     const int64_t row = rows > 1 ? ld_x * (x_dtype == GVQ_BF16 ? 2 : 4) : 0;   // a single row is aligned where it begins
     if (rows > 4 || mode == I8_INNER || (((uintptr_t)x | (uintptr_t)row) & 15) != 0) return false;

@@ -140,7 +140,7 @@ static int forward(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
     I8ProductArgs a = product(q.codes, q.scales, w_codes, w_scales, rows, n_out, n_in, y, ld_y, false);
     a.activation = activation;
     if (n_in > 0) {
-        if (gvq_i8_few_numbers_takes(x, dtype, rows, ld_x, n_out, n_in, mode))
+        if (gvq_i8_few_numbers_takes(x, dtype, rows, ld_x, n_in, mode))
             return gvq_launch_i8_few_numbers(a, x, dtype, ld_x, n_in, mode, y_dtype, (hipStream_t)stream);
         const int rc = quantize(x, dtype, rows, n_in, ld_x, q, Codes{nullptr, nullptr}, nullptr, stream);
         if (rc != GVQ_OK) return rc;

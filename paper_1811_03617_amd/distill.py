@@ -3,8 +3,9 @@
     losses, dlogits = distill.loss_and_gradient(logits, top, index, temperature=2.0, weight=weight)
 
 For every row, with p = softmax(top / t) over the row's entries and q = softmax(logits / t) over all of the row:
-loss = w t^2 sum_j p_j (log p_j - log q[index_j]), gradient = w t (q - p at its places).  Everything runs on the device's current
-stream.  No call records a gradient: `loss` refuses logits that need one, `loss_and_gradient` gives it.
+loss = w t^2 sum_j p_j (log p_j - log q[index_j]), gradient = w t (q - p at its places); t is from 0.001 to 1000.  Everything runs on
+the device's current stream.  No call records a gradient: `loss` refuses logits that need one, `loss_and_gradient` gives it; what the teacher's
+logits or the weights would need is refused by both.
 """
 import torch
 
@@ -13,6 +14,9 @@ from .mx import _check, _matrix, _device, _no_graph, _now, _size
 
 
 def _run(logits, top, index, temperature, weight, grad, want):
+    _no_graph(top, "top")
+    if weight is not None:
+        _no_graph(weight, "weight")
     code, ld, rows, vocab = _matrix(logits, "logits")
     code_top, ld_top, rows_top, n = _matrix(top, "top")
     if rows_top != rows or tuple(index.shape) != (rows, n) or index.dtype is not torch.int64 or index.get_device() != _device():

@@ -54,7 +54,8 @@ def _check(got, z, a, index, t, w, dtype):
     assert (np.abs(_np(grad) - want_grad) <= room + last * (np.abs(want_grad) + room) + 2.0 ** -125).all()
 
 
-SIZES = [(1, 1, 1), (3, 5, 2), (2, 64, 64), (5, 1000, 8), (7, 1001, 17), (2, 8193, 5), (3, 50021, 16), (1, 140000, 100), (33, 4096, 1), (300, 70, 3), (600, 9, 2)]
+SIZES = [(1, 1, 1), (3, 5, 2), (2, 64, 64), (5, 1000, 8), (7, 1001, 17), (2, 8193, 5), (3, 50021, 16), (1, 140000, 100), (33, 4096, 1), (300, 70, 3), (600, 9, 2),
+         (1030, 9001, 4), (97, 33000, 5), (9, 1025, 300)]
 
 
 @pytest.mark.parametrize("rows,vocab,n", SIZES)
@@ -77,7 +78,7 @@ def test_the_teacher_s_type_is_its_own(distill):
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
 
 
-@pytest.mark.parametrize("rows,vocab", [(40, 1000), (6, 30011)])
+@pytest.mark.parametrize("rows,vocab", [(40, 1000), (6, 30011), (6, 66001)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_and_entries_that_are_not_there(distill, rows, vocab, dtype):
     z, a, index, w = _case(rows, vocab, 12, dtype)
@@ -102,7 +103,7 @@ def test_rows_and_entries_that_are_not_there(distill, rows, vocab, dtype):
     assert torch.equal(distill.loss(z, a, index, temperature=2.0, weight=w), got[0])
 
 
-@pytest.mark.parametrize("vocab", [40, 9001])
+@pytest.mark.parametrize("vocab", [40, 9001, 66001])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_logits_that_are_masked(distill, vocab, dtype):
     z, a, index, w = _case(8, vocab, 3, dtype)
@@ -148,6 +149,22 @@ def test_strides_windows_and_in_place(distill, rows, vocab, dtype):
     assert torch.isnan(big[:, :3]).all() and torch.isnan(big[:, 3 + vocab:]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_in_pieces_by_windows_and_in_place(distill, dtype):
+    rows, vocab = 5, 70001
+    z, a, index, w = (v.to(DEV) for v in _case(rows, vocab, 6, dtype))
+    index[0] = torch.tensor([0, vocab - 1, 35000, 35000, 8, 7])
+    big = torch.full((rows, vocab + 7), float("nan"), dtype=dtype, device=DEV)
+    big[:, 3:3 + vocab] = z
+    window = big[:, 3:3 + vocab]
+    for out in (None, torch.full((rows, vocab + 5), 7.0, dtype=dtype, device=DEV)[:, 1:1 + vocab], window):
+        _check(distill.loss_and_gradient(window, a, index, weight=w, out=out), z, a, index, 1.0, w, dtype)
+        if out is not None and out is not window:
+            edges = torch.as_strided(out, (rows, vocab + 5), (vocab + 5, 1), 0)
+            assert (edges[:, 0] == 7).all() and (edges[:, 1 + vocab:] == 7).all()
+    assert torch.isnan(big[:, :3]).all() and torch.isnan(big[:, 3 + vocab:]).all()
+
+
 @pytest.mark.parametrize("vocab", [50, 9000])
 def test_the_gradient_against_differences(distill, vocab):
     z, a, index, w = _case(4, vocab, 5, F32)
@@ -185,6 +202,8 @@ def test_refusals(distill):
     for call in (lambda: distill.loss(z, a, index.int()), lambda: distill.loss(z, a[:, :2], index), lambda: distill.loss(z, a[:3], index[:3]),
                  lambda: distill.loss(z, a, index, weight=w[:3]), lambda: distill.loss(z, a, index, weight=w.double()),
                  lambda: distill.loss(z, a, index.cpu()), lambda: distill.loss(z.clone().requires_grad_(), a, index),
+                 lambda: distill.loss(z, a.clone().requires_grad_(), index), lambda: distill.loss(z, a, index, weight=w.clone().requires_grad_()),
+                 lambda: distill.loss_and_gradient(z, a.clone().requires_grad_(), index),
                  lambda: distill.loss(z.t(), a, index), lambda: distill.loss(z, a, index.t().contiguous().t()),
                  lambda: distill.loss_and_gradient(z, a, index, out=torch.empty(4, 49, device=DEV)),
                  lambda: distill.loss_and_gradient(z, a, index, out=torch.empty(4, 50, device=DEV, dtype=BF16))):
