@@ -391,12 +391,13 @@ static int launch_rows(const DistillArgs& a, hipStream_t st)
 #define DISTILL_TEAM 256   // of a piece
 
 // Few rows of many logits leave most of the chip idle while each waits for its own loads; in pieces of at least 2048 they fill it, for a second
-// launch (whole and in pieces, us with the gradient: 1 x 32768 bf16 8.7 and 7.9, 16 x 50021 fp32 12.1 and 9.8, 1 x 131072 bf16 18.7 and 7.8,
-// 64 x 131072 20.1 and 13.1, 96 x 65536 13.4 and 13.0; but 1 x 20000 7.5 and 8.5, 64 x 32768 9.4 and 9.5, 96 x 50021 11.8 and 12.7, 112 x 131072
-// 20.5 and 21.4).  Pieces of at least 8192 instead: 1.5 us more for one row, nothing from 64 on.
+// launch (whole and in pieces, us with the gradient: 1 x 65536 bf16 12.1 and 7.9, 1 x 131072 18.7 and 7.8, 64 x 131072 20.1 and 13.1, 96 x 65536 13.4 and
+// 13.0, 96 x 262144 39 and 35; 112 x 131072 20.5 and 21.4).  That launch and its workspace are 4 us of the host's time: 16 x 50021 fp32 takes
+// 12.1 whole and 9.8 in pieces, but 11.3 and 14.5 where Python makes one call after the other, so that shorter rows stay whole.  Pieces of at least 8192
+// instead: 1.5 us more for one row, nothing from 64 on.
 int gvq_distill_parts(int64_t rows, int64_t vocab)
 {
-    if (rows > 96 || vocab < 32768 || vocab < 640 * rows) return 1;
+    if (rows > 96 || vocab < 65536) return 1;
     const int64_t want = (512 + rows - 1) / rows, most = vocab / 2048 < DISTILL_TEAM ? vocab / 2048 : DISTILL_TEAM;   // (a thread each joins them)
     return (int)(want < most ? want : most);
 }

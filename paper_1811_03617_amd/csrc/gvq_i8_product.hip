@@ -125,7 +125,9 @@ __device__ __forceinline__ bool i8_tile(const I8ProductArgs& a, int tm, int tn, 
 //   3               F (s + 1)    A1 (s + 2)   A1 F
 // Five quarters, ten copies of a wave, are younger than the one that the next turn reads.
 // Tried: work-groups that stay and ask for the next tile while they hand out the last one (no faster, and gated ones spill), reads spread over both turns of
-// a pair (2 % slower), a turn's last products behind the barrier (8 to 17 % slower), all eight waves in step (no room for the reads ahead).
+// a pair (2 % slower), a turn's last products behind the barrier (8 to 17 % slower), all eight waves in step (no room for the reads ahead), and
+// four waves of 128 x 128 each, one on a SIMD, that read a third less from LDS: 4096 x 4096 x 16384 203 us instead of 182, as fast as this one only without
+// copies (163 both), which then hold up the one wave that multiplies.
 struct I8Pong {
     static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, WAVES = 8, THREADS = 512, MI = 8, NI = 4;
     static constexpr int STAGE = 512 * I8_STEP, LDS = 2 * STAGE;

@@ -61,8 +61,8 @@ def test_workspaces_hold_what_a_call_needs(rows, n_in, n_out):
 
 
 def test_the_loss_s_workspace_is_for_few_rows_of_many_logits():
-    assert gvq.gvq_distill_workspace(4096, 131072, 64) == 0 and gvq.gvq_distill_workspace(64, 32768, 16) == 0
-    for rows, vocab in ((1, 32768), (1, 1 << 22), (16, 50021), (96, 262144)):
+    assert gvq.gvq_distill_workspace(4096, 131072, 64) == 0 and gvq.gvq_distill_workspace(16, 50021, 16) == 0 and gvq.gvq_distill_workspace(97, 131072, 16) == 0
+    for rows, vocab in ((1, 65536), (1, 1 << 22), (16, 131072), (96, 262144)):
         n = gvq.gvq_distill_workspace(rows, vocab, 64)
         assert 0 < n <= 8 * rows * 256 + 256      # a thread of 256 joins each piece's two numbers
 
