@@ -66,6 +66,30 @@ def test_rows_that_start_anywhere(i8, dtype, first, more):
     _same_matrix(i8.quantize_columns(x), ref.integers(want.T), cols, rows)
 
 
+@pytest.mark.parametrize("rows", [255, 256, 257, 511, 512, 513, 1023, 1024, 1025])
+@pytest.mark.parametrize("cols,first", [(77, 0), (264, 0), (2049, 0), (300, 1)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_columns_of_few_and_of_many_rows(i8, rows, cols, first, dtype):
+    gen = torch.Generator().manual_seed(rows + cols)
+    x = torch.randn(rows, cols + 3, generator=gen).to(dtype)
+    x[rows - 1, first] = float("inf")
+    x[0, cols // 2] = float("nan")
+    x[:, first + 2] = 0
+    x = x.to(DEV)[:, first:first + cols]
+    q, t = i8.quantize_both(x)
+    want = ref.integers(_np(x).T)
+    _same_matrix(q, ref.integers(_np(x)), rows, cols)
+    _same_matrix(t, want, cols, rows)
+    _same_matrix(i8.quantize_columns(x), want, cols, rows)
+
+
+def test_columns_of_1024_rows_that_are_too_many_for_one_launch(i8):
+    x = torch.randn(1024, 8200, generator=torch.Generator().manual_seed(5)).to(DEV)
+    want = ref.integers(_np(x).T)
+    _same_matrix(i8.quantize_columns(x), want, 8200, 1024)
+    _same_matrix(i8.quantize_columns(x[:, :8192].contiguous()), tuple(v[:8192] for v in want), 8192, 1024)
+
+
 @pytest.mark.parametrize("scale", [1.0, 2.0 ** -20, 2.0 ** 100, 127.0 / 254])
 def test_halves_go_to_the_even_integer(i8, scale):
     """Numbers half way between two integers, every one of them, and their neighbours on both sides."""
