@@ -410,8 +410,9 @@ int gvq_i8_gated_backward(const void* dh, int64_t ld_dh, const void* x, int64_t 
  *   loss[row] = w t^2 sum_j p_j (log p_j - log q[index_j]),   grad[row][v] = w t (q[v] - sum of p_j with index_j = v),
  * the gradient of the sum of all losses, in z's type.  An entry whose index is outside [0, vocab) is absent (-1, say, in rows of fewer entries);
  * entries of one index add up.  weight: w of each row, or NULL for 1.  A row of weight 0 or without entries has loss 0 and gradient 0,
- * whatever its logits hold.  Logits of -inf have q = 0; a row that holds +inf, a NaN or nothing but -inf is NaN.  grad may be NULL, or
- * the logits themselves (with ld_grad = ld).  n_top is at most GVQ_MAX_TOP.
+ * whatever its logits hold.  Logits of -inf have q = 0; a row that holds +inf, a NaN or nothing but -inf is NaN.  Where that is so of the
+ * teacher's entries, the loss is NaN and the gradient is at their places.  grad may be NULL, or the logits themselves (with ld_grad = ld).
+ * n_top is at most GVQ_MAX_TOP.
  */
 int64_t gvq_distill_workspace(int64_t rows, int64_t vocab, int64_t n_top);
 int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* top, gvq_dtype_t top_dtype,

@@ -129,6 +129,23 @@ def test_logits_that_are_masked(distill, vocab, dtype):
     assert np.allclose(_np(grad[3:4]), want[1], rtol=ref.BF16_HALF, atol=1e-6)
 
 
+@pytest.mark.parametrize("vocab", [40, 9001, 66001])
+def test_a_teacher_without_a_softmax(distill, vocab):
+    z, a, index, w = _case(5, vocab, 4, F32)
+    index[:] = torch.tensor([30, 2, 7, 2])
+    a[0, 1] = float("inf")
+    a[1] = -float("inf")
+    a[2, 3] = float("nan")
+    a[3, 0] = -float("inf")                   # one entry of none: as if it were not there
+    z, a, index, w = z.to(DEV), a.to(DEV), index.to(DEV), w.to(DEV)
+    loss, grad = distill.loss_and_gradient(z, a, index, temperature=2.0, weight=w)
+    places = torch.zeros(vocab, dtype=torch.bool, device=DEV)
+    places[[30, 2, 7]] = True
+    assert torch.isnan(loss[:3]).all() and torch.isnan(grad[:3, places]).all() and torch.isfinite(grad[:3, ~places]).all()
+    rest = slice(3, 5)
+    _check((loss[rest], grad[rest]), z[rest], a[rest], index[rest], 2.0, w[rest], F32)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,vocab", [(9, 515), (3, 20001)])
 def test_strides_windows_and_in_place(distill, rows, vocab, dtype):

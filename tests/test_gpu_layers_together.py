@@ -143,3 +143,35 @@ def test_a_step_in_an_autograd_function(example):
     Loss.apply(Layer.apply(Layer.apply(Gated.apply(x, leaves[0]), leaves[1]), leaves[2]), top, index, weight).backward()
     _, grads = example.gradients([both, down, head], x, top, index, weight)
     assert all(torch.equal(leaf.grad, g) for leaf, g in zip(leaves, grads))
+
+
+def test_two_streams_at_one_time():
+    """Calls that run side by side share nothing: each has its own workspace, from its own stream."""
+    from paper_1811_03617_amd import distill, i8
+    gen = torch.Generator(device=DEV).manual_seed(9)
+
+    def numbers(*shape):
+        return torch.randn(*shape, generator=gen, device=DEV)
+    sets = []
+    for rows in (500, 1300):
+        _, wt = i8.quantize_both(numbers(600, 700))
+        gate, gate_t = i8.quantize_both(numbers(900, 700))
+        logits, top = numbers(9, 70001), numbers(9, 5)
+        index = torch.randint(0, 70001, (9, 5), generator=gen, device=DEV)
+        sets.append((numbers(rows, 700), numbers(rows, 600), numbers(rows, 450), wt, gate, gate_t, logits, top, index))
+
+    def pass_(x, dy, dh, wt, gate, gate_t, logits, top, index):
+        return (*i8.linear_backward(dy, x, wt), i8.gated(x[:3], gate), *i8.gated_backward(dh, x, gate, gate_t), *distill.loss_and_gradient(logits, top, index))
+    want = [pass_(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for stream in streams:
+        stream.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(10):
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[k].append(pass_(*sets[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for one in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(one, want[k]))
