@@ -294,6 +294,7 @@ int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t voc
 {
     if (!is_dtype(dtype) || !is_dtype(top_dtype) || !in_range(rows) || !in_range(vocab) || n_top < 0 || n_top > GVQ_MAX_TOP) return GVQ_EINVAL;
     if (ld < vocab || ld_top < n_top || ld_index < n_top || (grad && ld_grad < vocab)) return GVQ_EINVAL;
+    if (grad && grad == logits && ld_grad != ld && rows > 1) return GVQ_EINVAL;   // in place, but other rows' places
     if (!(temperature >= 1e-3 && temperature <= 1e3)) return GVQ_EINVAL;
     if (rows == 0) return GVQ_OK;
     if (!loss || (vocab > 0 && !logits) || (n_top > 0 && (!top || !index)) || (gvq_distill_parts(rows, vocab) > 1 && !workspace)) return GVQ_EINVAL;

@@ -133,6 +133,7 @@ def test_gated_refusals():
 def test_loss_refusals():
     call = _caller(L.gvq_distill, [A, F, 8, 100, 100, A, B, A, 5, 5, 5, A, 1.0, A, A, 100, None, None])
     for change in ({0: None}, {1: 4}, {2: -1}, {3: -1}, {4: 99}, {5: None}, {6: 3}, {7: None}, {8: -1}, {8: gvq.MAX_TOP + 1, 9: 2000, 10: 2000}, {9: 4}, {10: 4},
+                   {15: 101}, {4: 101},                    # in place, with rows that start elsewhere
                    {12: 0.0}, {12: -1.0}, {12: float("nan")}, {12: float("inf")}, {12: 1e-4}, {12: 1e4}, {13: None}, {15: 99},
                    {3: 65536, 4: 65536, 15: 65536}):      # the last: few rows of many logits need a workspace
         assert call(change) == gvq.EINVAL, change
