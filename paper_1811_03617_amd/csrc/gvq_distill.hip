@@ -4,8 +4,9 @@
 //
 // Powers are of 2, of (z - largest) c with c = log2(e) / t: the difference first, since z c alone may leave fp32 (masks of the type's lowest
 // value) and loses bits that the difference keeps.  With e_j = 2^((a_j - top_a) c), A = sum e_j, S = sum_v 2^((z_v - top_z) c):
-//   l = w t^2 ln 2 (sum_j e_j ((a_j - top_a) c - (z_j - top_z) c) / A + log2 S - log2 A),
-// so that two rounds of joining are enough: the largest, then A, S and that sum.
+//   l = w t (sum_j e_j ((a_j - top_a) - (z_j - top_z)) / A + t ln 2 (log2 S - log2 A)),
+// so that two rounds of joining are enough: the largest, then A, S and that sum, D.  D is held in 64 bits: at an entry that the student's mask
+// covers the difference may be twice the type's largest number, and the loss of it, times w p, is a number still.
 //
 // A row to a wave, to four or to sixteen; each thread keeps its first words of the row in registers and reads only the rest a second
 // time, for the gradient.  Bound: memory, each logit in and out once: 4096 x 131072 bf16 445 us (4.8 TB/s, a plain copy's 5.1), the losses alone 179 (6.0);
@@ -110,6 +111,51 @@ __device__ __forceinline__ void team_all(float (&v)[3], float none, float* part,
         }
     }
 }
+// Two values of 32 bits, summed for everybody, and one of 64 bits, summed for the first thread: only the loss needs it.  part: [2][TEAM / 64], part_d: [TEAM / 64].
+__device__ __forceinline__ double wave_sum(double v)
+{
+    auto from = [&](auto ctrl, auto rows) {   // (lanes that nothing comes to get 0.0)
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const unsigned int lo = (unsigned int)__builtin_amdgcn_update_dpp(0, (int)b, decltype(ctrl)::value, decltype(rows)::value, 0xf, false),
+                           hi = (unsigned int)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    };
+    typedef std::integral_constant<int, 0xf> All;
+    from(std::integral_constant<int, 0x111>{}, All{});
+    from(std::integral_constant<int, 0x112>{}, All{});
+    from(std::integral_constant<int, 0x114>{}, All{});
+    from(std::integral_constant<int, 0x118>{}, All{});
+    from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const unsigned int lo = (unsigned int)__builtin_amdgcn_readlane((int)b, 63), hi = (unsigned int)__builtin_amdgcn_readlane((int)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int TEAM>
+__device__ __forceinline__ void team_sums(float (&v)[2], double& d, float* part, double* part_d)
+{
+    constexpr int WAVES = TEAM / 64;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) v[k] = wave_all(v[k], 0.f, [](float a, float b) { return a + b; });
+    d = wave_sum(d);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) part[k * WAVES + (threadIdx.x >> 6)] = v[k];
+            part_d[threadIdx.x >> 6] = d;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            v[k] = part[k * WAVES];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v[k] += part[k * WAVES + i];
+        }
+        if (threadIdx.x == 0)
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) d += part_d[i];
+    }
+}
 struct JoinMax {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
@@ -150,18 +196,22 @@ __device__ __forceinline__ void distill_entries(const DistillArgs& a, int64_t ro
 }
 // A and the sum of the loss.
 template <int TEAM>
-__device__ __forceinline__ void distill_sums(const DistillArgs& a, int t, const DistillEntries& n, float top, float from, float& A, float& D)
+__device__ __forceinline__ void distill_sums(const DistillArgs& a, int t, const DistillEntries& n, float top, float from, float& A, double& D)
 {
-    const float c = a.log2_t;
     A = 0.f;
-    D = 0.f;
+    D = 0.0;
     for (int j = t; j < a.n_top; j += TEAM)
         if (n.at[j] >= 0) {
-            const float d = (n.e[j] - top) * c, e = __builtin_amdgcn_exp2f(d);
+            const float v = n.e[j], e = __builtin_amdgcn_exp2f((v - top) * a.log2_t);
             n.e[j] = e;
             A += e;
-            if (e != 0.f) D += e * (d - (n.z[j] - from) * c);   // (0 log 0 is 0)
+            if (e != 0.f) D += (double)e * (((double)v - (double)top) - ((double)n.z[j] - (double)from));   // (0 log 0 is 0)
         }
+}
+__device__ __forceinline__ float distill_loss(float w, float t, float A, float S, double D)
+{
+    const double logs = (double)(__builtin_amdgcn_logf(S) - __builtin_amdgcn_logf(A)) * 0.69314718055994531;
+    return (float)((double)w * (double)t * (D * (double)(1.f / A) + (double)t * logs));
 }
 // The gradient at the entries' places in [lo, hi), once the rest has been written; the first of several entries of one place has the
 // sum of all.
@@ -203,6 +253,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
     constexpr int ROWS = TEAM > 64 ? 1 : 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][3][n_top]
     __shared__ float part[2][3 * TEAM / 64];
+    __shared__ double part_d[TEAM / 64];
     const int t = threadIdx.x % TEAM, which = threadIdx.x / TEAM;
     const int64_t row = (int64_t)blockIdx.x * ROWS + which;
     if (ROWS > 1 && row >= a.rows) return;
@@ -250,14 +301,14 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
         return;
     }
     const float from = distill_from(round[2]);
-    float sums[3];   // A, D, S
-    distill_sums<TEAM>(a, t, n, round[1], from, sums[0], sums[1]);
-    sums[2] = sum.sum * distill_power(sum.top, from, c);
-    team_all<TEAM>(sums, 0.f, part[1], JoinSum());
-    if (t == 0)
-        a.loss[row] = w * a.t * a.t * 0.69314718f * (sums[1] / sums[0] + __builtin_amdgcn_logf(sums[2]) - __builtin_amdgcn_logf(sums[0]));
+    float sums[2];   // A, S
+    double D;
+    distill_sums<TEAM>(a, t, n, round[1], from, sums[0], D);
+    sums[1] = sum.sum * distill_power(sum.top, from, c);
+    team_sums<TEAM>(sums, D, part[1], part_d);
+    if (t == 0) a.loss[row] = distill_loss(w, a.t, sums[0], sums[1], D);
     if constexpr (GRAD) {
-        const float scale = w * a.t / sums[2];
+        const float scale = w * a.t / sums[1];
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         // the rest backwards: what was read last is in the caches still (2048 x 131072 fp32 596 us forwards, 502 so, 4096 x 65536 544 and 448; bf16, a
         // row's rest being shorter, 422 and 417)
@@ -336,6 +387,7 @@ __global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int p
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float shared[2][3 * TEAM / 64];
+    __shared__ double shared_d[TEAM / 64];
     const int pieces = GRAD ? parts : 1, t = threadIdx.x;
     const int64_t row = blockIdx.x / pieces;
     const DistillPiece piece = distill_piece(a.vocab, parts, blockIdx.x % pieces);
@@ -361,14 +413,14 @@ __global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int p
         return;
     }
     const float from = distill_from(round[2]);
-    float s[3];
-    distill_sums<TEAM>(a, t, n, round[1], from, s[0], s[1]);
-    s[2] = mine.sum * distill_power(mine.top, from, c);
-    team_all<TEAM>(s, 0.f, shared[1], JoinSum());
-    if (t == 0 && piece.lo == 0)
-        a.loss[row] = w * a.t * a.t * 0.69314718f * (s[1] / s[0] + __builtin_amdgcn_logf(s[2]) - __builtin_amdgcn_logf(s[0]));
+    float s[2];
+    double D;
+    distill_sums<TEAM>(a, t, n, round[1], from, s[0], D);
+    s[1] = mine.sum * distill_power(mine.top, from, c);
+    team_sums<TEAM>(s, D, shared[1], shared_d);
+    if (t == 0 && piece.lo == 0) a.loss[row] = distill_loss(w, a.t, s[0], s[1], D);
     if constexpr (GRAD) {
-        const float scale = w * a.t / s[2];
+        const float scale = w * a.t / s[1];
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         distill_each<TEAM>(z, piece, [&](int i) {
             DistillWord<T> word;
