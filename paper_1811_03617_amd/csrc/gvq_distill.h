@@ -13,12 +13,13 @@ struct DistillArgs {
     int64_t ld_index;
     int n_top;
     const float* weight;      // [rows] or null: ones
-    float t, log2_t;          // temperature t, log2(e) / t
+    double t64;               // temperature t,
+    float t, per_t, log2_t;   // t, 1 / t, log2(e) / t
     float* loss;              // [rows]
     void* grad;               // [rows][vocab] or null
     int64_t ld_grad;
 };
 
-// Pieces that a row is cut into: few rows of many logits.  workspace: two floats for each.
+// Pieces that a row is cut into: few rows of many logits.  workspace: two floats for each, or half as many pieces of two doubles.
 int gvq_distill_parts(int64_t rows, int64_t vocab);
 int gvq_launch_distill(const DistillArgs& a, gvq_dtype_t dtype, void* workspace, hipStream_t st);

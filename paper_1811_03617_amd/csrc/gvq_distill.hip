@@ -46,25 +46,87 @@ __device__ __forceinline__ void distill_store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void distill_store(unsigned short* p, float v) { *p = (unsigned short)f32_to_bf16_rne(v); }
 
 // Largest z so far and the sum of 2^((z - largest) c).  As long as there is nothing but -inf, `top` is -inf and differences are taken from 0.
-struct DistillSum {
-    float top, sum;
-};
 __device__ __forceinline__ float distill_from(float top) { return top == -INFINITY ? 0.f : top; }
 __device__ __forceinline__ float distill_power(float z, float from, float c) { return __builtin_amdgcn_exp2f((z - from) * c); }
-template <int N>
-__device__ __forceinline__ void distill_add(DistillSum& a, const float (&v)[N], float c)
-{
-    float m = v[0];
+template <bool WARM>
+struct DistillSum {
+    typedef float Number;
+    float top = -INFINITY, sum = 0.f;
+    template <int N>
+    __device__ __forceinline__ void add(const DistillArgs& a, const float (&v)[N])
+    {
+        const float c = a.log2_t;
+        float m = v[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
-    m = fmaxf(a.top, m);
-    const float from = distill_from(m);
-    float s = a.sum * distill_power(a.top, from, c);
+        for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+        m = fmaxf(top, m);
+        const float from = distill_from(m);
+        float s = sum * distill_power(top, from, c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += distill_power(v[i], from, c);
-    a.sum = s;
-    a.top = m;
-}
+        for (int i = 0; i < N; ++i) s += distill_power(v[i], from, c);
+        sum = s;
+        top = m;
+    }
+    __device__ __forceinline__ float seen_from(const DistillArgs& a, float from) const { return sum * distill_power(top, from, a.log2_t); }
+};
+
+// High temperatures.  The loss is t^2 times a difference of logarithms, which are near each other where the entries hold most of the softmax: an
+// error of 2^-24 in S or A counts t^2 times, while the loss does not grow with t (1000 logits, all of them entries, off by, relative: 6e-6 at t = 8,
+// 3e-5 at 20, 9e-4 at 100, 8 % at 1000; this way 3e-7 at any).  Above DISTILL_WARM therefore, with x = (z - from) / t from a number `from` near z's,
+//   sum of e^x = sum of 1 + x + r(x) where |x| < 1, and of e^x elsewhere,   r(x) = e^x - 1 - x = x^2 P(x),
+// the number of the first and their sum of z in 64 bits, which holds that sum exactly where |z| is large against t.  What is left in 32 bits, r and
+// the other powers, is off by a few 2^-24 of x^2 at most, and that times t^2 is (z - from)^2, whatever t is.  `from` is a thread's first
+// word's largest, and moves only where powers would leave fp32.  Entries, logarithms and joined sums are in 64 bits.
+// Its price is arithmetic, and why it is not the way for all (us, the other way and this): 4096 x 131072 bf16 444 and 640, the losses alone 178 and 318, 2048 x
+// 131072 fp32 517 and 530, 8192 x 2048 bf16 18.6 and 28, 16 x 50021 fp32 12.0 and 18.1.
+#define DISTILL_WARM 8.0
+template <>
+struct DistillSum<true> {
+    typedef double Number;
+    float top = -INFINITY, ref = -INFINITY;
+    double z = 0.0, more = 0.0;   // of the near ones; r and the other powers
+    int near = 0;
+    template <int N>
+    __device__ __forceinline__ void add(const DistillArgs& a, const float (&v)[N])
+    {
+        float m = v[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+        top = fmaxf(top, m);
+        if ((m - ref) * a.per_t > 60.f) {   // (-inf - -inf is no number)
+            more = seen_from(a, m);
+            z = 0.0;
+            near = 0;
+            ref = m;
+        }
+        const float from = distill_from(ref);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = (v[i] - from) * a.per_t;
+            const bool is_near = fabsf(x) < 1.f;   // (not so of a NaN)
+            float p = 1.f / 3628800;               // (x^9 / 11! is 7e-8 of P at most)
+            p = __builtin_fmaf(p, x, 1.f / 362880);
+            p = __builtin_fmaf(p, x, 1.f / 40320);
+            p = __builtin_fmaf(p, x, 1.f / 5040);
+            p = __builtin_fmaf(p, x, 1.f / 720);
+            p = __builtin_fmaf(p, x, 1.f / 120);
+            p = __builtin_fmaf(p, x, 1.f / 24);
+            p = __builtin_fmaf(p, x, 1.f / 6);
+            p = __builtin_fmaf(p, x, 0.5f);
+            s += is_near ? x * x * p : distill_power(v[i], from, a.log2_t);
+            z += is_near ? (double)v[i] : 0.0;
+            near += is_near;
+        }
+        more += (double)s;
+    }
+    __device__ __forceinline__ double seen_from(const DistillArgs& a, float from) const
+    {
+        if (ref == -INFINITY) return more;   // nothing but -inf and NaN
+        const double per = 1.0 / a.t64, sum = near == 0 ? more : more + (double)near + (z - (double)near * (double)ref) * per;
+        return ref == from ? sum : sum * exp(((double)ref - (double)from) * per);
+    }
+};
 
 // A row's numbers before the first whole word of 16 bytes.
 template <typename T>
@@ -156,11 +218,31 @@ __device__ __forceinline__ void team_sums(float (&v)[2], double& d, float* part,
             for (int i = 1; i < WAVES; ++i) d += part_d[i];
     }
 }
+template <int TEAM>
+__device__ __forceinline__ void team_sums(double (&v)[2], double& d, double* part, double* part_d)
+{
+    constexpr int WAVES = TEAM / 64;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) v[k] = wave_sum(v[k]);
+    d = wave_sum(d);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) part[k * WAVES + (threadIdx.x >> 6)] = v[k];
+            part_d[threadIdx.x >> 6] = d;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            v[k] = part[k * WAVES];
+            for (int i = 1; i < WAVES; ++i) v[k] += part[k * WAVES + i];
+        }
+        if (threadIdx.x == 0)
+            for (int i = 1; i < WAVES; ++i) d += part_d[i];
+    }
+}
 struct JoinMax {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
-struct JoinSum {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
 template <int TEAM>
 __device__ __forceinline__ void team_sync()
@@ -195,23 +277,30 @@ __device__ __forceinline__ void distill_entries(const DistillArgs& a, int64_t ro
     }
 }
 // A and the sum of the loss.
-template <int TEAM>
-__device__ __forceinline__ void distill_sums(const DistillArgs& a, int t, const DistillEntries& n, float top, float from, float& A, double& D)
+__device__ __forceinline__ float distill_entry(const DistillArgs& a, float v, float top, float) { return __builtin_amdgcn_exp2f((v - top) * a.log2_t); }
+__device__ __forceinline__ double distill_entry(const DistillArgs& a, float v, float top, double) { return exp(((double)v - (double)top) / a.t64); }
+template <int TEAM, typename N>
+__device__ __forceinline__ void distill_sums(const DistillArgs& a, int t, const DistillEntries& n, float top, float from, N& A, double& D)
 {
-    A = 0.f;
+    A = 0;
     D = 0.0;
     for (int j = t; j < a.n_top; j += TEAM)
         if (n.at[j] >= 0) {
-            const float v = n.e[j], e = __builtin_amdgcn_exp2f((v - top) * a.log2_t);
-            n.e[j] = e;
+            const float v = n.e[j];
+            const N e = distill_entry(a, v, top, N());
+            n.e[j] = (float)e;
             A += e;
-            if (e != 0.f) D += (double)e * (((double)v - (double)top) - ((double)n.z[j] - (double)from));   // (0 log 0 is 0)
+            if (e != 0) D += (double)e * (((double)v - (double)top) - ((double)n.z[j] - (double)from));   // (0 log 0 is 0)
         }
 }
-__device__ __forceinline__ float distill_loss(float w, float t, float A, float S, double D)
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, float w, const float (&s)[2], double D)   // s: A and S
 {
-    const double logs = (double)(__builtin_amdgcn_logf(S) - __builtin_amdgcn_logf(A)) * 0.69314718055994531;
-    return (float)((double)w * (double)t * (D * (double)(1.f / A) + (double)t * logs));
+    const double logs = (double)(__builtin_amdgcn_logf(s[1]) - __builtin_amdgcn_logf(s[0])) * 0.69314718055994531;
+    return (float)((double)w * (double)a.t * (D * (double)(1.f / s[0]) + (double)a.t * logs));
+}
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, float w, const double (&s)[2], double D)
+{
+    return (float)((double)w * a.t64 * (D / s[0] + a.t64 * (log(s[1]) - log(s[0]))));
 }
 // The gradient at the entries' places in [lo, hi), once the rest has been written; the first of several entries of one place has the
 // sum of all.
@@ -247,12 +336,14 @@ __device__ __forceinline__ void distill_out(const DistillWord<T>& word, T* g, bo
 }
 
 // TEAM threads a row (64: four rows a work-group), HOLD times eight logits of each in registers.
-template <typename T, int TEAM, int HOLD, bool GRAD>
-__global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void distill_row_kernel(DistillArgs a)
+template <typename T, int TEAM, int HOLD, bool GRAD, bool WARM>
+__global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 && !WARM ? 8 : 4) void distill_row_kernel(DistillArgs a)
 {
+    typedef typename DistillSum<WARM>::Number Number;
     constexpr int ROWS = TEAM > 64 ? 1 : 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];   // [ROWS][3][n_top]
-    __shared__ float part[2][3 * TEAM / 64];
+    __shared__ float part[3 * TEAM / 64];
+    __shared__ Number part_s[2 * TEAM / 64];
     __shared__ double part_d[TEAM / 64];
     const int t = threadIdx.x % TEAM, which = threadIdx.x / TEAM;
     const int64_t row = (int64_t)blockIdx.x * ROWS + which;
@@ -267,7 +358,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
     float round[3] = {0.f, -INFINITY, -INFINITY};   // any entries, the largest of them, the largest logit
     const int head = distill_head(z, a.vocab), words = (a.vocab - head) / 8, rest = a.vocab - 8 * words;
     DistillWord<T> held[HOLD];
-    DistillSum sum = {-INFINITY, 0.f};
+    DistillSum<WARM> sum;
     if (w != 0.f) {
 #pragma unroll
         for (int i = 0; i < HOLD; ++i)
@@ -278,22 +369,22 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
             if (t + i * TEAM < words) {
                 float v[8];
                 held[i].numbers(v);
-                distill_add(sum, v, c);
+                sum.add(a, v);
             }
         for (int i = t + HOLD * TEAM; i < words; i += TEAM) {
             DistillWord<T> word;
             float v[8];
             word.load(z + head + 8 * i);
             word.numbers(v);
-            distill_add(sum, v, c);
+            sum.add(a, v);
         }
         for (int i = t; i < rest; i += TEAM) {
             const float v[1] = {distill_load(z + (i < head ? i : 8 * words + i))};
-            distill_add(sum, v, c);
+            sum.add(a, v);
         }
         round[2] = sum.top;
     }
-    team_all<TEAM>(round, -INFINITY, part[0], JoinMax());
+    team_all<TEAM>(round, -INFINITY, part, JoinMax());
     if (!(round[0] > 0.f)) {   // weight 0 or no entries
         if (t == 0) a.loss[row] = 0.f;
         if (GRAD)
@@ -301,14 +392,14 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
         return;
     }
     const float from = distill_from(round[2]);
-    float sums[2];   // A, S
+    Number sums[2];   // A, S
     double D;
     distill_sums<TEAM>(a, t, n, round[1], from, sums[0], D);
-    sums[1] = sum.sum * distill_power(sum.top, from, c);
-    team_sums<TEAM>(sums, D, part[1], part_d);
-    if (t == 0) a.loss[row] = distill_loss(w, a.t, sums[0], sums[1], D);
+    sums[1] = sum.seen_from(a, from);
+    team_sums<TEAM>(sums, D, part_s, part_d);
+    if (t == 0) a.loss[row] = distill_loss(a, w, sums, D);
     if constexpr (GRAD) {
-        const float scale = w * a.t / sums[1];
+        const float scale = w * a.t / (float)sums[1];
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         // the rest backwards: what was read last is in the caches still (2048 x 131072 fp32 596 us forwards, 502 so, 4096 x 65536 544 and 448; bf16, a
         // row's rest being shorter, 422 and 417)
@@ -327,13 +418,13 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256, TEAM > 256 ? 8 : 4) void di
             distill_store(g + at, distill_power(distill_load(z + at), from, c) * scale);
         }
         team_sync<TEAM>();
-        distill_places<TEAM>(a, t, n, g, 0, a.vocab, from, scale, w * a.t / sums[0]);
+        distill_places<TEAM>(a, t, n, g, 0, a.vocab, from, scale, w * a.t / (float)sums[0]);
     }
 }
 
 // ---- few rows of many logits -----------------------------------------------------------------------------------------
 
-// A row in `parts` pieces of whole words; its largest logits and sums go into sums [rows][parts][2], and a second launch joins them.
+// A row in `parts` pieces of whole words; its sums and largest logits go into sums [rows][parts][2], and a second launch joins them.
 struct DistillPiece {
     int lo, hi;
 };
@@ -352,41 +443,53 @@ __device__ __forceinline__ void distill_each(const T* z, DistillPiece p, F8 word
     for (int i = threadIdx.x; i < rest; i += TEAM) one(p.lo + (i < head ? i : 8 * words + i));
 }
 
-template <typename T, int TEAM>
-__global__ __launch_bounds__(TEAM) void distill_part_kernel(DistillArgs a, int parts, float* sums)
+template <typename T, int TEAM, bool WARM>
+__global__ __launch_bounds__(TEAM) void distill_part_kernel(DistillArgs a, int parts, typename DistillSum<WARM>::Number* sums)
 {
-    __shared__ float shared[2][3 * TEAM / 64];
+    typedef typename DistillSum<WARM>::Number Number;
+    __shared__ float shared[3 * TEAM / 64];
+    __shared__ Number shared_s[2 * TEAM / 64];
+    __shared__ double shared_d[TEAM / 64];
     const int64_t row = blockIdx.x / parts;
     const int part = blockIdx.x % parts;
     if (a.weight && a.weight[row] == 0.f) return;   // (nobody reads its sums)
     const T* z = (const T*)a.logits + row * a.ld;
-    const float c = a.log2_t;
-    DistillSum sum = {-INFINITY, 0.f};
+    DistillSum<WARM> sum;
     distill_each<TEAM>(z, distill_piece(a.vocab, parts, part), [&](int i) {
         DistillWord<T> word;
         float v[8];
         word.load(z + i);
         word.numbers(v);
-        distill_add(sum, v, c);
+        sum.add(a, v);
     }, [&](int i) {
         const float v[1] = {distill_load(z + i)};
-        distill_add(sum, v, c);
+        sum.add(a, v);
     });
     float top[3] = {sum.top, -INFINITY, -INFINITY};
-    team_all<TEAM>(top, -INFINITY, shared[0], JoinMax());
-    float s[3] = {sum.sum * distill_power(sum.top, distill_from(top[0]), c), 0.f, 0.f};
-    team_all<TEAM>(s, 0.f, shared[1], JoinSum());
+    team_all<TEAM>(top, -INFINITY, shared, JoinMax());
+    Number s[2] = {sum.seen_from(a, distill_from(top[0])), 0};
+    double none = 0.0;
+    team_sums<TEAM>(s, none, shared_s, shared_d);
     if (threadIdx.x == 0) {
-        sums[2 * (row * parts + part)] = top[0];
-        sums[2 * (row * parts + part) + 1] = s[0];
+        sums[2 * (row * parts + part)] = s[0];
+        sums[2 * (row * parts + part) + 1] = top[0];
     }
 }
 
-template <typename T, int TEAM, bool GRAD>
-__global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int parts, const float* sums)
+// A piece's sum from the largest logit of the row.
+__device__ __forceinline__ float distill_join(const DistillArgs& a, float sum, float top, float from) { return sum * distill_power(top, from, a.log2_t); }
+__device__ __forceinline__ double distill_join(const DistillArgs& a, double sum, float top, float from)
 {
+    return sum * exp(((double)top - (double)from) / a.t64);
+}
+
+template <typename T, int TEAM, bool GRAD, bool WARM>
+__global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int parts, const typename DistillSum<WARM>::Number* sums)
+{
+    typedef typename DistillSum<WARM>::Number Number;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float shared[2][3 * TEAM / 64];
+    __shared__ float shared[3 * TEAM / 64];
+    __shared__ Number shared_s[2 * TEAM / 64];
     __shared__ double shared_d[TEAM / 64];
     const int pieces = GRAD ? parts : 1, t = threadIdx.x;
     const int64_t row = blockIdx.x / pieces;
@@ -399,13 +502,17 @@ __global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int p
     n.z = n.e + a.n_top;
     n.at = (int*)(n.z + a.n_top);
     float round[3] = {0.f, -INFINITY, -INFINITY};
-    DistillSum mine = {-INFINITY, 0.f};
+    Number sum = 0;
+    float top = -INFINITY;
     if (w != 0.f) {
         distill_entries<TEAM>(a, row, t, z, n, round[0], round[1]);
-        if (t < parts) mine = {sums[2 * (row * parts + t)], sums[2 * (row * parts + t) + 1]};
-        round[2] = mine.top;
+        if (t < parts) {
+            sum = sums[2 * (row * parts + t)];
+            top = (float)sums[2 * (row * parts + t) + 1];
+        }
+        round[2] = top;
     }
-    team_all<TEAM>(round, -INFINITY, shared[0], JoinMax());
+    team_all<TEAM>(round, -INFINITY, shared, JoinMax());
     if (!(round[0] > 0.f)) {
         if (t == 0 && piece.lo == 0) a.loss[row] = 0.f;
         if (GRAD)
@@ -413,14 +520,14 @@ __global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int p
         return;
     }
     const float from = distill_from(round[2]);
-    float s[2];
+    Number s[2];
     double D;
     distill_sums<TEAM>(a, t, n, round[1], from, s[0], D);
-    s[1] = mine.sum * distill_power(mine.top, from, c);
-    team_sums<TEAM>(s, D, shared[1], shared_d);
-    if (t == 0 && piece.lo == 0) a.loss[row] = distill_loss(w, a.t, s[0], s[1], D);
+    s[1] = distill_join(a, sum, top, from);
+    team_sums<TEAM>(s, D, shared_s, shared_d);
+    if (t == 0 && piece.lo == 0) a.loss[row] = distill_loss(a, w, s, D);
     if constexpr (GRAD) {
-        const float scale = w * a.t / s[1];
+        const float scale = w * a.t / (float)s[1];
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         distill_each<TEAM>(z, piece, [&](int i) {
             DistillWord<T> word;
@@ -428,18 +535,18 @@ __global__ __launch_bounds__(TEAM) void distill_join_kernel(DistillArgs a, int p
             distill_out(word, g + i, same, from, c, scale);
         }, [&](int i) { distill_store(g + i, distill_power(distill_load(z + i), from, c) * scale); });
         __syncthreads();
-        distill_places<TEAM>(a, t, n, g, piece.lo, piece.hi, from, scale, w * a.t / s[0]);
+        distill_places<TEAM>(a, t, n, g, piece.lo, piece.hi, from, scale, w * a.t / (float)s[0]);
     }
 }
 
-template <typename T, int TEAM, int HOLD>
+template <typename T, int TEAM, int HOLD, bool WARM>
 static int launch_rows(const DistillArgs& a, hipStream_t st)
 {
     constexpr int ROWS = TEAM > 64 ? 1 : 4;
     const unsigned lds = (unsigned)(ROWS * 12 * a.n_top);
     const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS)), threads(TEAM > 64 ? TEAM : 256);
-    if (a.grad) hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, true>), grid, threads, lds, st, a);
-    else hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, false>), grid, threads, lds, st, a);
+    if (a.grad) hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, true, WARM>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((distill_row_kernel<T, TEAM, HOLD, false, WARM>), grid, threads, lds, st, a);
     GVQ_HIP(hipGetLastError());
     return GVQ_OK;
 }
@@ -458,18 +565,20 @@ int gvq_distill_parts(int64_t rows, int64_t vocab)
     return (int)(want < most ? want : most);
 }
 
-template <typename T>
-static int launch_distill(const DistillArgs& a, float* sums, hipStream_t st)
+template <typename T, bool WARM>
+static int launch_distill(const DistillArgs& a, void* workspace, hipStream_t st)
 {
-    // in place the second launch's work-groups would read the student's logits at entries that another piece's have replaced: rows stay whole
-    const int parts = a.grad == a.logits ? 1 : gvq_distill_parts(a.rows, a.vocab);
+    // in place the second launch's work-groups would read the student's logits at entries that another piece's have replaced: rows stay whole.  Warm: a
+    // piece's numbers are of 64 bits, and there are half as many for the same workspace.
+    const int parts = a.grad == a.logits ? 1 : gvq_distill_parts(a.rows, a.vocab) / (WARM ? 2 : 1);
     if (parts > 1) {
+        auto* sums = (typename DistillSum<WARM>::Number*)workspace;
         const unsigned lds = (unsigned)(12 * a.n_top);
         const dim3 grid((unsigned)(a.rows * parts)), threads(DISTILL_TEAM);
-        hipLaunchKernelGGL((distill_part_kernel<T, DISTILL_TEAM>), grid, threads, 0, st, a, parts, sums);
+        hipLaunchKernelGGL((distill_part_kernel<T, DISTILL_TEAM, WARM>), grid, threads, 0, st, a, parts, sums);
         GVQ_HIP(hipGetLastError());
-        if (a.grad) hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, true>), grid, threads, lds, st, a, parts, sums);
-        else hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, false>), dim3((unsigned)a.rows), threads, lds, st, a, parts, sums);
+        if (a.grad) hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, true, WARM>), grid, threads, lds, st, a, parts, sums);
+        else hipLaunchKernelGGL((distill_join_kernel<T, DISTILL_TEAM, false, WARM>), dim3((unsigned)a.rows), threads, lds, st, a, parts, sums);
         GVQ_HIP(hipGetLastError());
         return GVQ_OK;
     }
@@ -477,12 +586,14 @@ static int launch_distill(const DistillArgs& a, float* sums, hipStream_t st)
     // 36, 30; 4096 x 8192 bf16 35, 28, 48; 8192 x 4096 fp32 77, 54, 81; 4096 x 16384 bf16 -, 50, 60; 4096 x 32000 bf16 -, 112, 107; 64 x 32000 -, 13,
     // 9.2.  Many entries would take a wave's row too much LDS.
     const int64_t bytes = (int64_t)a.vocab * (int64_t)sizeof(T);
-    if (bytes <= 4096 && a.n_top <= 256) return launch_rows<T, 64, sizeof(T) == 2 ? 4 : 2>(a, st);
-    if (bytes <= (a.rows >= 1024 ? 32768 : 16384)) return launch_rows<T, 256, 4>(a, st);
-    return launch_rows<T, 1024, sizeof(T) == 2 ? 6 : 3>(a, st);
+    if (bytes <= 4096 && a.n_top <= 256) return launch_rows<T, 64, sizeof(T) == 2 ? 4 : 2, WARM>(a, st);
+    if (bytes <= (a.rows >= 1024 ? 32768 : 16384)) return launch_rows<T, 256, 4, WARM>(a, st);
+    return launch_rows<T, 1024, sizeof(T) == 2 ? 6 : 3, WARM>(a, st);
 }
 
 int gvq_launch_distill(const DistillArgs& a, gvq_dtype_t dtype, void* workspace, hipStream_t st)
 {
-    return dtype == GVQ_BF16 ? launch_distill<unsigned short>(a, (float*)workspace, st) : launch_distill<float>(a, (float*)workspace, st);
+    const bool warm = a.t64 > DISTILL_WARM;
+    if (dtype == GVQ_BF16) return warm ? launch_distill<unsigned short, true>(a, workspace, st) : launch_distill<unsigned short, false>(a, workspace, st);
+    return warm ? launch_distill<float, true>(a, workspace, st) : launch_distill<float, false>(a, workspace, st);
 }

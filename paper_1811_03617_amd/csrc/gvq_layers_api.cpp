@@ -306,7 +306,7 @@ int gvq_distill(const void* logits, gvq_dtype_t dtype, int64_t rows, int64_t voc
     a.top = top; a.top_bf16 = top_dtype == GVQ_BF16; a.ld_top = ld_top;
     a.index = index; a.ld_index = ld_index; a.n_top = (int)n_top;
     a.weight = weight;
-    a.t = (float)temperature; a.log2_t = (float)(1.4426950408889634 / temperature);
+    a.t64 = temperature; a.t = (float)temperature; a.per_t = (float)(1.0 / temperature); a.log2_t = (float)(1.4426950408889634 / temperature);
     a.loss = loss; a.grad = grad; a.ld_grad = ld_grad;
     return gvq_launch_distill(a, dtype, workspace, (hipStream_t)stream);
 }

@@ -1,4 +1,5 @@
-"""The loss on a teacher's top logits at the ends of its ranges: entries that the student's mask covers with the type's lowest value."""
+"""The loss on a teacher's top logits at the ends of its ranges: entries that the student's mask covers with the type's lowest value, and high
+temperatures, at which it is a small difference of large numbers."""
 import numpy as np
 import pytest
 
@@ -45,3 +46,148 @@ def test_entries_under_a_mask_of_the_lowest_value(distill, vocab, dtype, t):
         last = ref.BF16_HALF if dtype == BF16 else 0
         assert (np.abs(_np(grad) - want_grad) <= 0.01 * t * room + last * np.abs(want_grad)).all()
     assert torch.equal(distill.loss(z.to(DEV), a.to(DEV), index.to(DEV), temperature=t, weight=w.to(DEV)), loss) or vocab == 66001
+
+
+def _check_warm(got, z, a, index, t, w, dtype):
+    """Room of the loss, in halves of float32 steps, that does not grow with t.  With x = (z - largest) / t: where x > -1 what is beyond 1 + x is off
+    by 20 of its own halves (x by 3, twice, the polynomial by 3, products 2, sums of eight 8), and is at most x^2 / 2; a power e^x elsewhere is
+    off by 10 + 4 |x|, at most 14 x^2 e^x.  Times t^2, over a sum of at least 1 and averaged over the row: 14 (z - largest)^2 at most.  Then one
+    rounding of the loss.  float64's own roundings are multiplied by t^2 too, here and in the definition: four logarithms of up to 1 + log(vocab), each
+    to half a step (2^-53), and powers and sums of a few, 16 (1 + log(vocab)) altogether; at t = 1000 that is 1e-8 of w.  Gradients: as for other temperatures."""
+    loss, grad = got
+    zn, an, wn, i = _np(z), _np(a), _np(w), index.cpu().numpy()
+    want_loss, want_grad = ref.distill(zn, an, i, t, wn)
+    ok = np.isfinite(zn)
+    top = np.where(ok, zn, -np.inf).max(1)
+    span = np.where(ok, top[:, None] - zn, 0)
+    power = np.where(ok, np.exp(-span / t), 0)
+    far = (np.minimum(span, 90 * t) ** 2 * np.where(span < t, 1, power)).max(1)
+    double = wn * t * t * 2.0 ** -53 * 16 * (1 + np.log(zn.shape[1]))
+    assert (np.abs(_np(loss) - want_loss) <= wn * ref.F32_HALF * 16 * far + ref.F32_HALF * np.abs(want_loss) + double).all()
+    q = power / power.sum(1, keepdims=True)
+    there = np.zeros_like(zn)
+    for r in range(len(zn)):
+        there[r, i[r][(i[r] >= 0) & (i[r] < zn.shape[1])]] = 1
+    e = ref.F32_HALF * (40 + 8 * (span.max() + np.abs(an).max()) / t)
+    room = wn[:, None] * t * (q + there) * e
+    last = ref.BF16_HALF if dtype == BF16 else 0
+    assert (np.abs(_np(grad) - want_grad) <= room + last * (np.abs(want_grad) + room) + 2.0 ** -125).all()
+
+
+def _whole(rows, vocab, n, dtype, seed=0, spread=3.0, at=0.0):
+    """All the mass on the entries: logits behind a mask but for n of them, which the teacher names too."""
+    gen = torch.Generator().manual_seed(seed + vocab + rows)
+    z = torch.full((rows, vocab), -float("inf"))
+    index = torch.stack([torch.randperm(vocab, generator=gen)[:n] for _ in range(rows)])
+    z.scatter_(1, index, at + spread * torch.randn(rows, n, generator=gen))
+    a = spread * torch.randn(rows, n, generator=gen)
+    w = torch.rand(rows, generator=gen) + 0.5
+    return z.to(dtype), a.to(dtype), index, w
+
+
+@pytest.mark.parametrize("rows,vocab,n", [(3, 1, 1), (7, 64, 64), (16, 1000, 1000), (5, 9001, 1000), (4, 33000, 1024), (9, 70001, 1000), (1, 600001, 1024),
+                                          (97, 66000, 300)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [8.5, 20.0, 100.0, 1000.0])
+def test_high_temperatures_where_the_entries_hold_everything(distill, rows, vocab, n, dtype, t):
+    z, a, index, w = (v.to(DEV) for v in _whole(rows, vocab, n, dtype))
+    got = distill.loss_and_gradient(z, a, index, temperature=t, weight=w)
+    _check_warm(got, z, a, index, t, w, dtype)
+    if vocab < 70000:
+        assert torch.equal(distill.loss(z, a, index, temperature=t, weight=w), got[0])
+    same = z.clone()
+    _check_warm(distill.loss_and_gradient(same, a, index, temperature=t, weight=w, out=same), z, a, index, t, w, dtype)
+
+
+@pytest.mark.parametrize("vocab", [1000, 70001])
+@pytest.mark.parametrize("t", [20.0, 1000.0])
+@pytest.mark.parametrize("at,spread", [(1e6, 40.0), (-3e4, 2000.0), (0.0, 1e-3), (0.0, 0.0)])
+def test_high_temperatures_far_from_zero_and_wide(distill, vocab, t, at, spread):
+    z, a, index, w = (v.to(DEV) for v in _whole(6, vocab, 500, F32, spread=spread, at=at))
+    _check_warm(distill.loss_and_gradient(z, a, index, temperature=t, weight=w), z, a, index, t, w, F32)
+
+
+@pytest.mark.parametrize("rows,vocab,n", [(1, 1, 1), (2, 64, 3), (5, 1001, 17), (300, 70, 3), (3, 50021, 16), (2, 140000, 100), (96, 65536, 8), (97, 65536, 8)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [9.0, 300.0])
+def test_high_temperatures_in_ordinary_rows(distill, rows, vocab, n, dtype, t):
+    gen = torch.Generator().manual_seed(rows + vocab)
+    z = (3 * torch.randn(rows, vocab, generator=gen)).to(dtype).to(DEV)
+    a = (3 * torch.randn(rows, n, generator=gen)).to(dtype).to(DEV)
+    index, w = torch.randint(0, vocab, (rows, n), generator=gen).to(DEV), (torch.rand(rows, generator=gen) + 0.5).to(DEV)
+    got = distill.loss_and_gradient(z, a, index, temperature=t, weight=w)
+    _check_warm(got, z, a, index, t, w, dtype)
+    big = torch.full((rows, vocab + 7), float("nan"), dtype=dtype, device=DEV)
+    window = big[:, 3:3 + vocab]
+    window.copy_(z)
+    _check_warm(distill.loss_and_gradient(window, a, index, temperature=t, weight=w, out=window), z, a, index, t, w, dtype)
+    assert torch.isnan(big[:, :3]).all() and torch.isnan(big[:, 3 + vocab:]).all()
+
+
+@pytest.mark.parametrize("vocab", [40, 9001, 70001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_high_temperatures_masks_and_what_is_not_there(distill, vocab, dtype):
+    t = 50.0
+    gen = torch.Generator().manual_seed(vocab)
+    z = (3 * torch.randn(12, vocab, generator=gen)).to(dtype)
+    a = torch.randn(12, 3, generator=gen).to(dtype)
+    index = torch.tensor([[1, 5, 2]]).repeat(12, 1)
+    w = torch.full((12,), 0.01)
+    low = torch.finfo(dtype).min
+    z[0, 6:] = -float("inf")
+    z[1, 30:] = low
+    z[2] = low                                 # a softmax of equal numbers
+    z[3] = -float("inf")                       # no softmax: rows 3 to 7
+    z[4, 9] = float("nan")
+    z[5, 9] = float("inf")
+    z[6] = float("nan")
+    a[7, 1] = float("nan")
+    z[8, 5] = low                              # a loss as large as numbers get
+    z[9] = float("nan")                        # not looked at: rows 9 to 11
+    w[9] = 0
+    index[10] = -1
+    z[11, 7] = float("inf")
+    index[11] = vocab
+    a[0, 1] = -float("inf")                    # an entry of probability 0
+    index[8, 2] = 1                            # two of one place
+    z, a, index, w = z.to(DEV), a.to(DEV), index.to(DEV), w.to(DEV)
+    loss, grad = distill.loss_and_gradient(z, a, index, temperature=t, weight=w)
+    assert torch.isnan(loss[3:8]).all() and torch.isnan(grad[3:7]).all() and torch.isnan(grad[7, [1, 5, 2]]).all()
+    assert int(torch.isnan(grad[7]).sum()) == 3
+    assert not loss[9:].any() and not grad[9:].any() and not grad[0, 6:].any() and not grad[1, 30:].any()
+    for rows in ([0, 1], [2]):
+        finite = z[rows] if rows == [2] else torch.where(z[rows] < -1e30, torch.full_like(z[rows], -float("inf")), z[rows])
+        _check_warm((loss[rows], grad[rows]), finite, torch.nan_to_num(a[rows], neginf=-1e9), index[rows], t, w[rows], dtype)
+    want = ref.distill(_np(z[8:9]), _np(a[8:9]), index[8:9].cpu().numpy(), t, _np(w[8:9]))
+    assert abs(float(loss[8]) - want[0][0]) <= 4 * ref.F32_HALF * want[0][0]
+    assert torch.equal(distill.loss(z[8:9], a[8:9], index[8:9], temperature=t, weight=w[8:9]), loss[8:9])
+
+
+def test_high_temperatures_on_streams_and_in_graphs(distill):
+    """Replays among eager work, and two graphs of one input: workspaces of their own, the same bits each time."""
+    cases = [tuple(v.to(DEV) for v in _whole(rows, vocab, 60, F32)) for rows, vocab in ((40, 3000), (2, 70001), (300, 1000))]
+
+    def all_of_it():
+        return [o for z, a, index, w in cases for o in distill.loss_and_gradient(z, a, index, temperature=30.0, weight=w)]
+    want = all_of_it()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = all_of_it()
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, other))
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(all_of_it())
+        graphs.append(g)
+    for turn in range(4):
+        for z, _, _, _ in cases:
+            z.mul_(0.9)
+        want = all_of_it()
+        for g in graphs[::1 if turn % 2 else -1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for out in outs:
+            assert all(torch.equal(x, y) for x, y in zip(want, out)), turn
