@@ -584,10 +584,10 @@ static int launch_distill(const DistillArgs& a, void* workspace, hipStream_t st)
     }
     // by a row's bytes.  A wave, four and sixteen of them (us with the gradient): 16384 x 1000 bf16 23, 37; 8192 x 2048 bf16 19, 23; 8192 x 2048 fp32
     // 36, 30; 4096 x 8192 bf16 35, 28, 48; 8192 x 4096 fp32 77, 54, 81; 4096 x 16384 bf16 -, 50, 60; 4096 x 32000 bf16 -, 112, 107; 64 x 32000 -, 13,
-    // 9.2.  Many entries would take a wave's row too much LDS.
+    // 9.2.  Many entries would take a wave's row too much LDS, and a launch has fewer than 2^32 threads.
     const int64_t bytes = (int64_t)a.vocab * (int64_t)sizeof(T);
     if (bytes <= 4096 && a.n_top <= 256) return launch_rows<T, 64, sizeof(T) == 2 ? 4 : 2, WARM>(a, st);
-    if (bytes <= (a.rows >= 1024 ? 32768 : 16384)) return launch_rows<T, 256, 4, WARM>(a, st);
+    if (bytes <= (a.rows >= 1024 ? 32768 : 16384) || a.rows * 1024 > 0xffffffffll) return launch_rows<T, 256, 4, WARM>(a, st);
     return launch_rows<T, 1024, sizeof(T) == 2 ? 6 : 3, WARM>(a, st);
 }
 

@@ -191,3 +191,22 @@ def test_high_temperatures_on_streams_and_in_graphs(distill):
         torch.cuda.synchronize()
         for out in outs:
             assert all(torch.equal(x, y) for x, y in zip(want, out)), turn
+
+
+def test_as_many_rows_as_there_may_be(distill):
+    """2^22 rows that sixteen waves each would take: more threads than a launch has.  All but the last are padding, which is not looked at."""
+    rows, vocab = 1 << 22, 16400
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("less than 160 GB of memory are free")
+    z = torch.empty(rows, vocab, dtype=BF16, device=DEV)
+    some = torch.randn(3, vocab, generator=torch.Generator().manual_seed(1)).to(BF16).to(DEV)
+    z[-3:] = some
+    a, index = torch.zeros(rows, 2, device=DEV), torch.zeros(rows, 2, dtype=torch.int64, device=DEV)
+    a[-3:, 1], index[-3:, 1] = 1.5, 7
+    w = torch.zeros(rows, device=DEV)
+    w[-3:] = 1
+    losses = distill.loss(z, a, index, temperature=2.0, weight=w)
+    del z
+    torch.cuda.empty_cache()
+    want = distill.loss(some, a[-3:].contiguous(), index[-3:].contiguous(), temperature=2.0)
+    assert not losses[:-3].any() and torch.allclose(losses[-3:], want, rtol=1e-5)
