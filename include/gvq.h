@@ -377,7 +377,10 @@ int gvq_i8_matmul(const void* a_codes, const float* a_scales, const void* b_code
  * A layer with an 8-bit weight: y [rows][n_out] = Q(x) W^T, a scale for each row of x (token) and of W (channel).  Any number of rows,
  * from one token on.  Its gradients: dx [rows][n_in] = Q(dy) Q(W^T)^T, wt_codes and wt_scales W's transpose ([n_in][n_out], the second pair of
  * gvq_i8_quantize); dw [n_out][n_in] = Q(dy^T) Q(x^T)^T (accumulate != 0: added to dw).  dx or dw may be NULL; what only it
- * needs is then not looked at.
+ * needs is then not looked at, and its sum's length has no limit: n_out up to GVQ_MX_MAX without dx, rows up to GVQ_MX_MAX without dw.
+ * Workspace: gvq_i8_linear_backward_workspace for both, enough for either alone.  Where that has no answer, it is for dx alone
+ * gvq_i8_linear_workspace(rows, n_out), and for dw alone gvq_i8_linear_workspace(n_out, rows) + gvq_i8_quantize_workspace(rows, n_out) +
+ * gvq_i8_linear_workspace(n_in, rows) + gvq_i8_quantize_workspace(rows, n_in).
  */
 int64_t gvq_i8_linear_workspace(int64_t rows, int64_t n_in);
 int gvq_i8_linear(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales,
@@ -391,7 +394,8 @@ int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t
  * A gated block's first half: h [rows][n] = act(g) u, [g | u] = Q(x) W^T, W [2 n][n_in] with the gate's rows first.  Workspace:
  * gvq_i8_linear_workspace(rows, n_in).  gvq_i8_gated_gradient: from dh the gradient of the sums, dg [rows][2 n] = [dh u act'(g) | dh act(g)] in x's type, g
  * and u computed anew (the same workspace).  gvq_i8_gated_backward: that, and then the gradients of a layer of 2 n outputs whose dy it is, as
- * gvq_i8_linear_backward gives them: dx, and dw [2 n][n_in]; wt is the transpose of all of W ([n_in][2 n]).
+ * gvq_i8_linear_backward gives them: dx, and dw [2 n][n_in]; wt is the transpose of all of W ([n_in][2 n]).  Its workspace for one of them where
+ * gvq_i8_gated_backward_workspace has no answer: 8 rows n, rounded up to 256, and the larger of the other two calls' (above).
  */
 int gvq_i8_gated(const void* x, gvq_dtype_t dtype, int64_t rows, int64_t n_in, int64_t ld_x, const void* w_codes, const float* w_scales, int64_t n,
                  gvq_activation_t activation, void* h, gvq_dtype_t h_dtype, int64_t ld_h, void* workspace, void* stream);

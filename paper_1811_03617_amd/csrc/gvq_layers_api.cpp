@@ -161,13 +161,14 @@ int64_t gvq_i8_linear_backward_workspace(int64_t rows, int64_t n_in, int64_t n_o
 }
 
 // Whether there is nothing to do, or the arguments are refused: what a backward pass looks at before it begins.  dy: of the layer's outputs, or
-// null where it is about to be made.
+// null where it is about to be made.  Only dx sums the outputs, only dw the rows.
 static int look_at_backward(const void* dy, bool dy_is_given, int64_t ld_dy, const void* x, int64_t ld_x, gvq_dtype_t dtype, int64_t rows, int64_t n_in,
                             int64_t n_out, const void* wt_codes, const float* wt_scales, const void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx,
                             const void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, const void* workspace, bool* nothing)
 {
     *nothing = false;
-    if (!is_dtype(dtype) || (dx && !is_dtype(dx_dtype)) || (dw && !is_dtype(dw_dtype)) || !is_sum(rows) || !in_range(n_in) || !is_sum(n_out))
+    if (!is_dtype(dtype) || (dx && !is_dtype(dx_dtype)) || (dw && !is_dtype(dw_dtype)) || !in_range(rows) || !in_range(n_in) || !in_range(n_out) ||
+        (dw && !is_sum(rows)) || (dx && !is_sum(n_out)))
         return GVQ_EINVAL;
     if (ld_dy < n_out || (dx && ld_dx < n_in) || (dw && (ld_x < n_in || ld_dw < n_in))) return GVQ_EINVAL;
     *nothing = n_in == 0 || (rows == 0 && n_out == 0);
@@ -195,12 +196,15 @@ int gvq_i8_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t
     const Codes none{nullptr, nullptr};
     Codes q = none, qt = none, xt = none;
     if (some) {
-        q = take_matrix(p, rows, n_out);
-        qt = take_matrix(p, n_out, rows);
-        void* y_peaks = p.take(peaks_of(rows, n_out));
-        xt = take_matrix(p, n_in, rows);
-        void* x_peaks = p.take(peaks_of(rows, n_in));
-        const I8QuantArgs both[2] = {matrix(dy, rows, n_out, ld_dy, dx ? q : none, dw ? qt : none, y_peaks), matrix(x, rows, n_in, ld_x, none, xt, x_peaks)};
+        void *y_peaks = nullptr, *x_peaks = nullptr;
+        if (dx) q = take_matrix(p, rows, n_out);
+        if (dw) {
+            qt = take_matrix(p, n_out, rows);
+            y_peaks = p.take(peaks_of(rows, n_out));
+            xt = take_matrix(p, n_in, rows);
+            x_peaks = p.take(peaks_of(rows, n_in));
+        }
+        const I8QuantArgs both[2] = {matrix(dy, rows, n_out, ld_dy, q, qt, y_peaks), matrix(x, rows, n_in, ld_x, none, xt, x_peaks)};
         rc = gvq_launch_i8_quantize(both, dw ? 2 : 1, dtype, (hipStream_t)stream);
         if (rc != GVQ_OK) return rc;
     }
@@ -266,7 +270,7 @@ int gvq_i8_gated_backward(const void* dh, int64_t ld_dh, const void* x, int64_t 
                           void* dx, gvq_dtype_t dx_dtype, int64_t ld_dx, void* dw, gvq_dtype_t dw_dtype, int64_t ld_dw, int accumulate,
                           void* workspace, void* stream)
 {
-    if (n < 0 || n > GVQ_I8_MAX_SUM / 2) return GVQ_EINVAL;
+    if (!in_range(n)) return GVQ_EINVAL;
     bool nothing;
     int rc = look_at_gradient(dh, ld_dh, x, ld_x, dtype, rows, n_in, n, w_codes, w_scales, activation, nullptr, false, 2 * n, workspace);
     if (rc == GVQ_OK)

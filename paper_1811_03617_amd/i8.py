@@ -11,6 +11,7 @@ Tensors are two-dimensional, float32 or bfloat16, with neighbouring elements of 
 device's current stream, and what a call allocates comes from PyTorch's allocator on that stream.  No call records a gradient: one whose
 result would need it is refused (wrap forward and backward in a torch.autograd.Function, where gradients are off).
 """
+import functools
 from typing import NamedTuple
 
 import torch
@@ -121,8 +122,12 @@ def linear(x, w, dtype=None):
     return y
 
 
-def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, x):
-    """(tensor, dtype code, row stride) of dw, given or made."""
+def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, x, need_dx, need_dw):
+    """(tensor, its address, dtype code, row stride) of dw, given or made; of none if it is not needed."""
+    if not need_dw:
+        if dw is not None or accumulate or not need_dx:
+            raise ValueError("need_dw: has to be true where dw is given or added to, or dx is not needed either")
+        return None, None, 0, cols
     if dw is None:
         if accumulate:
             raise ValueError("dw: is needed to add to")
@@ -130,22 +135,34 @@ def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, x):
     code, ld, r, c = _matrix(dw, "dw")
     if (r, c) != (rows, cols):
         raise ValueError(f"dw: shape ({rows}, {cols}) is needed")
-    return dw, code, ld
+    return dw, dw.data_ptr(), code, ld
 
 
-def linear_backward(dy, x, wt, dw=None, accumulate=False, dw_dtype=torch.float32, need_dx=True):
+@functools.lru_cache(maxsize=4096)
+def _backward_bytes(rows, n_in, n_out, need_dx, need_dw):
+    """Of a layer's workspace; what one gradient alone needs knows no limit for the other's sum."""
+    if need_dx and need_dw:
+        return _size("gvq_i8_linear_backward_workspace", rows, n_in, n_out)
+    if need_dx:
+        return _size("gvq_i8_linear_workspace", rows, n_out)
+    return (_size("gvq_i8_linear_workspace", n_out, rows) + _size("gvq_i8_quantize_workspace", rows, n_out) +
+            _size("gvq_i8_linear_workspace", n_in, rows) + _size("gvq_i8_quantize_workspace", rows, n_in))
+
+
+def linear_backward(dy, x, wt, dw=None, accumulate=False, dw_dtype=torch.float32, need_dx=True, need_dw=True):
     """(dx, dw) of `linear`: wt is the weight's transpose with a scale for each of its rows.  dx has x's dtype (None unless needed), dw is
-    given (and added to, if `accumulate`) or made."""
+    given (and added to, if `accumulate`) or made (None unless needed).  dx sums n_out numbers and dw as many as there are rows: up to 131072,
+    of the gradients that are needed."""
     code, ld_dy, rows, n_out = _matrix(dy, "dy")
     code_x, ld_x, rows_x, n_in = _matrix(x, "x")
     if rows_x != rows or code_x != code:
         raise ValueError("x: as many rows as dy, and its dtype, are needed")
     codes, scales = _stored(wt, "wt", n_in, n_out) if need_dx else (None, None)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
-    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, n_out, n_in, x)
-    ws = _space(x, "gvq_i8_linear_backward_workspace", rows, n_in, n_out)
+    dw, at_dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, n_out, n_in, x, need_dx, need_dw)
+    ws = x.new_empty(_backward_bytes(rows, n_in, n_out, need_dx, need_dw), dtype=torch.uint8)
     _check(gvq.lib().gvq_i8_linear_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, code, rows, n_in, n_out, codes, scales,
-                                            None if dx is None else dx.data_ptr(), code, n_in, dw.data_ptr(), code_w, ld_dw,
+                                            None if dx is None else dx.data_ptr(), code, n_in, at_dw, code_w, ld_dw,
                                             int(accumulate), ws.data_ptr(), _now()), "gvq_i8_linear_backward")
     return dx, dw
 
@@ -191,15 +208,18 @@ def gated_gradient(dh, x, w, activation="silu"):
     return dg
 
 
-def gated_backward(dh, x, w, wt, activation="silu", dw=None, accumulate=False, dw_dtype=torch.float32, need_dx=True):
+def gated_backward(dh, x, w, wt, activation="silu", dw=None, accumulate=False, dw_dtype=torch.float32, need_dx=True,
+                   need_dw=True):
     """(dx, dw) of `gated`: linear_backward of gated_gradient.  wt is the transpose of all of w; dx, dw as there, dw of w's shape."""
     act = _activation(activation)
     code, ld_dh, ld_x, rows, n_in, n, codes, scales = _gated_inputs(dh, x, w)
     t_codes, t_scales = _stored(wt, "wt", n_in, 2 * n) if need_dx else (None, None)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
-    dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, 2 * n, n_in, x)
-    ws = _space(x, "gvq_i8_gated_backward_workspace", rows, n_in, n)
+    dw, at_dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, 2 * n, n_in, x, need_dx, need_dw)
+    size = (_size("gvq_i8_gated_backward_workspace", rows, n_in, n) if need_dx and need_dw else
+            (8 * rows * n + 255 & -256) + max(_size("gvq_i8_linear_workspace", rows, n_in), _backward_bytes(rows, n_in, 2 * n, need_dx, need_dw)))
+    ws = x.new_empty(size, dtype=torch.uint8)
     _check(gvq.lib().gvq_i8_gated_backward(dh.data_ptr(), ld_dh, x.data_ptr(), ld_x, code, rows, n_in, n, codes, scales, t_codes, t_scales, act,
-                                           None if dx is None else dx.data_ptr(), code, n_in, dw.data_ptr(), code_w, ld_dw, int(accumulate),
+                                           None if dx is None else dx.data_ptr(), code, n_in, at_dw, code_w, ld_dw, int(accumulate),
                                            ws.data_ptr(), _now()), "gvq_i8_gated_backward")
     return dx, dw
