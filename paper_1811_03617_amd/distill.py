@@ -5,7 +5,7 @@
 For every row, with p = softmax(top / t) over the row's entries and q = softmax(logits / t) over all of the row:
 loss = w t^2 sum_j p_j (log p_j - log q[index_j]), gradient = w t (q - p at its places); t is from 0.001 to 1000.  Everything runs on
 the device's current stream.  No call records a gradient: `loss` refuses logits that need one, `loss_and_gradient` gives it; what the teacher's
-logits or the weights would need is refused by both.
+logits or the weights would need is refused by both, and so is an `out` that needs one, unless it is the logits.
 """
 import torch
 
@@ -32,6 +32,8 @@ def _run(logits, top, index, temperature, weight, grad, want):
         if grad is None:
             grad = logits.new_empty((rows, vocab))
         else:
+            if grad is not logits:
+                _no_graph(grad, "out")
             code_g, ld_grad, rows_g, cols_g = _matrix(grad, "out")
             if (rows_g, cols_g) != (rows, vocab) or code_g != code:
                 raise ValueError("out: the shape and dtype of logits are needed")

@@ -9,7 +9,8 @@ layers (include/gvq.h, `gvq_i8_*`).
 
 Tensors are two-dimensional, float32 or bfloat16, with neighbouring elements of a row next to each other; everything runs on the
 device's current stream, and what a call allocates comes from PyTorch's allocator on that stream.  No call records a gradient: one whose
-result would need it is refused (wrap forward and backward in a torch.autograd.Function, where gradients are off).
+result would need it is refused (wrap forward and backward in a torch.autograd.Function, where gradients are off; a Function's backward
+under create_graph=True has them on).  Quantising a weight that needs one is not refused: what it gives carries none.
 """
 import functools
 from typing import NamedTuple
@@ -39,6 +40,7 @@ def _stored(q, name, rows, cols):
     if (codes.dtype is not torch.int8 or scales.dtype is not torch.float32 or codes.numel() != rows * (cols + 127 & -128) or scales.numel() != rows
             or not codes.is_contiguous() or not scales.is_contiguous() or codes.get_device() != here or scales.get_device() != here):
         raise ValueError(f"{name}: codes and scales are not those of a {rows} x {cols} matrix on the current GPU")
+    _no_graph(scales, name)
     return codes.data_ptr(), scales.data_ptr()
 
 
@@ -101,6 +103,7 @@ def matmul(a, b, dtype=torch.float32, out=None, accumulate=False):
         if accumulate:
             raise ValueError("out: is needed to add to")
         out = torch.empty((m, n), dtype=dtype, device=a.codes.device)
+    _no_graph(out, "out")
     code, ld, rows, cols = _matrix(out, "out")
     if (rows, cols) != (m, n):
         raise ValueError(f"out: shape ({m}, {n}) is needed")
@@ -132,6 +135,7 @@ def _weight_gradient(dw, accumulate, dw_dtype, rows, cols, x, need_dx, need_dw):
         if accumulate:
             raise ValueError("dw: is needed to add to")
         dw = x.new_empty((rows, cols), dtype=dw_dtype)
+    _no_graph(dw, "dw")
     code, ld, r, c = _matrix(dw, "dw")
     if (r, c) != (rows, cols):
         raise ValueError(f"dw: shape ({rows}, {cols}) is needed")
@@ -153,6 +157,8 @@ def linear_backward(dy, x, wt, dw=None, accumulate=False, dw_dtype=torch.float32
     """(dx, dw) of `linear`: wt is the weight's transpose with a scale for each of its rows.  dx has x's dtype (None unless needed), dw is
     given (and added to, if `accumulate`) or made (None unless needed).  dx sums n_out numbers and dw as many as there are rows: up to 131072,
     of the gradients that are needed."""
+    _no_graph(dy, "dy")
+    _no_graph(x, "x")
     code, ld_dy, rows, n_out = _matrix(dy, "dy")
     code_x, ld_x, rows_x, n_in = _matrix(x, "x")
     if rows_x != rows or code_x != code:
@@ -189,6 +195,8 @@ def gated(x, w, activation="silu", dtype=None):
 
 
 def _gated_inputs(dh, x, w):
+    _no_graph(dh, "dh")
+    _no_graph(x, "x")
     code, ld_dh, rows, n = _matrix(dh, "dh")
     code_x, ld_x, rows_x, n_in = _matrix(x, "x")
     if rows_x != rows or code_x != code:
