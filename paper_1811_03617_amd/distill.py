@@ -10,6 +10,7 @@ logits or the weights would need is refused by both, and so is an `out` that nee
 import torch
 
 from . import gvq
+from .i8 import _written
 from .mx import _check, _matrix, _device, _no_graph, _now, _size
 
 
@@ -27,9 +28,9 @@ def _run(logits, top, index, temperature, weight, grad, want):
     if weight is not None and (weight.dtype is not torch.float32 or tuple(weight.shape) != (rows,) or not weight.is_contiguous()
                                or weight.get_device() != _device()):
         raise ValueError(f"weight: float32 of shape ({rows},), contiguous, on the current GPU is needed")
-    ld_grad = vocab
+    ld_grad, given = vocab, grad is not None
     if want:
-        if grad is None:
+        if not given:
             grad = logits.new_empty((rows, vocab))
         else:
             if grad is not logits:
@@ -43,6 +44,8 @@ def _run(logits, top, index, temperature, weight, grad, want):
     _check(gvq.lib().gvq_distill(logits.data_ptr(), code, rows, vocab, ld, top.data_ptr(), code_top, index.data_ptr(), n, ld_top,
                                  s0 if rows > 1 else n, None if weight is None else weight.data_ptr(), temperature, losses.data_ptr(),
                                  grad.data_ptr() if want else None, ld_grad, None if ws is None else ws.data_ptr(), _now()), "gvq_distill")
+    if given:
+        _written(grad)
     return losses, grad
 
 

@@ -53,6 +53,12 @@ def _space(x, name, *sizes):
     return x.new_empty(_size(name, *sizes), dtype=torch.uint8)
 
 
+def _written(t):
+    """Autograd is told that a tensor of the caller's holds other numbers now: a backward pass that kept it will say so."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _activation(name):
     code = _ACTIVATIONS.get(name)
     if code is None:
@@ -99,7 +105,8 @@ def matmul(a, b, dtype=torch.float32, out=None, accumulate=False):
     m, n, k = a.rows, b.rows, a.cols
     a_codes, a_scales = _stored(a, "a", m, k)
     b_codes, b_scales = _stored(b, "b", n, k)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("out: is needed to add to")
         out = torch.empty((m, n), dtype=dtype, device=a.codes.device)
@@ -109,6 +116,8 @@ def matmul(a, b, dtype=torch.float32, out=None, accumulate=False):
         raise ValueError(f"out: shape ({m}, {n}) is needed")
     _check(gvq.lib().gvq_i8_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out.data_ptr(), code, ld, int(accumulate), _now()),
            "gvq_i8_matmul")
+    if given:
+        _written(out)
     return out
 
 
@@ -165,11 +174,14 @@ def linear_backward(dy, x, wt, dw=None, accumulate=False, dw_dtype=torch.float32
         raise ValueError("x: as many rows as dy, and its dtype, are needed")
     codes, scales = _stored(wt, "wt", n_in, n_out) if need_dx else (None, None)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
+    given = dw is not None
     dw, at_dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, n_out, n_in, x, need_dx, need_dw)
     ws = x.new_empty(_backward_bytes(rows, n_in, n_out, need_dx, need_dw), dtype=torch.uint8)
     _check(gvq.lib().gvq_i8_linear_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, code, rows, n_in, n_out, codes, scales,
                                             None if dx is None else dx.data_ptr(), code, n_in, at_dw, code_w, ld_dw,
                                             int(accumulate), ws.data_ptr(), _now()), "gvq_i8_linear_backward")
+    if given:
+        _written(dw)
     return dx, dw
 
 
@@ -223,6 +235,7 @@ def gated_backward(dh, x, w, wt, activation="silu", dw=None, accumulate=False, d
     code, ld_dh, ld_x, rows, n_in, n, codes, scales = _gated_inputs(dh, x, w)
     t_codes, t_scales = _stored(wt, "wt", n_in, 2 * n) if need_dx else (None, None)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
+    given = dw is not None
     dw, at_dw, code_w, ld_dw = _weight_gradient(dw, accumulate, dw_dtype, 2 * n, n_in, x, need_dx, need_dw)
     size = (_size("gvq_i8_gated_backward_workspace", rows, n_in, n) if need_dx and need_dw else
             (8 * rows * n + 255 & -256) + max(_size("gvq_i8_linear_workspace", rows, n_in), _backward_bytes(rows, n_in, 2 * n, need_dx, need_dw)))
@@ -230,4 +243,6 @@ def gated_backward(dh, x, w, wt, activation="silu", dw=None, accumulate=False, d
     _check(gvq.lib().gvq_i8_gated_backward(dh.data_ptr(), ld_dh, x.data_ptr(), ld_x, code, rows, n_in, n, codes, scales, t_codes, t_scales, act,
                                            None if dx is None else dx.data_ptr(), code, n_in, at_dw, code_w, ld_dw, int(accumulate),
                                            ws.data_ptr(), _now()), "gvq_i8_gated_backward")
+    if given:
+        _written(dw)
     return dx, dw

@@ -86,3 +86,33 @@ def test_a_second_derivative_is_refused_and_the_first_is_not():
     with pytest.raises(ValueError):
         torch.autograd.grad(y, (x, w), dy, create_graph=True)
     i8.quantize_both(w)                        # a weight itself is quantised with gradients on
+
+
+def test_what_autograd_kept_is_not_written_unseen():
+    """A tensor that is written into is another one for a backward pass that needs its numbers."""
+    from paper_1811_03617_amd import distill
+    i8, x, dy, dh, q, qt = _case()
+    z, top, index = _numbers(6, 10), _numbers(6, 3), torch.zeros(6, 3, dtype=torch.int64, device=DEV)
+    writes = {
+        "matmul": ((6, 6), lambda t: i8.matmul(q, q, out=t)),
+        "linear_backward": ((6, 10), lambda t: i8.linear_backward(dy, x, qt, dw=t, accumulate=True)),
+        "gated_backward": ((6, 10), lambda t: i8.gated_backward(dh, x, q, None, dw=t, need_dx=False)),
+        "loss_and_gradient": ((6, 10), lambda t: distill.loss_and_gradient(z, top, index, out=t)),
+    }
+    for name, (shape, write) in writes.items():
+        kept, leaf = _numbers(*shape), torch.ones(shape, device=DEV, requires_grad=True)
+        y = (leaf * kept).sum()
+        before = kept._version
+        write(kept)
+        assert kept._version > before, name
+        with pytest.raises(RuntimeError):
+            y.backward()
+    leaf = torch.ones(10, 10, device=DEV, requires_grad=True)
+    logits = z @ leaf
+    y = logits.square().sum()
+    distill.loss_and_gradient(logits, top, index, out=logits)
+    with pytest.raises(RuntimeError):
+        y.backward()
+    with torch.inference_mode():               # tensors that count no versions
+        for name, (shape, write) in writes.items():
+            write(torch.zeros(shape, device=DEV))
