@@ -88,7 +88,7 @@ __device__ __forceinline__ unsigned int i8_pack4(float a, float b, float c, floa
 }
 
 // The gate's activation and its derivative.  gelu: g Phi(g), with Phi(-y) = e^(-y^2/2) t P(t), t = 1 / (1 + y / sqrt(8)), y = |g|.  P is a
-// polynomial fitted here to the least relative error of erfc(x) e^(x^2) / 2t, x = y / sqrt(2) up to 14: 5e-8, 2.5e-7 with fp32's rounding.
+// polynomial fitted here to the least relative error of erfc(x) e^(x^2) / 2t, x = y / sqrt(2) up to 14: 8e-8, 3e-7 with fp32's rounding.
 // Reciprocals and powers of 2 are the instructions', good to a step of the last place.
 struct I8Gelu {
     float phi, bell;   // Phi(g), e^(-g^2/2)

@@ -5,8 +5,9 @@
 // straight into registers: row lane % 16, 16 bytes of 64.  The waves' sums are whole numbers and are added exactly.  Up to four rows of x
 // are quantised by every work-group for itself, into LDS, while the first turns of W are on their way: that costs it one read of x from the
 // caches and saves a launch.  More rows come in codes, 16 or 32 to a work-group.
-// Bound: memory, W once; what a compute unit can have on its way (about 29 bytes a ns) and the latency at both ends for small ones.  One bf16 row through
-// 4096 x 25088 20.2 us (5.1 TB/s of W), through 25088 x 4096 23, through 4096 x 4096 6.2; gated 2 x 8192 x 4096 19; codes of 16 rows through 4096 x 4096 7.1.
+// Bound: memory, W once; what a compute unit can have on its way (about 29 bytes a ns) and the latency at both ends for small ones.  One bf16 row of
+// 25088 numbers into 4096 20.1 us (5.1 TB/s of W), of 4096 into 25088 22.6, of 4096 into 4096 5.0; gated, of 4096 into 2 x 8192, 15.8; codes of 16 rows of 4096 numbers into
+// 4096 6.3.
 #include "gvq_i8.h"
 #include "gvq_tile.h"
 
@@ -349,9 +350,9 @@ static int launch_numbers_mode(const I8ProductArgs& a, const void* x, int64_t ld
     return mode == I8_PLAIN ? launch_rows<X, I8_PLAIN, OUT>(a, x, ld_x, k, st) : launch_rows<X, I8_GATED, OUT>(a, x, ld_x, k, st);
 }
 
-// Against a launch that quantises and another that multiplies (us, one and four bf16 rows): 1000 x 1000 4.1 and 6.2, 4.4 and 6.4; 4096 x 4096 6.2 and 9.4,
-// 6.9 and 10.2; 4096 x 25088 20 and 29, 30 and 31; gated 8192 x 4096 19 and 24, 20 and 25; at worst 25088 x 4096 23 and 22, 24 and 22, where each unit goes
-// through many groups.  At most 64 KB of codes: LDS has to hold them beside as much of sums.
+// Against a launch that quantises and another that multiplies (us, one and four bf16 rows, numbers in and out): 1000, 1000 4.0 and 6.1, 4.4 and 6.4; 4096, 4096 5.0
+// and 7.9, 5.6 and 8.4; 25088, 4096 20 and 29, 30.5 and 30.4; gated 4096, 8192 15.8 and 19.8, 16.8 and 20.2; at worst 4096, 25088 22.7 and 21.7, 24.0 and 22.1, where
+// each unit goes through many groups.  At most 64 KB of codes: LDS has to hold them beside as much of sums.
 bool gvq_i8_few_numbers_takes(const void* x, gvq_dtype_t x_dtype, int64_t rows, int64_t ld_x, int64_t k, I8Mode mode)
 {
     const int64_t row = rows > 1 ? ld_x * (x_dtype == GVQ_BF16 ? 2 : 4) : 0;   // a single row is aligned where it begins

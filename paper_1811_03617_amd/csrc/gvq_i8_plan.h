@@ -4,7 +4,10 @@
 
 // A way's time: rounds over 256 compute units, of up to `share` work-groups a unit; each round has a start and so much a step (128 numbers
 // of the sum), more for every work-group that shares the unit.  Fitted to 263 products (17 to 4096 rows, 256 to 25088 columns, sums of 384 to
-// 16384) that were each measured in all ways: what is picked is 1.2 % behind the fastest on average, four in a hundred more than 10 %, one 44 %.
+// 16384) that were each measured in all ways: what is picked is 1.2 % behind the fastest of them on average, four in a hundred more than 10 %, one 44 %.
+// How far the fastest of them is from what the card could do is another matter: none shares a sum among work-groups, and 46 of the 263, those of few
+// results and long sums, take more than three times the time of their bytes, their operations or a launch (500 x 256 x 16384 24 to 33 us of 3.5, 64 x
+// 64 x 131072, beyond what was fitted, 114 of 3.5).
 // Without the tiles whose sums two or four teams share the fastest of the others is 9 % behind on average; 64 x 64 with more stages, 128 x 128 with two
 // teams and 128 x 64 with three would add 0.4 % and are not built.
 struct I8Way {
